@@ -34,7 +34,8 @@
  *    channels.  G = d_out / n packed kernels.
  *  - Integer path: int8 activations and weights, int32 accumulation and bias
  *    (Section 4: weights and activations quantised to 8 bits).  Float path:
- *    fp32 throughout.  Integer sums wrap modulo 2^32 on overflow (the
+ *    fp32 throughout (CS_F16 and CS_BF16 are types of the 8-bit attention
+ *    operators alone; every other call refuses them).  Integer sums wrap modulo 2^32 on overflow (the
  *    configurations used stay below 2^31 by a wide margin).
  */
 #ifndef CS_H_
@@ -58,7 +59,7 @@ typedef enum {
   CS_ERR_UNSUPPORTED = -7 /* not available in this build of the library          */
 } cs_status;
 
-typedef enum { CS_I8 = 0, CS_I32 = 1, CS_F32 = 2 } cs_dtype;
+typedef enum { CS_I8 = 0, CS_I32 = 1, CS_F32 = 2, CS_F16 = 3, CS_BF16 = 4 } cs_dtype;
 
 /* Supported limits (checked, CS_ERR_SHAPE beyond them). */
 #define CS_MAX_ROW 65535   /* row length / c_in: indices are stored as uint16  */
@@ -711,6 +712,150 @@ int cs_kwta_lists(cs_dtype it, const void* in, int64_t rows, int c, int k, cs_dt
  * xt.  Returns 0 for invalid arguments.  Host only.
  */
 size_t cs_workspace_bytes(int op, cs_dtype xt, int64_t rows, int c_in);
+
+/*
+ * 8-bit operators of a transformer's attention layer
+ * --------------------------------------------------
+ * Floats of these calls are CS_F32, CS_F16 (IEEE half) or CS_BF16; sums,
+ * softmax statistics and scales are 32 bits wide whatever their type, and a
+ * result is rounded to it once.  Rows may be strided: ld* is the distance of
+ * two rows and hs* that of two heads, in elements; a row's own elements are
+ * contiguous.  Vector loads are used where pointers and strides are multiples
+ * of 16 bytes, single elements elsewhere, with the same results.
+ *
+ * Codes: a row of floats is held as int8 codes with one scale,
+ * s = fl32(max|x| / 127), code = rne(fl32(x / s)) (fl32: rounded to 32 bits,
+ * rne: to the nearest integer, ties to even) in [-127, 127]; value = code * s.
+ * A row whose s is 0 has codes 0; a row with an infinity or a NaN has scale
+ * NaN and codes 0, so that what is computed from it is NaN.
+ */
+
+/* Limit of k in cs_linear_q8: 131,072 products of two codes fit int32. */
+#define CS_MAX_Q8_K 131072
+
+/*
+ * cs_quantise_rows - codes and scales of the rows of a float matrix (tokens
+ * before a product; a weight matrix, once).  DEVICE memory.
+ *  xt      CS_F32, CS_F16 or CS_BF16.  x device [rows][c], row stride ldx >= c.
+ *  q       device [rows][c] out, row stride ldq >= c (bytes between c and ldq
+ *          are left alone); 8-byte stores where rows start on 8 bytes.
+ *  scale   device [rows] out.  rows may be 0.
+ *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (a stride below c, more than
+ *  2^31 - 1 rows), CS_ERR_DEVICE.
+ */
+int cs_quantise_rows(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int c, int8_t* q,
+                     int64_t ldq, float* scale, void* stream);
+
+/*
+ * cs_linear_q8 - a dense linear layer on 8-bit codes:
+ * y[t][n] = (sum_k x[t][k] w[n][k]) * (sx[t] * sw[n]) + bias[n], the sum exact
+ * in int32.  DEVICE memory.
+ *  xt      CS_I8: x holds codes with scales sx.  CS_F32, CS_F16 or CS_BF16: x
+ *          holds floats, sx is NULL, and the call first gives every row codes
+ *          and a scale as cs_quantise_rows does, in ws.
+ *  x       device [rows][k], row stride ldx >= k; sx device [rows].
+ *  w       device [d_out][k] codes, row stride ldw >= k; sw device [d_out].
+ *  bias    device [d_out] float or NULL.
+ *  yt, y   CS_F32, CS_F16 or CS_BF16; device [rows][d_out] out, row stride
+ *          ldy >= d_out.  rows may be 0.
+ *  ws      device, 16-byte aligned, cs_linear_q8_workspace_bytes bytes (may be
+ *          NULL where that is 0); undefined afterwards.
+ *  Rows of x and w that start on 16 bytes are staged 16 bytes at a time; pad
+ *  the row stride of an odd k to a multiple of 16 to have that.
+ *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (a stride below its row,
+ *  k > CS_MAX_Q8_K, more than 2^31 - 1 rows), CS_ERR_WORKSPACE, CS_ERR_DEVICE.
+ */
+int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64_t rows, int k,
+                 const int8_t* w, int64_t ldw, const float* sw, int d_out, const float* bias,
+                 cs_dtype yt, void* y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+
+/* cs_linear_q8_workspace_bytes - workspace of cs_linear_q8 (0 for invalid
+ * arguments too).  Host only. */
+size_t cs_linear_q8_workspace_bytes(cs_dtype xt, int64_t rows, int k, int d_out);
+
+/*
+ * A paged cache of keys and values in 8 bits: per page and head, `page` rows
+ * of d codes, and a scale per row.  Slot s is offset s % page of page
+ * s / page.  Every array is the caller's device memory, codes 16-byte aligned.
+ *  page    tokens of a page: a power of two from 16 to 1024.
+ *  d       channels of a head: a multiple of 16 up to 256.
+ *  pages * page is at most 2^31 - 1.
+ */
+typedef struct {
+  int8_t* k;       /* [pages][heads][page][d] */
+  int8_t* v;       /* [pages][heads][page][d] */
+  float* k_scale;  /* [pages][heads][page]    */
+  float* v_scale;  /* [pages][heads][page]    */
+  int pages, heads, page, d;
+} cs_q8_cache;
+
+/*
+ * cs_cache_write - quantise new tokens' keys and values into the cache, a
+ * scale per token and head.  DEVICE memory (the cs_q8_cache itself is host
+ * memory, read before the call returns).
+ *  xt      CS_F32, CS_F16 or CS_BF16.
+ *  k, v    device [tokens][heads][d], token strides ldk, ldv, head strides
+ *          hsk, hsv >= d.
+ *  slots   device [tokens]: each token's slot; a slot below 0 or past the cache
+ *          leaves its token out.  The slots of one call that are in the cache
+ *          must differ.  tokens may be 0.
+ *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (cache geometry, strides,
+ *  tokens * heads over 2^31 - 1), CS_ERR_DEVICE.
+ */
+int cs_cache_write(const cs_q8_cache* cache, cs_dtype xt, const void* k, int64_t ldk, int64_t hsk,
+                   const void* v, int64_t ldv, int64_t hsv, const int64_t* slots, int64_t tokens,
+                   void* stream);
+
+/*
+ * cs_cache_read - the values code * scale of the slots' tokens.  DEVICE memory.
+ *  slots   device [tokens], any order, repeats allowed; a slot below 0 or past
+ *          the cache reads as zeros.  tokens may be 0.
+ *  yt      CS_F32, CS_F16 or CS_BF16; k, v device [tokens][heads][d] out
+ *          (dense, 16-byte aligned).
+ *  Errors: as cs_cache_write.
+ */
+int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens, cs_dtype yt,
+                  void* k, void* v, void* stream);
+
+/*
+ * cs_paged_attention - attention of a chunk of new tokens of each sequence
+ * over the cache, in which the new tokens' own keys and values already are.
+ * New token i of sequence b is at position p = lens[b] - n_b + i (n_b =
+ * starts[b+1] - starts[b] new tokens) and sees the positions from
+ * max(0, p - window + 1) (0 without a window) to p:
+ * o = sum_j softmax_j(scale * q.k_j) v_j.  Query head h reads the cache's head
+ * h / (q_heads / heads).  A token that sees nothing (p < 0) has o = 0.
+ * DEVICE memory, the cs_q8_cache excepted.
+ *  qt      CS_F32, CS_F16 or CS_BF16: type of q and out.
+ *  q       device [tokens][q_heads][d], token stride ldq, head stride hsq >= d.
+ *  table   device int32 [batch][table_width]: page numbers of each sequence's
+ *          positions, page after page; a number outside the cache hides its
+ *          positions.
+ *  lens    device int32 [batch]: positions of each sequence, its new tokens
+ *          included; more than table_width pages hold is cut to that.
+ *  starts  device int32 [batch + 1]: ascending, starts[0] = 0; sequence b's new
+ *          tokens are starts[b] .. starts[b+1] - 1 of q.  Tokens past the last
+ *          sequence get zeros (a batch padded to a fixed size).
+ *  max_len what the work is split by: the longest of lens as far as the caller
+ *          knows, 0 for table_width pages.  Any value gives right results.
+ *  scale   finite, > 0.  window >= 0 (0: none).
+ *  out     device [tokens][q_heads][d] out (dense).  tokens may be 0.
+ *  ws      device, 16-byte aligned, cs_paged_attention_workspace_bytes bytes
+ *          (may be NULL where that is 0); undefined afterwards.
+ *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (cache geometry, strides,
+ *  q_heads not a multiple of heads, tokens * q_heads over 2^31 - 1),
+ *  CS_ERR_WORKSPACE, CS_ERR_DEVICE.
+ */
+int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
+                       int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,
+                       int table_width, const int32_t* lens, const int32_t* starts, int max_len,
+                       float scale, int window, void* out, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* cs_paged_attention_workspace_bytes - workspace of cs_paged_attention (0 for
+ * invalid arguments too).  Host only. */
+size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt, int tokens,
+                                          int q_heads, int batch, int table_width, int max_len);
 
 /*
  * cs_product_count - the number of weight x activation products the

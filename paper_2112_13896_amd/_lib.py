@@ -22,16 +22,26 @@ CS_ERR_WORKSPACE = -5
 CS_ERR_DEVICE = -6
 CS_ERR_UNSUPPORTED = -7
 
-CS_I8, CS_I32, CS_F32 = 0, 1, 2
+CS_I8, CS_I32, CS_F32, CS_F16, CS_BF16 = 0, 1, 2, 3, 4
 
 CS_MAX_ROW = 65535
 CS_MAX_N = 32
 CS_MAX_KWTA_ROW = 2048
 CS_NOALLOC_SCRATCH_BYTES = 64 << 20
+CS_MAX_Q8_K = 131072
 
 # name -> (restype, argtypes), in the order of include/cs.h
 _c = ctypes
 _vp, _i, _i64, _sz = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_size_t
+
+
+class Q8Cache(ctypes.Structure):
+    """cs_q8_cache"""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _i),
+                ("heads", _i), ("page", _i), ("d", _i)]
+
+
+_cache = _c.POINTER(Q8Cache)
 SIGNATURES = {
     "cs_pack": (_i, [_i, _vp, _i, _i, _i, _vp, _c.POINTER(_i64), _c.POINTER(_i), _c.POINTER(_i)]),
     "cs_compact": (_i, [_i, _vp, _i64, _i, _vp, _vp, _vp, _vp]),
@@ -84,6 +94,15 @@ SIGNATURES = {
     "cs_kwta": (_i, [_i, _vp, _i64, _i, _i, _i, _i, _vp, _vp]),
     "cs_kwta_lists": (_i, [_i, _vp, _i64, _i, _i, _i, _i, _vp, _vp, _vp, _i, _vp]),
     "cs_workspace_bytes": (_sz, [_i, _i, _i64, _i]),
+    "cs_quantise_rows": (_i, [_i, _vp, _i64, _i64, _i, _vp, _i64, _vp, _vp]),
+    "cs_linear_q8": (_i, [_i, _vp, _i64, _vp, _i64, _i, _vp, _i64, _vp, _i, _vp, _i, _vp, _i64,
+                          _vp, _sz, _vp]),
+    "cs_linear_q8_workspace_bytes": (_sz, [_i, _i64, _i, _i]),
+    "cs_cache_write": (_i, [_cache, _i, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp]),
+    "cs_cache_read": (_i, [_cache, _vp, _i64, _i, _vp, _vp, _vp]),
+    "cs_paged_attention": (_i, [_cache, _i, _vp, _i64, _i64, _i, _i, _i, _vp, _i, _vp, _vp, _i,
+                                _c.c_float, _i, _vp, _vp, _sz, _vp]),
+    "cs_paged_attention_workspace_bytes": (_sz, [_cache, _i, _i, _i, _i, _i, _i]),
     "cs_product_count": (_i, [_c.POINTER(_c.c_ulonglong), _i]),
     "cs_phase_stamps": (_i, [_c.POINTER(_c.c_ulonglong), _i, _i, _c.POINTER(_c.c_int)]),
     "cs_status_str": (_c.c_char_p, [_i]),

@@ -2,10 +2,12 @@
 
     python -m paper_2112_13896_amd.build
 
-Compiles the HIP kernels and C ABI (csrc/cs_api.hip) and the host pack
-routine (csrc/cs_pack.cpp) with hipcc, once as the product library and once
-with the product counter compiled in (libcs_count.so, used by tests).  Packed-fp32 instruction generation is
-switched off for all device code.
+Compiles the HIP kernels and C ABI (csrc/cs_api.hip, the sparse layers;
+csrc/q8_api.hip, the 8-bit attention-layer operators) and the host pack
+routine (csrc/cs_pack.cpp) with hipcc and links them, once as the product
+library and once with the product counter compiled in (libcs_count.so, used by
+tests).  Packed-fp32 instruction generation is switched off for all device
+code.
 """
 from __future__ import annotations
 
@@ -13,6 +15,7 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -34,7 +37,8 @@ def hipcc() -> str:
 
 
 def sources() -> list:
-    return [os.path.join(CSRC, "cs_api.hip"), os.path.join(CSRC, "cs_pack.cpp")]
+    """Translation units; only the first knows the instrumented builds' defines."""
+    return [os.path.join(CSRC, f) for f in ("cs_api.hip", "q8_api.hip", "cs_pack.cpp")]
 
 
 def source_digest() -> str:
@@ -50,44 +54,64 @@ def source_digest() -> str:
     return h.hexdigest()
 
 
-def _cmd(out: str, extra: list) -> list:
-    return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
-            "-Wall", "-Wno-unused-command-line-argument", *DEVICE_FLAGS, "-I", INCLUDE, "-I", CSRC,
-            *extra, "-o", out, *sources()]
+def _compile(src: str, out: str, extra: list) -> list:
+    return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-c", "-Wall",
+            "-Wno-unused-command-line-argument", *DEVICE_FLAGS, "-I", INCLUDE, "-I", CSRC, *extra,
+            "-o", out, src]
 
 
-def build(verbose: bool = False, extra: list | None = None, counting: bool = True) -> str:
-    """Compile libcs.so (always recompiles) and, with `counting`, the two
-    instrumented builds: libcs_count.so (every multiply-route-sum kernel counts
-    the products it forms; tests only) and libcs_stamps.so (phase stamps; the
-    benchmark's phase report), the compilations side by side.  Returns the
-    path of libcs.so."""
-    jobs = [(LIB, list(extra or []))]
-    if counting:
-        jobs.append((COUNT_LIB, list(extra or []) + ["-DCS_COUNT_PRODUCTS"]))
-        jobs.append((STAMP_LIB, list(extra or []) + ["-DCS_PHASE_STAMPS"]))
+def _link(out: str, objects: list) -> list:
+    return [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", "-o", out, *objects]
+
+
+def _run(cmds: list, verbose: bool) -> None:
+    """The commands side by side; raises when one fails, after all have ended."""
     procs = []
-    for out, ex in jobs:
-        cmd = _cmd(out + ".tmp", ex)
+    for cmd in cmds:
         if verbose:
             print(" ".join(cmd), flush=True)
-        procs.append((out, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
+        procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
                                             text=True)))
     failed = None
     noise = "is not a recognized feature for this target"
-    for out, p in procs:
+    for cmd, p in procs:
         text = p.communicate()[0]
         if p.returncode != 0:
             sys.stderr.write(text)
-            failed = failed or f"hipcc failed with exit code {p.returncode} ({os.path.basename(out)})"
+            failed = failed or (f"hipcc failed with exit code {p.returncode} "
+                                f"({os.path.basename(cmd[cmd.index('-o') + 1])})")
             continue
         msgs = [ln for ln in text.splitlines() if noise not in ln and ln.strip()]
         if msgs and verbose:
             print("\n".join(msgs))
     if failed:
         raise RuntimeError(failed)
-    for out, _ in procs:
-        os.replace(out + ".tmp", out)
+
+
+def build(verbose: bool = False, extra: list | None = None, counting: bool = True) -> str:
+    """Compile libcs.so (always recompiles) and, with `counting`, the two
+    instrumented builds: libcs_count.so (every multiply-route-sum kernel counts
+    the products it forms; tests only) and libcs_stamps.so (phase stamps; the
+    benchmark's phase report), the compilations side by side.  The other two
+    sources know neither define: the three libraries share their objects.
+    Returns the path of libcs.so."""
+    extra = list(extra or [])
+    libs = [(LIB, [])]
+    if counting:
+        libs += [(COUNT_LIB, ["-DCS_COUNT_PRODUCTS"]), (STAMP_LIB, ["-DCS_PHASE_STAMPS"])]
+    api, *shared = sources()
+    with tempfile.TemporaryDirectory(prefix="cs_build_") as tmp:
+        cmds, links = [], []
+        common = [os.path.join(tmp, os.path.basename(s) + ".o") for s in shared]
+        for i, (lib, define) in enumerate(libs):
+            obj = os.path.join(tmp, f"{i}.o")
+            cmds.append(_compile(api, obj, extra + define))
+            links.append(_link(lib + ".tmp", [obj, *common]))
+        cmds += [_compile(s, o, extra) for s, o in zip(shared, common)]
+        _run(cmds, verbose)
+        _run(links, verbose)
+    for lib, _ in libs:
+        os.replace(lib + ".tmp", lib)
     return LIB
 
 

@@ -1,0 +1,228 @@
+// C ABI entry points of the 8-bit attention-layer operators (declared in
+// include/cs.h).  Every argument is checked on the host before the first HIP
+// call; kernels are enqueued on the caller's stream and nothing is allocated,
+// freed or synchronised here.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "cs.h"
+#include "q8_attention.h"
+#include "q8_linear.h"
+#include "q8_rows.h"
+
+namespace {
+
+constexpr int64_t kMaxCount = 0x7FFFFFFF;
+
+size_t float_size(cs_dtype t) { return t == CS_F32 ? 4 : 2; }
+bool is_float(cs_dtype t) { return t == CS_F32 || t == CS_F16 || t == CS_BF16; }
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+size_t round_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
+
+int launched() { return hipGetLastError() == hipSuccess ? CS_OK : CS_ERR_DEVICE; }
+
+// f(T{}) with the C++ type of a float dtype.
+template <typename F>
+int with_float(cs_dtype t, F f) {
+  if (t == CS_F32) return f(float{});
+  if (t == CS_F16) return f(_Float16{});
+  return f(__bf16{});
+}
+
+// ---------------------------------------------------------------- rows
+template <typename T, int WPR>
+int quantise_launch(const T* x, int64_t ldx, int64_t rows, int c, int8_t* q, int64_t ldq,
+                    float* scale, hipStream_t s) {
+  const dim3 grid((unsigned)((rows * WPR + 3) / 4)), block(256);
+  if (aligned(x, 16) && (rows == 1 || ldx * sizeof(T) % 16 == 0))
+    hipLaunchKernelGGL((cs::quantise_rows<T, true, WPR>), grid, block, 0, s, x, ldx, rows, c, q,
+                       ldq, scale);
+  else
+    hipLaunchKernelGGL((cs::quantise_rows<T, false, WPR>), grid, block, 0, s, x, ldx, rows, c, q,
+                       ldq, scale);
+  return launched();
+}
+
+int quantise(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int c, int8_t* q, int64_t ldq,
+             float* scale, hipStream_t s) {
+  return with_float(xt, [&](auto t) {
+    using T = decltype(t);
+    const T* p = static_cast<const T*>(x);
+    // one wavefront holds rows of up to 2,048 elements in registers, a workgroup longer ones
+    if (c <= 64 * 8 * cs::kRowHeld)
+      return quantise_launch<T, 1>(p, ldx, rows, c, q, ldq, scale, s);
+    return quantise_launch<T, 4>(p, ldx, rows, c, q, ldq, scale, s);
+  });
+}
+
+// ---------------------------------------------------------------- cache
+int cache_view(const cs_q8_cache* c, cs::CacheView* out) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return CS_ERR_ARG;
+  if (c->pages < 1 || c->heads < 1 || c->page < 1 || c->d < 1) return CS_ERR_ARG;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) ||
+      !aligned(c->v_scale, 4))
+    return CS_ERR_ARG;
+  if (c->d % 16 != 0 || c->d > 256) return CS_ERR_SHAPE;
+  if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)) != 0) return CS_ERR_SHAPE;
+  if ((int64_t)c->pages * c->page > kMaxCount) return CS_ERR_SHAPE;
+  int lg = 4;
+  while ((1 << lg) < c->page) ++lg;
+  *out = {c->k, c->v, c->k_scale, c->v_scale, (int64_t)c->pages * c->page, c->heads, lg, c->d};
+  return CS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int cs_quantise_rows(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int c, int8_t* q,
+                     int64_t ldq, float* scale, void* stream) {
+  if (!is_float(xt)) return CS_ERR_DTYPE;
+  if (rows < 0 || c < 1) return CS_ERR_ARG;
+  if (rows == 0) return CS_OK;
+  if (!x || !q || !scale || !aligned(x, float_size(xt)) || !aligned(scale, 4)) return CS_ERR_ARG;
+  if (ldx < c || ldq < c || rows > kMaxCount) return CS_ERR_SHAPE;
+  return quantise(xt, x, ldx, rows, c, q, ldq, scale, static_cast<hipStream_t>(stream));
+}
+
+size_t cs_linear_q8_workspace_bytes(cs_dtype xt, int64_t rows, int k, int d_out) {
+  if (rows < 1 || rows > kMaxCount || k < 1 || k > CS_MAX_Q8_K || d_out < 1) return 0;
+  if (!is_float(xt)) return 0;
+  return round_up((size_t)rows * round_up((size_t)k, 16) + (size_t)rows * 4, 256);
+}
+
+int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64_t rows, int k,
+                 const int8_t* w, int64_t ldw, const float* sw, int d_out, const float* bias,
+                 cs_dtype yt, void* y, int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
+  if (!(is_float(xt) || xt == CS_I8) || !is_float(yt)) return CS_ERR_DTYPE;
+  if (rows < 0 || k < 1 || d_out < 1) return CS_ERR_ARG;
+  if (rows == 0) return CS_OK;
+  if (!x || !w || !sw || !y || (xt == CS_I8) != (sx != nullptr)) return CS_ERR_ARG;
+  if ((is_float(xt) && !aligned(x, float_size(xt))) || !aligned(y, float_size(yt)) ||
+      !aligned(sx, 4) || !aligned(sw, 4) || !aligned(bias, 4))
+    return CS_ERR_ARG;
+  if (k > CS_MAX_Q8_K || rows > kMaxCount || ldx < k || ldw < k || ldy < d_out)
+    return CS_ERR_SHAPE;
+  const size_t need = cs_linear_q8_workspace_bytes(xt, rows, k, d_out);
+  if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  cs::Q8Linear a{static_cast<const int8_t*>(x), ldx, sx, rows, k, w, ldw, sw, d_out, bias, y, ldy};
+  if (is_float(xt)) {
+    const int64_t ld = (int64_t)round_up((size_t)k, 16);
+    int8_t* q = static_cast<int8_t*>(ws);
+    float* sq = reinterpret_cast<float*>(q + rows * ld);
+    const int st = quantise(xt, x, ldx, rows, k, q, ld, sq, s);
+    if (st != CS_OK) return st;
+    a.x = q; a.ldx = ld; a.sx = sq;
+  }
+  const int64_t tiles_t = (rows + 63) / 64;
+  if (tiles_t > 65535) return CS_ERR_SHAPE;
+  const dim3 grid((unsigned)((d_out + 63) / 64), (unsigned)tiles_t), block(256);
+  const bool al = aligned(a.x, 16) && aligned(w, 16) && a.ldx % 16 == 0 && ldw % 16 == 0;
+  return with_float(yt, [&](auto t) {
+    using T = decltype(t);
+    if (al) hipLaunchKernelGGL((cs::linear_q8_tile<T, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((cs::linear_q8_tile<T, false>), grid, block, 0, s, a);
+    return launched();
+  });
+}
+
+int cs_cache_write(const cs_q8_cache* cache, cs_dtype xt, const void* k, int64_t ldk, int64_t hsk,
+                   const void* v, int64_t ldv, int64_t hsv, const int64_t* slots, int64_t tokens,
+                   void* stream) {
+  if (!is_float(xt)) return CS_ERR_DTYPE;
+  cs::CacheView c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 0) return CS_ERR_ARG;
+  if (tokens == 0) return CS_OK;
+  if (!k || !v || !slots || !aligned(k, float_size(xt)) || !aligned(v, float_size(xt)) ||
+      !aligned(slots, 8))
+    return CS_ERR_ARG;
+  if (ldk < 0 || ldv < 0 || hsk < c.d || hsv < c.d) return CS_ERR_SHAPE;
+  if (tokens > kMaxCount / c.heads) return CS_ERR_SHAPE;
+  const uint32_t rows = (uint32_t)(tokens * c.heads);
+  const dim3 grid((rows + 15) / 16, 2), block(256);
+  return with_float(xt, [&](auto t) {
+    using T = decltype(t);
+    const int64_t e = sizeof(T);
+    const bool vec = aligned(k, 16) && aligned(v, 16) && ldk * e % 16 == 0 && ldv * e % 16 == 0 &&
+                     hsk * e % 16 == 0 && hsv * e % 16 == 0;
+    const cs::FastDiv by = cs::make_fastdiv((uint32_t)c.heads);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (vec)
+      hipLaunchKernelGGL((cs::cache_write<T, true>), grid, block, 0, s, c,
+                         static_cast<const T*>(k), ldk, hsk, static_cast<const T*>(v), ldv, hsv,
+                         slots, rows, by);
+    else
+      hipLaunchKernelGGL((cs::cache_write<T, false>), grid, block, 0, s, c,
+                         static_cast<const T*>(k), ldk, hsk, static_cast<const T*>(v), ldv, hsv,
+                         slots, rows, by);
+    return launched();
+  });
+}
+
+int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens, cs_dtype yt,
+                  void* k, void* v, void* stream) {
+  if (!is_float(yt)) return CS_ERR_DTYPE;
+  cs::CacheView c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 0) return CS_ERR_ARG;
+  if (tokens == 0) return CS_OK;
+  if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8))
+    return CS_ERR_ARG;
+  if (tokens > kMaxCount / c.heads) return CS_ERR_SHAPE;
+  const uint32_t rows = (uint32_t)(tokens * c.heads);
+  const dim3 grid((rows + 15) / 16, 2), block(256);
+  return with_float(yt, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL((cs::cache_read<T>), grid, block, 0, static_cast<hipStream_t>(stream), c,
+                       slots, rows, cs::make_fastdiv((uint32_t)c.heads), static_cast<T*>(k),
+                       static_cast<T*>(v));
+    return launched();
+  });
+}
+
+size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt, int tokens,
+                                          int q_heads, int batch, int table_width, int max_len) {
+  return 0;
+}
+
+int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
+                       int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,
+                       int table_width, const int32_t* lens, const int32_t* starts, int max_len,
+                       float scale, int window, void* out, void* ws, size_t ws_bytes,
+                       void* stream) {
+  if (!is_float(qt)) return CS_ERR_DTYPE;
+  cs::CacheView c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 0 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0 || window < 0)
+    return CS_ERR_ARG;
+  if (!(scale > 0.0f) || std::isinf(scale)) return CS_ERR_ARG;
+  if (tokens == 0) return CS_OK;
+  if (!q || !table || !lens || !starts || !out || !aligned(q, float_size(qt)) ||
+      !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4))
+    return CS_ERR_ARG;
+  if (q_heads % c.heads != 0 || ldq < 0 || hsq < c.d) return CS_ERR_SHAPE;
+  if ((int64_t)tokens * q_heads > kMaxCount) return CS_ERR_SHAPE;
+  if (((int64_t)table_width << c.page_log) > kMaxCount) return CS_ERR_SHAPE;
+  const size_t need = cs_paged_attention_workspace_bytes(cache, qt, tokens, q_heads, batch,
+                                                         table_width, max_len);
+  if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
+  const cs::PagedAttention a{c, q, ldq, hsq, tokens, q_heads, batch, table, table_width, lens,
+                             starts, scale, window, out};
+  const dim3 grid((unsigned)(((int64_t)tokens * q_heads + 3) / 4)), block(256);
+  return with_float(qt, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL((cs::attention_row<T>), grid, block, 0, static_cast<hipStream_t>(stream),
+                       a);
+    return launched();
+  });
+}
+
+}  // extern "C"

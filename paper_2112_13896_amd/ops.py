@@ -8,12 +8,14 @@ host and have no fallback.
 from __future__ import annotations
 
 import ctypes
+import math
+from dataclasses import dataclass
 
 import numpy as np
 import torch
 
 from . import _lib
-from ._lib import CS_F32, CS_I8, CS_I32, check, lib
+from ._lib import CS_BF16, CS_F16, CS_F32, CS_I8, CS_I32, check, lib
 
 _TORCH_DT = {torch.int8: CS_I8, torch.int32: CS_I32, torch.float32: CS_F32}
 _NP_DT = {np.dtype(np.int8): CS_I8, np.dtype(np.float32): CS_F32}
@@ -830,3 +832,225 @@ def kwta_lists(x: torch.Tensor, k: int, out_dtype: torch.dtype | None = None, sh
         _dt(x), _dev(x, "x"), rows, c, k, _TORCH_DT[odt], shift, _dev(idx, "idx"),
         _dev(val, "val"), _dev(cnt, "cnt"), cap, _stream()))
     return idx, val, cnt
+
+
+# ------------------------------------------------- 8-bit attention-layer operators
+_FLOAT_DT = {torch.float32: CS_F32, torch.float16: CS_F16, torch.bfloat16: CS_BF16}
+
+
+def _float_dt(t: torch.dtype) -> int:
+    try:
+        return _FLOAT_DT[t]
+    except KeyError:
+        raise TypeError(f"unsupported dtype {t}") from None
+
+
+def _rows(t: torch.Tensor, name: str):
+    """Device pointer and row stride of a GPU matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _heads(t: torch.Tensor, name: str):
+    """Device pointer, token stride and head stride of a GPU tensor [tokens][heads][d]."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens][heads][d]")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}'s heads must be contiguous")
+    hs = t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * hs, hs
+
+
+def _vector(t: torch.Tensor | None, name: str, dtype: torch.dtype, n: int):
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != (n,):
+        raise ValueError(f"{name} must be {dtype} [{n}]")
+    return _dev(t, name)
+
+
+def _ws(ws: torch.Tensor | None, need: int, device):
+    """Pointer and size of a workspace, one made for the call where the caller keeps none
+    (torch's allocator orders its reuse on the stream)."""
+    if ws is None:
+        ws = torch.empty((need,), dtype=torch.uint8, device=device)
+    return ws, _dev(ws, "ws"), ws.numel() * ws.element_size()
+
+
+def quantise_rows(x: torch.Tensor, q: torch.Tensor | None = None,
+                  scale: torch.Tensor | None = None):
+    """Codes int8 [rows][c] and scales float32 [rows] of the rows of x (float32, float16 or
+    bfloat16 [rows][c]): cs_quantise_rows.  Codes made here have a row stride that is a multiple
+    of 16, which cs_linear_q8 reads fastest."""
+    px, ldx = _rows(x, "x")
+    rows, c = x.shape
+    if q is None:
+        q = torch.empty((rows, (c + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :c]
+    if q.dtype != torch.int8 or q.shape != x.shape:
+        raise ValueError("q must be int8 of x's shape")
+    if scale is None:
+        scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    pq, ldq = _rows(q, "q")
+    check("cs_quantise_rows", lib().cs_quantise_rows(
+        _float_dt(x.dtype), px, ldx, rows, c, pq, ldq,
+        _vector(scale, "scale", torch.float32, rows), _stream()))
+    return q, scale
+
+
+def linear_q8_workspace(dtype: torch.dtype, rows: int, k: int, d_out: int,
+                        device="cuda") -> torch.Tensor:
+    """Workspace of linear_q8 for inputs of up to `rows` rows of this dtype."""
+    dt = CS_I8 if dtype == torch.int8 else _float_dt(dtype)
+    return torch.empty((int(lib().cs_linear_q8_workspace_bytes(dt, rows, k, d_out)),),
+                       dtype=torch.uint8, device=device)
+
+
+def linear_q8(x: torch.Tensor, w: torch.Tensor, sw: torch.Tensor, sx: torch.Tensor | None = None,
+              bias: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+              ws: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y = (x @ w.T) * sx * sw + bias on 8-bit codes (cs_linear_q8).  w int8 [d_out][k] with
+    scales sw (quantise_rows of the weight matrix gives both).  x [rows][k] is int8 with scales
+    sx, or a float tensor that the call quantises row by row.  out_dtype: x's by default, float32
+    for int8 x."""
+    px, ldx = _rows(x, "x")
+    pw, ldw = _rows(w, "w")
+    rows, k = x.shape
+    d_out = w.shape[0]
+    if w.dtype != torch.int8 or w.shape[1] != k:
+        raise ValueError(f"w must be int8 [d_out][{k}]")
+    xt = CS_I8 if x.dtype == torch.int8 else _float_dt(x.dtype)
+    if (x.dtype == torch.int8) != (sx is not None):
+        raise ValueError("sx goes with int8 x")
+    if out_dtype is None:
+        out_dtype = torch.float32 if x.dtype == torch.int8 else x.dtype
+    if out is None:
+        out = torch.empty((rows, d_out), dtype=out_dtype, device=x.device)
+    if out.dtype != out_dtype or tuple(out.shape) != (rows, d_out):
+        raise ValueError(f"out must be {out_dtype} [{rows}][{d_out}]")
+    py, ldy = _rows(out, "out")
+    need = int(lib().cs_linear_q8_workspace_bytes(xt, rows, k, d_out))
+    ws, pws, nws = _ws(ws, need, x.device)
+    check("cs_linear_q8", lib().cs_linear_q8(
+        xt, px, ldx, _vector(sx, "sx", torch.float32, rows), rows, k, pw, ldw,
+        _vector(sw, "sw", torch.float32, d_out), d_out,
+        _vector(bias, "bias", torch.float32, d_out), _float_dt(out_dtype), py, ldy, pws, nws,
+        _stream()))
+    return out
+
+
+@dataclass
+class PagedCache:
+    """Keys and values of many sequences in 8 bits (cs_q8_cache): codes int8
+    [pages][heads][page][d], scales float32 [pages][heads][page]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    def __post_init__(self):
+        if self.k.dim() != 4:
+            raise ValueError("codes must be [pages][heads][page][d]")
+        for t, dt, shape, name in ((self.k, torch.int8, self.k.shape, "k"),
+                                   (self.v, torch.int8, self.k.shape, "v"),
+                                   (self.k_scale, torch.float32, self.k.shape[:3], "k_scale"),
+                                   (self.v_scale, torch.float32, self.k.shape[:3], "v_scale")):
+            if t.dtype != dt or t.shape != shape:
+                raise ValueError(f"{name} must be {dt} {list(shape)}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        self.pages, self.heads, self.page, self.d = self.k.shape
+        self._c = _lib.Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                               self.v_scale.data_ptr(), *self.k.shape)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page: int, d: int, device="cuda") -> "PagedCache":
+        def codes():
+            return torch.empty((pages, heads, page, d), dtype=torch.int8, device=device)
+
+        def scales():
+            return torch.empty((pages, heads, page), dtype=torch.float32, device=device)
+        return cls(codes(), codes(), scales(), scales())
+
+    def _ptr(self):
+        if not self.k.is_cuda:
+            raise ValueError("the cache must be on the GPU")
+        return ctypes.byref(self._c)
+
+
+def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Quantise k and v (float [tokens][heads][d]) into the cache's slots (int64 [tokens], slot =
+    page number * page + offset; one outside the cache leaves its token out): cs_cache_write."""
+    pk, ldk, hsk = _heads(k, "k")
+    pv, ldv, hsv = _heads(v, "v")
+    if k.dtype != v.dtype or k.shape != v.shape or tuple(k.shape[1:]) != (cache.heads, cache.d):
+        raise ValueError(f"k and v must be of one type and [tokens][{cache.heads}][{cache.d}]")
+    check("cs_cache_write", lib().cs_cache_write(
+        cache._ptr(), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
+        _vector(slots, "slots", torch.int64, k.shape[0]), k.shape[0], _stream()))
+
+
+def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
+               out: tuple | None = None):
+    """(k, v), each [tokens][heads][d] of `dtype`, of the slots' tokens: cs_cache_read."""
+    shape = (slots.shape[0], cache.heads, cache.d)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=dtype, device=slots.device) for _ in range(2))
+    for t in out:
+        if t.dtype != dtype or tuple(t.shape) != shape:
+            raise ValueError(f"out must be {dtype} {list(shape)}")
+    check("cs_cache_read", lib().cs_cache_read(
+        cache._ptr(), _vector(slots, "slots", torch.int64, shape[0]), shape[0], _float_dt(dtype),
+        _dev(out[0], "out"), _dev(out[1], "out"), _stream()))
+    return out
+
+
+def _attention_args(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, max_len: int | None):
+    if q.dim() != 3 or q.shape[2] != cache.d:
+        raise ValueError(f"q must be [tokens][q_heads][{cache.d}]")
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise ValueError("table must be int32 [batch][pages]")
+    return _float_dt(q.dtype), 0 if max_len is None else int(max_len)
+
+
+def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
+                              max_len: int | None = None) -> torch.Tensor:
+    """Workspace of paged_attention for arguments of these shapes."""
+    qt, ml = _attention_args(q, cache, table, max_len)
+    n = lib().cs_paged_attention_workspace_bytes(ctypes.byref(cache._c), qt, q.shape[0],
+                                                 q.shape[1], table.shape[0], table.shape[1], ml)
+    return torch.empty((int(n),), dtype=torch.uint8, device=q.device)
+
+
+def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, lens: torch.Tensor,
+                    starts: torch.Tensor, *, scale: float | None = None, window: int = 0,
+                    max_len: int | None = None, ws: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """Causal attention of each sequence's new tokens over the cache that already holds them
+    (cs_paged_attention).  q float [tokens][q_heads][d]; table int32 [batch][pages] page numbers;
+    lens int32 [batch] positions with the new ones; starts int32 [batch + 1] first new token of
+    each sequence in q.  scale: 1 / sqrt(d) by default.  window: positions seen, 0 for all.
+    max_len: the longest of lens if the caller knows it (a hint for how the work is split)."""
+    qt, ml = _attention_args(q, cache, table, max_len)
+    pq, ldq, hsq = _heads(q, "q")
+    b = table.shape[0]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if out.dtype != q.dtype or out.shape != q.shape:
+        raise ValueError("out must be of q's type and shape")
+    need = int(lib().cs_paged_attention_workspace_bytes(
+        ctypes.byref(cache._c), qt, q.shape[0], q.shape[1], b, table.shape[1], ml))
+    ws, pws, nws = _ws(ws, need, q.device)
+    check("cs_paged_attention", lib().cs_paged_attention(
+        cache._ptr(), qt, pq, ldq, hsq, q.shape[0], q.shape[1], b, _dev(table, "table"),
+        table.shape[1], _vector(lens, "lens", torch.int32, b),
+        _vector(starts, "starts", torch.int32, b + 1), ml,
+        1.0 / math.sqrt(cache.d) if scale is None else scale, window, _dev(out, "out"), pws, nws,
+        _stream()))
+    return out
