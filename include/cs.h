@@ -730,8 +730,8 @@ size_t cs_workspace_bytes(int op, cs_dtype xt, int64_t rows, int c_in);
  * NaN and codes 0, so that what is computed from it is NaN.
  */
 
-/* Limit of k in cs_linear_q8: 131,072 products of two codes fit int32. */
-#define CS_MAX_Q8_K 131072
+#define CS_MAX_Q8_K 131072      /* k of cs_linear_q8: that many products of two codes fit int32 */
+#define CS_MAX_Q8_LEN (1 << 30) /* positions that a row of cs_paged_attention's table holds     */
 
 /*
  * cs_quantise_rows - codes and scales of the rows of a float matrix (tokens
@@ -843,7 +843,8 @@ int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens
  *  ws      device, 16-byte aligned, cs_paged_attention_workspace_bytes bytes
  *          (may be NULL where that is 0); undefined afterwards.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (cache geometry, strides,
- *  q_heads not a multiple of heads, tokens * q_heads over 2^31 - 1),
+ *  q_heads not a multiple of heads, heads over 65535, tokens * q_heads over
+ *  2^31 - 1, table_width * page over CS_MAX_Q8_LEN),
  *  CS_ERR_WORKSPACE, CS_ERR_DEVICE.
  */
 int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int64_t ldq,

@@ -74,6 +74,32 @@ int cache_view(const cs_q8_cache* c, cs::CacheView* out) {
   return CS_OK;
 }
 
+// ---------------------------------------------------------------- attention
+struct AttentionPlan {
+  int64_t tiles;       // numbers of row tiles (find_tile)
+  int splits, chunk;
+};
+
+AttentionPlan attention_plan(const cs::CacheView& c, int tokens, int q_heads, int batch,
+                             int table_width, int max_len, int window) {
+  AttentionPlan p;
+  const int64_t group = q_heads / c.heads;
+  p.tiles = tokens * group / 16 + batch + 1;
+  int64_t len = (int64_t)table_width << c.page_log;
+  if (max_len > 0) len = std::min<int64_t>(len, max_len);
+  if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
+  const int64_t items = std::max<int64_t>(1, (tokens * group + 15) / 16) * c.heads;
+  int64_t splits = std::min<int64_t>({1024 / items, (len + 127) / 128, 128});
+  if (splits < 1) splits = 1;
+  p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
+  p.splits = (int)((len + p.chunk - 1) / p.chunk);
+  return p;
+}
+
+size_t attention_part_bytes(const AttentionPlan& p, int64_t rows, int d) {
+  return p.splits > 1 ? (size_t)p.splits * rows * ((size_t)d * 4 + 8) : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -189,7 +215,13 @@ int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens
 
 size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt, int tokens,
                                           int q_heads, int batch, int table_width, int max_len) {
-  return 0;
+  cs::CacheView c;
+  if (!is_float(qt) || cache_view(cache, &c) != CS_OK) return 0;
+  if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0) return 0;
+  if (q_heads % c.heads != 0) return 0;
+  // the split without a window is the finest: it serves any window
+  const AttentionPlan p = attention_plan(c, tokens, q_heads, batch, table_width, max_len, 0);
+  return attention_part_bytes(p, (int64_t)tokens * q_heads, c.d);
 }
 
 int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
@@ -209,19 +241,37 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
       !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4))
     return CS_ERR_ARG;
   if (q_heads % c.heads != 0 || ldq < 0 || hsq < c.d) return CS_ERR_SHAPE;
-  if ((int64_t)tokens * q_heads > kMaxCount) return CS_ERR_SHAPE;
-  if (((int64_t)table_width << c.page_log) > kMaxCount) return CS_ERR_SHAPE;
+  if ((int64_t)tokens * q_heads > kMaxCount || c.heads > 65535) return CS_ERR_SHAPE;
+  if (((int64_t)table_width << c.page_log) > CS_MAX_Q8_LEN) return CS_ERR_SHAPE;
   const size_t need = cs_paged_attention_workspace_bytes(cache, qt, tokens, q_heads, batch,
                                                          table_width, max_len);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
-  const cs::PagedAttention a{c, q, ldq, hsq, tokens, q_heads, batch, table, table_width, lens,
-                             starts, scale, window, out};
-  const dim3 grid((unsigned)(((int64_t)tokens * q_heads + 3) / 4)), block(256);
+  const AttentionPlan p = attention_plan(c, tokens, q_heads, batch, table_width, max_len, window);
+  const int group = q_heads / c.heads;
+  const int64_t rows = (int64_t)tokens * q_heads;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int e = (int)float_size(qt);
+  const bool vec = aligned(q, 16) && (tokens == 1 || ldq * e % 16 == 0) && hsq * e % 16 == 0;
+  cs::PagedAttention a{c, q, ldq, hsq, vec, tokens, q_heads, group, batch,
+                       cs::make_fastdiv((uint32_t)group), table, table_width, lens, starts, scale,
+                       window, out, p.splits, p.chunk, nullptr, nullptr};
+  if (p.splits > 1) {
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)p.splits * rows * c.d);
+  }
   return with_float(qt, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL((cs::attention_row<T>), grid, block, 0, static_cast<hipStream_t>(stream),
-                       a);
-    return launched();
+    const dim3 grid((unsigned)p.tiles, (unsigned)c.heads, (unsigned)p.splits), block(256);
+    if (c.d <= 64) hipLaunchKernelGGL((cs::attention_few<T, 64>), grid, block, 0, s, a);
+    else if (c.d <= 128) hipLaunchKernelGGL((cs::attention_few<T, 128>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((cs::attention_few<T, 256>), grid, block, 0, s, a);
+    int r = launched();
+    if (r == CS_OK && p.splits > 1) {
+      hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s,
+                         a);
+      r = launched();
+    }
+    return r;
   });
 }
 

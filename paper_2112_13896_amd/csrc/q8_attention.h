@@ -1,19 +1,48 @@
 // Attention of new tokens over the paged int8 cache: token i of sequence b,
 // at position p = len_b - n_b + i, has o = sum_j e_j v_j / sum_j e_j with
-// e_j = exp(scale * q.k_j - m) over the positions j in (p - window, p].
+// e_j = exp(scale * q.k_j) over the positions j in (p - window, p].
+//
+// What both kernels below share:
+//  - The rows of a cache head are the (new token, query head) pairs that read
+//    it, token-major: row r is token r / group, head r % group.
+//  - Products run on the f16 matrix instructions.  A code is exact in f16; a
+//    query row is scaled by a power of two so that its largest element lies
+//    in [2^8, 2^9), which keeps a 16-bit query exact or within 2^-25 of its
+//    largest element.  fp32 queries are held as two halves (22 bits), and so
+//    are the weights that multiply the values: twice the products, and an
+//    error of fp32's order.
+//  - Logits are formed transposed (keys x rows), so that a lane holds several
+//    keys of one row: maximum and sum run mostly inside a lane, and the
+//    weights are already laid out as the operand of the second product
+//    (channels x rows), whose order of keys only has to agree with the
+//    values' operand.
+//  - With v_j = sv_j * code_j, a weight that meets the codes is e_j * sv_j.
+//    To round it to f16 it is kept relative to the row's own largest: with
+//    sv_j = a_j 2^E_j (1 <= a_j < 2), x_j = log2(e_j) + E_j and m the running
+//    maximum of x_j over the keys the row sees, w_j = a_j 2^(x_j - m + 12) is
+//    at most 2^13 and the denominator is the sum of 2^(x_j - m + 12) 2^-E_j.
+//    A token with large values that a row does not see, or hardly weighs,
+//    takes no precision from the others.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "q8_rows.h"
 
 namespace cs {
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 struct PagedAttention {
   CacheView c;
   const void* q;
   int64_t ldq, hsq;
-  int tokens, q_heads, batch;
+  int q_vec;           // query heads start on 16 bytes
+  int tokens, q_heads, group, batch;
+  FastDiv by_group;
   const int32_t* table;
   int table_width;
   const int32_t* lens;
@@ -21,80 +50,446 @@ struct PagedAttention {
   float scale;
   int window;          // 0: none
   void* out;
+  int splits, chunk;   // parts of the key axis and their length (the last takes the rest)
+  float* part_o;       // [splits][tokens * q_heads][d], splits > 1
+  float2* part_ml;     // [splits][tokens * q_heads]: m, l
 };
 
-// The sequence that new token t belongs to: the last b with starts[b] <= t,
-// `batch` for tokens past the last sequence.
-__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int t) {
-  int lo = 0, hi = batch;                                  // starts[lo] <= t < starts[hi + 1]
+// A tile of `rows` rows of one sequence.  Sequence b's tiles have the numbers
+// from starts[b] * group / rows + b on, which leaves room for its last,
+// partial one: a tile number gives its sequence by a binary search, and the
+// few numbers without rows leave at once.  Tokens past the last sequence are
+// a sequence of length 0.
+struct RowTile {
+  int b, token0, n;    // sequence, its first new token, its new tokens
+  int row0, rows;      // first row of the tile in the sequence, the sequence's rows
+  int len;             // positions
+};
+
+__device__ __forceinline__ bool find_tile(const PagedAttention& a, int tile, int per, RowTile* t) {
+  auto base = [&](int b) {
+    const int s = b > a.batch ? a.tokens : a.starts[b];
+    return (int)((int64_t)s * a.group / per) + b;
+  };
+  int lo = 0, hi = a.batch;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
-    if (starts[mid] <= t) lo = mid;
+    if (base(mid) <= tile) lo = mid;
     else hi = mid - 1;
   }
-  return lo;
+  t->b = lo;
+  t->token0 = min(max(a.starts[lo], 0), a.tokens);
+  const int end = lo == a.batch ? a.tokens : min(max(a.starts[lo + 1], 0), a.tokens);
+  t->n = max(end - t->token0, 0);
+  t->rows = t->n * a.group;
+  t->row0 = (tile - base(lo)) * per;
+  t->len = lo == a.batch ? 0 : min(max(a.lens[lo], 0), a.table_width << a.c.page_log);
+  return t->row0 >= 0 && t->row0 < t->rows;
 }
 
-// One wavefront to a (token, query head): 64 keys at a time, a key to a lane
-// for the logits, then d / 64 channels to a lane for the values.
+// Positions [lo, hi) that some row of tokens t0 .. t1 of the tile sees.
+__device__ __forceinline__ void tile_keys(const PagedAttention& a, const RowTile& t, int t0,
+                                          int t1, int* lo, int* hi) {
+  const int p0 = t.len - t.n + t0, p1 = t.len - t.n + t1;
+  *hi = max(p1 + 1, 0);
+  *lo = a.window > 0 ? max(p0 - a.window + 1, 0) : 0;
+}
+
+// Four codes (a dword) as two pairs of halves code * 2^-9: the byte with its
+// sign bit turned is code + 128; alone in a half it is a denormal number,
+// (code + 128) 2^-24, and one fused multiply-add takes it to code * 2^-9,
+// exactly.  `hi` and `lo` may be different dwords: that is the transposition
+// of the values' bytes.
+constexpr float kCodeScale = 512.0f;                       // undoes 2^-9
+__device__ __forceinline__ f16x2 code_pair(uint32_t hi, uint32_t lo, uint32_t sel) {
+  const uint32_t u = __builtin_amdgcn_perm(hi, lo, sel);
+  f16x2 h;
+  __builtin_memcpy(&h, &u, 4);
+  const f16x2 up = {(_Float16)32768.0f, (_Float16)32768.0f};
+  const f16x2 off = {(_Float16)-0.25f, (_Float16)-0.25f};
+  return __builtin_elementwise_fma(h, up, off);
+}
+constexpr uint32_t kFlip = 0x80808080u;
+
+// Eight codes of one row, in order (two dwords, flipped here).
+__device__ __forceinline__ f16x8 codes_f16(uint32_t a, uint32_t b) {
+  a ^= kFlip;
+  b ^= kFlip;
+  const f16x2 p0 = code_pair(a, a, 0x0C010C00u), p1 = code_pair(a, a, 0x0C030C02u);
+  const f16x2 p2 = code_pair(b, b, 0x0C010C00u), p3 = code_pair(b, b, 0x0C030C02u);
+  return f16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+
+// Byte c of eight dwords (flipped already), in order.
+template <int C>
+__device__ __forceinline__ f16x8 codes_f16_across(const uint32_t (&v)[8]) {
+  constexpr uint32_t sel = 0x0C000C00u | (uint32_t)C | ((uint32_t)(4 + C) << 16);
+  const f16x2 p0 = code_pair(v[1], v[0], sel), p1 = code_pair(v[3], v[2], sel);
+  const f16x2 p2 = code_pair(v[5], v[4], sel), p3 = code_pair(v[7], v[6], sel);
+  return f16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+
+// Reductions over the lanes that share lane % 16 (four) or lane % 32 (two).
+template <typename Op>
+__device__ __forceinline__ float reduce_x32(float v, Op op) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <typename Op>
+__device__ __forceinline__ float reduce_x16_x32(float v, Op op) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return reduce_x32(op(__uint_as_float(r[0]), __uint_as_float(r[1])), op);
+}
+struct FMax {
+  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct FAdd {
+  __device__ float operator()(float a, float b) const { return a + b; }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kHead = 12.0f;                             // weights are scaled by 2^12
+
+// A query row's power of two and what turns its products into log2 units.
+struct RowNorm {
+  int shift;     // q * 2^shift is what the products take
+  float c;       // logit * log2(e) = product * ks * c
+  bool bad;      // not finite: the row's outputs are NaN
+};
+__device__ __forceinline__ RowNorm row_norm(float amax, float scale) {
+  RowNorm r;
+  r.bad = !(amax < __builtin_inff());
+  int ex = 0;
+  if (!r.bad && amax > 0.0f) ex = __builtin_amdgcn_frexp_expf(amax) - 1;
+  r.shift = 8 - ex;
+  r.c = ldexpf(scale * 1.4426950408889634f * kCodeScale, ex - 8);
+  return r;
+}
+
+// How a token's values enter: sv = a 2^E (zero values: any E far below).
+struct ValueScale {
+  float e, a, r;                                           // E, a, 2^-E
+};
+__device__ __forceinline__ ValueScale value_scale(float sv) {
+  ValueScale v;
+  const int ex = fabsf(sv) > 0.0f ? max(__builtin_amdgcn_frexp_expf(sv) - 1, -120) : -60;
+  v.e = (float)ex;
+  v.a = ldexpf(sv, -ex);                                   // NaN stays
+  v.r = ldexpf(1.0f, -ex);
+  return v;
+}
+
 template <typename T>
-__global__ __launch_bounds__(256) void attention_row(PagedAttention a) {
-  __shared__ float lq[4][256];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, d = a.c.d;
-  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  if (item >= (int64_t)a.tokens * a.q_heads) return;
-  const int t = (int)(item / a.q_heads), head = (int)(item % a.q_heads);
-  const int kv = head / (a.q_heads / a.c.heads);
-  const T* q = static_cast<const T*>(a.q) + t * a.ldq + head * a.hsq;
-  for (int i = lane; i < d; i += 64) lq[wave][i] = to_f32(q[i]) * a.scale;
-  wave_lds_order();
-  const int b = sequence_of(a.starts, a.batch, t);
-  int pos = -1;
-  if (b < a.batch) {
-    const int len = min(max(a.lens[b], 0), a.table_width << a.c.page_log);
-    pos = len - (a.starts[b + 1] - t);
+__device__ __forceinline__ void load_q8(const T* p, int vec, float (&f)[8]) {
+  if (vec) load8(p, f);
+  else load8_some(p, 8, f);
+}
+
+// One row's weights as operand halves: the value, and for fp32 what it lacks.
+// The empty asm keeps w a rounded 32-bit number: the compiler may otherwise
+// take a product and its conversion to half in one instruction (one rounding
+// instead of two) for the first half only, and where the two roundings
+// differ - one number in ten thousand - the second half would not be what the
+// first one lacks.
+template <int NP>
+__device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float v = w[j];
+    if constexpr (NP == 2) asm volatile("" : "+v"(v));
+    p[0][j] = (_Float16)v;
+    if constexpr (NP == 2) p[1][j] = (_Float16)(v - (float)p[0][j]);
   }
-  const int first = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-  float m = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int j0 = first; j0 <= pos; j0 += 64) {
-    const int j = j0 + lane;
-    float s = -INFINITY, sv = 0.0f;
-    int64_t at = 0;
-    if (j <= pos) {
-      const int page = a.table[(int64_t)b * a.table_width + (j >> a.c.page_log)];
-      const int64_t slot = ((int64_t)page << a.c.page_log) | (j & ((1 << a.c.page_log) - 1));
-      if (slot >= 0 && slot < a.c.slots) {
-        at = cache_row(a.c, slot, kv);
-        float dot = 0.0f;
-        for (int i = 0; i < d; ++i) dot += lq[wave][i] * (float)a.c.k[at * d + i];
-        s = dot * a.c.ks[at];
-        sv = a.c.vs[at];
+}
+
+// ---------------------------------------------------------------- few rows
+// attention_few: up to 16 rows of a cache head (a decoding token's query
+// heads, a few drafted tokens) to a workgroup of four wavefronts, the keys
+// read once.  A wavefront takes 32 keys a step, every fourth step of the
+// workgroup's part of the key axis: keys and values go from memory to
+// registers (no LDS), the next step's loads in flight under this one's
+// arithmetic.  Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles
+// of 16, channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels
+// r DT/16 .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
+template <int DT>
+struct FewStep {
+  u32x4 k[2][DT / 64];
+  uint32_t v[DT / 64][8];
+  f32x4 ks[2], vs[2];
+};
+
+template <typename T, int DT>
+__global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAttention a) {
+  constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+  constexpr int KS = DT / 32, CT = DT / 16;
+  __shared__ float l_o[4][16][DT + 4];
+  __shared__ float l_m[4][16], l_l[4][16];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 16, h = lane / 16, d = a.c.d, head = blockIdx.y, split = blockIdx.z;
+  RowTile t;
+  if (!find_tile(a, blockIdx.x, 16, &t)) return;
+  const int row = t.row0 + r, rows_end = min(t.rows, t.row0 + 16);
+  const bool row_live = row < t.rows;
+  const int tok = (int)fdiv((uint32_t)min(row, t.rows - 1), a.by_group);
+  const int tok0 = (int)fdiv((uint32_t)t.row0, a.by_group);
+  const int tok1 = (int)fdiv((uint32_t)(rows_end - 1), a.by_group);
+  const int qh = head * a.group + min(row, t.rows - 1) - tok * a.group;
+  int lo, hi;
+  tile_keys(a, t, tok0, tok1, &lo, &hi);
+  const int pos = t.len - t.n + tok;                       // the row sees [see, pos]
+  const int see = a.window > 0 ? pos - a.window + 1 : 0;
+  const int pos0 = t.len - t.n + tok0;                     // every row sees up to pos0 ...
+  const int see1 = a.window > 0 ? t.len - t.n + tok1 - a.window + 1 : 0;   // ... from see1 on
+  // this workgroup's part
+  int j0 = lo / 32 * 32 + split * a.chunk;
+  if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
+  const int steps = hi > j0 ? (hi - j0 + 31) / 32 : 0;
+
+  // the query rows' operand
+  f16x8 q[NP][KS];
+  float c;
+  {
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
+    float f[KS][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int ch = h * (DT / 4) + 8 * s;
+      if (ch < d) load_q8(qp + ch, a.q_vec, f[s]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (ch >= d) f[s][e] = 0.0f;
+        top = max(top, abs_bits(f[s][e]));
       }
     }
-    float top = s;
-    for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float mn = fmaxf(m, top);
-    const float base = mn == -INFINITY ? 0.0f : mn;
-    const float e = s == -INFINITY ? 0.0f : expf(s - base), r = expf(m - base);
-    float sum = e;
-    for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
-    l = l * r + sum;
-    m = mn;
+    // bits of magnitudes are ordered as unsigned numbers, and as floats but for NaN
+    const auto s16 = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+    top = max(s16[0], s16[1]);
+    const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    const RowNorm nm = row_norm(__uint_as_float(max(s32[0], s32[1])), a.scale);
+    c = nm.c;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) o[u] *= r;
-    const float pv = s == -INFINITY ? 0.0f : e * sv;
-    for (int x = 0; x < 64; ++x) {
-      const float p = __shfl(pv, x);
-      const int64_t row = __shfl(at, x);
+    for (int s = 0; s < KS; ++s) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (lane + 64 * u < d) o[u] += p * (float)a.c.v[row * d + lane + 64 * u];
+      for (int e = 0; e < 8; ++e)
+        f[s][e] = nm.bad ? __uint_as_float(0x7FC00000u) : ldexpf(f[s][e], nm.shift);
+      f16x8 p[NP];
+      split_f16<NP>(f[s], p);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) q[n][s] = p[n];
     }
   }
-  T* y = static_cast<T*>(a.out) + item * d;
+
+  const int32_t* table = a.table + (int64_t)t.b * a.table_width;
+  const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
+  // rows (of codes) of the two tiles of 16 keys of a step; -1: no such page
+  auto rows_of = [&](int j, int64_t (&at)[2]) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
-    if (lane + 64 * u < d) y[lane + 64 * u] = (T)(l == 0.0f ? 0.0f : o[u] / l);
+    for (int u = 0; u < 2; ++u) {
+      const int k0 = min(j + 16 * u, hi - 1);
+      const int page = __builtin_amdgcn_readfirstlane(table[k0 >> lg]);
+      at[u] = (uint32_t)page < (uint32_t)n_pages
+                  ? (((int64_t)page * a.c.heads + head) << lg) + ((j + 16 * u) & in_page)
+                  : -1;
+    }
+  };
+  FewStep<DT> st;
+  int64_t at[2];
+  auto fetch = [&](FewStep<DT>& s, const int64_t (&at)[2]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t row0 = at[u] < 0 ? 0 : at[u];          // any rows: hidden ones are masked
+      const int8_t* kp = a.c.k + (row0 + r) * d;
+#pragma unroll
+      for (int p = 0; p < DT / 64; ++p) {
+        const int ch = h * (DT / 4) + 16 * p;              // channels past d meet zeros in q
+        s.k[u][p] = *reinterpret_cast<const u32x4*>(kp + (ch < d ? ch : 0));
+      }
+      s.ks[u] = *reinterpret_cast<const f32x4*>(a.c.ks + row0 + 4 * h);
+      s.vs[u] = *reinterpret_cast<const f32x4*>(a.c.vs + row0 + 4 * h);
+      const int ch = r * (DT / 16);                        // channels past d are not stored
+      const int8_t* vp = a.c.v + (row0 + 4 * h) * d + (ch < d ? ch : 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w[DT / 64];
+        __builtin_memcpy(w, __builtin_assume_aligned(vp + (int64_t)i * d, DT / 16), DT / 16);
+#pragma unroll
+        for (int x = 0; x < DT / 64; ++x) s.v[x][4 * u + i] = w[x];
+      }
+    }
+  };
+
+  f32x4 o[CT];
+#pragma unroll
+  for (int x = 0; x < CT; ++x) o[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = kNegInf, l = 0.0f;
+  int step = wave;
+  if (step < steps) {
+    rows_of(j0 + 32 * step, at);
+    fetch(st, at);
+  }
+#pragma unroll 2
+  for (; step < steps; step += 4) {
+    const int j = j0 + 32 * step;
+    const bool ok0 = at[0] >= 0, ok1 = at[1] >= 0;
+    FewStep<DT> nx;
+    if (step + 4 < steps) {
+      rows_of(j + 128, at);
+      fetch(nx, at);
+    }
+    // logits in log2 units, plus E
+    float x[8], av[8], rv[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const f16x8 kf = codes_f16(st.k[u][k / 2][k % 2 * 2], st.k[u][k / 2][k % 2 * 2 + 1]);
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+          s = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][k], s, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const ValueScale sv = value_scale(st.vs[u][i]);
+        av[4 * u + i] = sv.a;
+        rv[4 * u + i] = sv.r;
+        x[4 * u + i] = fmaf(s[i] * st.ks[u][i], c, sv.e);
+      }
+    }
+    // hidden keys: past the row's position, before its window, past the part, no page
+    if (j + 31 > pos0 || j < see1 || j + 31 >= hi || !ok0 || !ok1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = j + 16 * (i / 4) + 4 * h + i % 4;
+        if (key > pos || key < see || key >= hi || !(i < 4 ? ok0 : ok1)) {
+          x[i] = kNegInf;
+          av[i] = 0.0f;
+        }
+      }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+    top = fmaxf(m, reduce_x16_x32(top, FMax{}));
+    if (__builtin_amdgcn_ballot_w64(top > m)) {
+      const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
+      l *= f;
+#pragma unroll
+      for (int y = 0; y < CT; ++y) o[y] *= f;
+      m = top;
+    }
+    const float base = m == kNegInf ? 0.0f : m - kHead;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float e = exp2_fast(x[i] - base);
+      l = fmaf(e, rv[i], l);
+      w[i] = e * av[i];
+    }
+    f16x8 p[NP];
+    split_f16<NP>(w, p);
+    auto values = [&](auto cc, int xw) {
+      constexpr int C = decltype(cc)::value;
+      const f16x8 vf = codes_f16_across<C>(st.v[xw]);
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        o[4 * xw + C] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[n], o[4 * xw + C], 0, 0, 0);
+    };
+#pragma unroll
+    for (int xw = 0; xw < DT / 64; ++xw) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) st.v[xw][i] ^= kFlip;
+      values(std::integral_constant<int, 0>{}, xw);
+      values(std::integral_constant<int, 1>{}, xw);
+      values(std::integral_constant<int, 2>{}, xw);
+      values(std::integral_constant<int, 3>{}, xw);
+    }
+    st = nx;
+  }
+  l = reduce_x16_x32(l, FAdd{});
+
+  // the four wavefronts' sums, joined in order
+  if (h == 0) {
+    l_m[wave][r] = m;
+    l_l[wave][r] = l;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int x = 0; x < CT; x += 4)
+      *reinterpret_cast<f32x4*>(&l_o[wave][r][(4 * h + i) * CT + x]) =
+          f32x4{o[x][i], o[x + 1][i], o[x + 2][i], o[x + 3][i]};
+  __syncthreads();
+  // 16 lanes to a row
+  const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16;
+  if (t.row0 + rr >= rows_end) return;
+  float top = kNegInf;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, l_m[w][rr]);
+  const float base = top == kNegInf ? 0.0f : top;
+  float f[4], sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = exp2_fast(l_m[w][rr] - base);
+    // a wavefront without a key has l = 0; one with a NaN among its keys alone has m = -inf
+    sum += l_l[w][rr] == 0.0f ? 0.0f : l_l[w][rr] * f[w];
+  }
+  const int orow = t.row0 + rr;
+  const int otok = (int)fdiv((uint32_t)orow, a.by_group);
+  const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
+                     otok * a.group;
+  if (a.splits > 1 && x0 == 0) a.part_ml[(int64_t)split * a.tokens * a.q_heads + ro] =
+      float2{top, sum};
+  const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
+  for (int x = 8 * x0; x < d; x += 128) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
+      y[i] = a.splits > 1 ? s : s * inv;
+    }
+    if (a.splits > 1)
+      store8(a.part_o + ((int64_t)split * a.tokens * a.q_heads + ro) * d + x, y);
+    else
+      store8(static_cast<T*>(a.out) + ro * d + x, y);
+  }
+}
+
+// attention_join: the parts of a row, in order, a wavefront to a row.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
+  const int lane = threadIdx.x % 64, d = a.c.d;
+  const int64_t rows = (int64_t)a.tokens * a.q_heads;
+  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (row >= rows) return;
+  float top = kNegInf;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[s * rows + row].x);
+  const float base = top == kNegInf ? 0.0f : top;
+  float sum = 0.0f, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = a.part_ml[s * rows + row];
+    if (ml.y == 0.0f) continue;                            // a part without a key
+    const float f = exp2_fast(ml.x - base);
+    sum = fmaf(ml.y, f, sum);
+    const float* po = a.part_o + (s * rows + row) * d;
+    if (4 * lane < d) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(po + 4 * lane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], f, y[i]);
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
+  if (4 * lane < d) {
+    T* yp = static_cast<T*>(a.out) + row * d + 4 * lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) yp[i] = (T)(y[i] * inv);
+  }
 }
 
 }  // namespace cs
