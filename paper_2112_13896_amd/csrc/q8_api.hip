@@ -75,7 +75,16 @@ int cache_view(const cs_q8_cache* c, cs::CacheView* out) {
 }
 
 // ---------------------------------------------------------------- attention
+// f(integral_constant) with the width of the kernels' registers for d channels.
+template <typename F>
+void with_width(int d, F f) {
+  if (d <= 64) f(std::integral_constant<int, 64>{});
+  else if (d <= 128) f(std::integral_constant<int, 128>{});
+  else f(std::integral_constant<int, 256>{});
+}
+
 struct AttentionPlan {
+  bool many;           // attention_many, else attention_few
   int64_t tiles;       // numbers of row tiles (find_tile)
   int splits, chunk;
 };
@@ -83,13 +92,15 @@ struct AttentionPlan {
 AttentionPlan attention_plan(const cs::CacheView& c, int tokens, int q_heads, int batch,
                              int table_width, int max_len, int window) {
   AttentionPlan p;
-  const int64_t group = q_heads / c.heads;
-  p.tiles = tokens * group / 16 + batch + 1;
+  const int64_t group = q_heads / c.heads, rows = tokens * group;
+  p.many = rows > 32 * (int64_t)batch;
+  const int per = p.many ? 128 : 16;
+  p.tiles = rows / per + batch + 1;
   int64_t len = (int64_t)table_width << c.page_log;
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
-  const int64_t items = std::max<int64_t>(1, (tokens * group + 15) / 16) * c.heads;
-  int64_t splits = std::min<int64_t>({1024 / items, (len + 127) / 128, 128});
+  const int64_t items = (rows + per - 1) / per * c.heads;
+  int64_t splits = std::min<int64_t>({(p.many ? 512 : 1024) / items, (len + 127) / 128, 128});
   if (splits < 1) splits = 1;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
@@ -253,22 +264,31 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
   const int e = (int)float_size(qt);
   const bool vec = aligned(q, 16) && (tokens == 1 || ldq * e % 16 == 0) && hsq * e % 16 == 0;
   cs::PagedAttention a{c, q, ldq, hsq, vec, tokens, q_heads, group, batch,
-                       cs::make_fastdiv((uint32_t)group), table, table_width, lens, starts, scale,
+                       cs::make_fastdiv((uint32_t)group), cs::make_fastdiv((uint32_t)c.heads),
+                       cs::make_fastdiv((uint32_t)p.tiles), table, table_width, lens, starts, scale,
                        window, out, p.splits, p.chunk, nullptr, nullptr};
   if (p.splits > 1) {
     a.part_o = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)p.splits * rows * c.d);
   }
+  const int64_t blocks = p.tiles * c.heads * p.splits;
+  if (blocks > kMaxCount) return CS_ERR_SHAPE;
   return with_float(qt, [&](auto t) {
     using T = decltype(t);
-    const dim3 grid((unsigned)p.tiles, (unsigned)c.heads, (unsigned)p.splits), block(256);
-    if (c.d <= 64) hipLaunchKernelGGL((cs::attention_few<T, 64>), grid, block, 0, s, a);
-    else if (c.d <= 128) hipLaunchKernelGGL((cs::attention_few<T, 128>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((cs::attention_few<T, 256>), grid, block, 0, s, a);
+    const dim3 grid((unsigned)blocks), block(256);
+    auto few = [&](auto dt) {
+      hipLaunchKernelGGL((cs::attention_few<T, decltype(dt)::value>), grid, block, 0, s, a);
+    };
+    auto many = [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      hipLaunchKernelGGL((cs::attention_many<T, DT>), grid, block, 2 * sizeof(cs::ManyLds<DT>), s,
+                         a);
+    };
+    if (p.many) with_width(c.d, many);
+    else with_width(c.d, few);
     int r = launched();
     if (r == CS_OK && p.splits > 1) {
-      hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s,
-                         a);
+      hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, a);
       r = launched();
     }
     return r;

@@ -34,6 +34,7 @@
 namespace cs {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 struct PagedAttention {
@@ -42,7 +43,7 @@ struct PagedAttention {
   int64_t ldq, hsq;
   int q_vec;           // query heads start on 16 bytes
   int tokens, q_heads, group, batch;
-  FastDiv by_group;
+  FastDiv by_group, by_heads, by_tiles;
   const int32_t* table;
   int table_width;
   const int32_t* lens;
@@ -54,6 +55,17 @@ struct PagedAttention {
   float* part_o;       // [splits][tokens * q_heads][d], splits > 1
   float2* part_ml;     // [splits][tokens * q_heads]: m, l
 };
+
+// Workgroups go to the eight XCDs in turn: heads vary fastest, so that the
+// tiles and parts that read one head's keys meet in few L2s (with eight heads,
+// or a multiple, in one).
+__device__ __forceinline__ void place(const PagedAttention& a, int* head, int* tile, int* split) {
+  const uint32_t rest = fdiv(blockIdx.x, a.by_heads);
+  *head = (int)(blockIdx.x - rest * a.by_heads.d);
+  const uint32_t s = fdiv(rest, a.by_tiles);
+  *tile = (int)(rest - s * a.by_tiles.d);
+  *split = (int)s;
+}
 
 // A tile of `rows` rows of one sequence.  Sequence b's tiles have the numbers
 // from starts[b] * group / rows + b on, which leaves room for its last,
@@ -228,11 +240,12 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
   __shared__ float l_o[4][16][DT + 4];
   __shared__ float l_m[4][16], l_l[4][16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int r = lane % 16, h = lane / 16, d = a.c.d, head = blockIdx.y, split = blockIdx.z;
+  const int r = lane % 16, h = lane / 16, d = a.c.d;
+  int head, tile, split;
+  place(a, &head, &tile, &split);
   RowTile t;
-  if (!find_tile(a, blockIdx.x, 16, &t)) return;
+  if (!find_tile(a, tile, 16, &t)) return;
   const int row = t.row0 + r, rows_end = min(t.rows, t.row0 + 16);
-  const bool row_live = row < t.rows;
   const int tok = (int)fdiv((uint32_t)min(row, t.rows - 1), a.by_group);
   const int tok0 = (int)fdiv((uint32_t)t.row0, a.by_group);
   const int tok1 = (int)fdiv((uint32_t)(rows_end - 1), a.by_group);
@@ -360,12 +373,12 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
         x[4 * u + i] = fmaf(s[i] * st.ks[u][i], c, sv.e);
       }
     }
-    // hidden keys: past the row's position, before its window, past the part, no page
-    if (j + 31 > pos0 || j < see1 || j + 31 >= hi || !ok0 || !ok1) {
+    // hidden keys: past the row's position (the last part's end), before its window, no page
+    if (j + 31 > pos0 || j < see1 || !ok0 || !ok1) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = j + 16 * (i / 4) + 4 * h + i % 4;
-        if (key > pos || key < see || key >= hi || !(i < 4 ? ok0 : ok1)) {
+        if (key > pos || key < see || !(i < 4 ? ok0 : ok1)) {
           x[i] = kNegInf;
           av[i] = 0.0f;
         }
@@ -459,6 +472,299 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
     else
       store8(static_cast<T*>(a.out) + ro * d + x, y);
   }
+}
+
+// ---------------------------------------------------------------- many rows
+// attention_many: 128 rows of a cache head to a workgroup of four wavefronts,
+// 32 rows each, 64 keys a step.  A step's codes are turned to halves once for
+// all four: keys [64][DT], values transposed [DT][64], both in 16-byte chunks
+// whose place in a row is permuted (xor) so that eight lanes that read or
+// write one column of chunks meet all banks; two buffers, the next step's
+// codes in flight in registers under this one's arithmetic, one barrier a
+// step.  Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y
+// = 0..3) of row r.  So a lane's eight weights of 16 keys are those at 4 h ..
+// and 8 + 4 h .., and the values' chunk g = 2 s + h of a channel holds just
+// the keys 16 s + 4 h .. +3 and 16 s + 8 + 4 h .. +3.
+template <int DT>
+struct ManyLds {
+  _Float16 k[64][DT];
+  _Float16 v[DT][64];
+  float ks[64], ls[64], rs[64];                            // ks, log2(vs), 1 / vs
+};
+
+__device__ __forceinline__ int value_chunk(int ch, int g) {
+  return g ^ ((ch & 3) * 2) ^ ((ch >> 2) & 7);
+}
+
+template <typename T, int DT>
+__global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAttention a) {
+  constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+  constexpr int KS = DT / 16, CT = DT / 32;
+  constexpr int KP = DT / 64;                              // key pieces of 16 codes a thread
+  extern __shared__ __align__(16) unsigned char smem[];
+  ManyLds<DT>* lds = reinterpret_cast<ManyLds<DT>*>(smem);
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int r = lane % 32, h = lane / 32, d = a.c.d;
+  int head, tile, split;
+  place(a, &head, &tile, &split);
+  RowTile t;
+  // the last tiles of a sequence see most keys: first
+  if (!find_tile(a, (int)a.by_tiles.d - 1 - tile, 128, &t)) return;
+  const int rows_end = min(t.rows, t.row0 + 128);
+  const int row = t.row0 + wave * 32 + r;
+  const int row_c = min(row, t.rows - 1);
+  const int tok = (int)fdiv((uint32_t)row_c, a.by_group);
+  const int qh = head * a.group + row_c - tok * a.group;
+  const int back = t.len - t.n;                            // position of new token 0
+  int lo, hi;
+  tile_keys(a, t, (int)fdiv((uint32_t)t.row0, a.by_group),
+            (int)fdiv((uint32_t)(rows_end - 1), a.by_group), &lo, &hi);
+  const int pos = back + tok, see = a.window > 0 ? pos - a.window + 1 : 0;
+  // the wavefront's rows: all see up to pos0 and from see1 on, none from pos1 + 1 on or before see0
+  const int w0 = min(t.row0 + wave * 32, t.rows - 1), w1 = min(w0 + 31, t.rows - 1);
+  const int pos0 = back + (int)fdiv((uint32_t)w0, a.by_group);
+  const int pos1 = back + (int)fdiv((uint32_t)w1, a.by_group);
+  const int see0 = a.window > 0 ? pos0 - a.window + 1 : 0;
+  const int see1 = a.window > 0 ? pos1 - a.window + 1 : 0;
+  const int j0 = lo / 64 * 64 + split * a.chunk;
+  if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
+  const int steps = hi > j0 ? (hi - j0 + 63) / 64 : 0;
+
+  f16x8 q[NP][KS];
+  float c;
+  {
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
+    uint32_t top = 0;
+    float f[8];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int ch = 16 * s + 8 * h;
+      if (ch < d) {
+        load_q8(qp + ch, a.q_vec, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+      }
+    }
+    const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    const RowNorm nm = row_norm(__uint_as_float(max(s32[0], s32[1])), a.scale);
+    c = nm.c;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int ch = 16 * s + 8 * h;
+      if (ch < d) load_q8(qp + ch, a.q_vec, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        f[e] = nm.bad ? __uint_as_float(0x7FC00000u) : ch < d ? ldexpf(f[e], nm.shift) : 0.0f;
+      f16x8 p[NP];
+      split_f16<NP>(f, p);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) q[n][s] = p[n];
+    }
+  }
+
+  // staging: which codes this thread brings
+  const int32_t* table = a.table + (int64_t)t.b * a.table_width;
+  const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
+  auto page_of = [&](int j) { return table[min(j, hi - 1) >> lg]; };
+  auto row_at = [&](int page, int j) {                     // a page outside the cache: any row
+    return (((int64_t)((uint32_t)page < (uint32_t)n_pages ? page : 0) * a.c.heads + head) << lg) +
+           (j & in_page);
+  };
+  constexpr int PR = DT / 16;                              // pieces of a key
+  const int k_key = tid / PR, k_ch = tid % PR * 16;        // + 256 / PR keys a piece
+  constexpr int VR = DT / 4;                               // dwords of a value
+  constexpr int VG = DT == 64 ? 8 : 256 / VR;              // groups of keys a round, of 8
+  constexpr int VN = 8 / VG;
+  const int v_ch = tid % VR * 4, v_g = tid / VR;           // DT 64: the second half has none
+  int kpage[KP], vpage[VN], spage = 0;
+  u32x4 kreg[KP];
+  uint32_t vreg[VN][8];
+  float ks_reg = 0.0f, vs_reg = 0.0f;
+  bool s_ok = false;
+  auto pages = [&](int j) {
+#pragma unroll
+    for (int p = 0; p < KP; ++p) kpage[p] = page_of(j + k_key + p * (256 / PR));
+#pragma unroll
+    for (int p = 0; p < VN; ++p) vpage[p] = page_of(j + (v_g + p * VG) / 2 * 16);
+    spage = page_of(j + lane);
+  };
+  auto fetch = [&](int j) {
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+      const int64_t at = row_at(kpage[p], j + k_key + p * (256 / PR));
+      kreg[p] = *reinterpret_cast<const u32x4*>(a.c.k + at * d + (k_ch < d ? k_ch : 0));
+    }
+#pragma unroll
+    for (int p = 0; p < VN; ++p) {
+      if (DT == 64 && v_g >= 8) break;
+      const int g = v_g + p * VG, key = g / 2 * 16 + g % 2 * 4;
+      const int8_t* vp = a.c.v + row_at(vpage[p], j + key) * d + (v_ch < d ? v_ch : 0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        vreg[p][i] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)(i / 4 * 8 + i % 4) * d);
+    }
+    if (wave == 0) {
+      const int64_t at = row_at(spage, j + lane);
+      s_ok = (uint32_t)spage < (uint32_t)n_pages;
+      ks_reg = a.c.ks[at];
+      vs_reg = a.c.vs[at];
+    }
+  };
+  auto stage = [&](ManyLds<DT>& b) {
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+      const int key = k_key + p * (256 / PR), ck = k_ch / 8;
+      *reinterpret_cast<f16x8*>(&b.k[key][((ck + 0) ^ (key & 7)) * 8]) =
+          codes_f16(kreg[p][0], kreg[p][1]);
+      *reinterpret_cast<f16x8*>(&b.k[key][((ck + 1) ^ (key & 7)) * 8]) =
+          codes_f16(kreg[p][2], kreg[p][3]);
+    }
+#pragma unroll
+    for (int p = 0; p < VN; ++p) {
+      if (DT == 64 && v_g >= 8) break;
+      const int g = v_g + p * VG;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vreg[p][i] ^= kFlip;
+      *reinterpret_cast<f16x8*>(&b.v[v_ch + 0][value_chunk(v_ch + 0, g) * 8]) =
+          codes_f16_across<0>(vreg[p]);
+      *reinterpret_cast<f16x8*>(&b.v[v_ch + 1][value_chunk(v_ch + 1, g) * 8]) =
+          codes_f16_across<1>(vreg[p]);
+      *reinterpret_cast<f16x8*>(&b.v[v_ch + 2][value_chunk(v_ch + 2, g) * 8]) =
+          codes_f16_across<2>(vreg[p]);
+      *reinterpret_cast<f16x8*>(&b.v[v_ch + 3][value_chunk(v_ch + 3, g) * 8]) =
+          codes_f16_across<3>(vreg[p]);
+    }
+    if (wave == 0) {
+      // values all zero: a scale far below, their codes are 0; no page: weight 0
+      const float sv = vs_reg == 0.0f ? 0x1p-60f : fmaxf(vs_reg, 0x1p-120f);
+      const bool num = vs_reg == vs_reg;
+      b.ks[lane] = s_ok ? ks_reg : 0.0f;
+      b.ls[lane] = !s_ok ? kNegInf : num ? __builtin_amdgcn_logf(sv) : vs_reg;
+      b.rs[lane] = num ? 1.0f / sv : 1.0f;
+    }
+  };
+
+  f32x16 o[CT];
+#pragma unroll
+  for (int x = 0; x < CT; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[x][i] = 0.0f;
+  float m = kNegInf, l = 0.0f;
+  if (steps > 0) {
+    pages(j0);
+    fetch(j0);
+    stage(lds[0]);
+    pages(j0 + 64);
+  }
+  __syncthreads();
+  for (int step = 0; step < steps; ++step) {
+    const int j = j0 + 64 * step;
+    const ManyLds<DT>& b = lds[step & 1];
+    const bool more = step + 1 < steps;
+    if (more) {
+      fetch(j + 64);
+      pages(j + 128);
+    }
+    if (j <= pos1 && j + 63 >= see0) {                     // some row sees a key of the step
+      float x[2][16];
+      float top = kNegInf;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const f16x8 kf =
+              *reinterpret_cast<const f16x8*>(&b.k[32 * u + r][((2 * k + h) ^ (r & 7)) * 8]);
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s, 0, 0, 0);
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const f32x4 ks = *reinterpret_cast<const f32x4*>(&b.ks[32 * u + 8 * y + 4 * h]);
+          const f32x4 ls = *reinterpret_cast<const f32x4*>(&b.ls[32 * u + 8 * y + 4 * h]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[u][4 * y + i] = fmaf(s[4 * y + i] * ks[i], c, ls[i]);
+        }
+      }
+      if (j + 63 > pos0 || j < see1) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = j + 32 * u + 8 * (i / 4) + 4 * h + i % 4;
+            if (key > pos || key < see) x[u][i] = kNegInf;
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(x[0][i], x[1][i]));
+      top = fmaxf(m, reduce_x32(top, FMax{}));
+      if (__builtin_amdgcn_ballot_w64(top > m)) {
+        const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
+        l *= f;
+#pragma unroll
+        for (int y = 0; y < CT; ++y) o[y] *= f;
+        m = top;
+      }
+      const float base = m == kNegInf ? 0.0f : m - kHead;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float w[8];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const f32x4 rs =
+                *reinterpret_cast<const f32x4*>(&b.rs[32 * u + 16 * s + 8 * y + 4 * h]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              w[4 * y + i] = exp2_fast(x[u][8 * s + 4 * y + i] - base);
+              l = fmaf(w[4 * y + i], rs[i], l);
+            }
+          }
+          f16x8 p[NP];
+          split_f16<NP>(w, p);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            const int ch = 32 * ct + r;
+            const f16x8 vf = *reinterpret_cast<const f16x8*>(
+                &b.v[ch][value_chunk(ch, 4 * u + 2 * s + h) * 8]);
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+              o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);
+          }
+        }
+    }
+    if (more) stage(lds[(step + 1) & 1]);
+    __syncthreads();
+  }
+  l = reduce_x32(l, FAdd{});
+  if (row >= rows_end) return;
+  const int64_t ro = (int64_t)(t.token0 + tok) * a.q_heads + qh;
+  const bool part = a.splits > 1;
+  const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
+  if (part && h == 0) a.part_ml[po] = float2{m, l};
+  const float inv = part ? 1.0f : l == 0.0f ? 0.0f : kCodeScale / l;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const int ch = 32 * ct + 8 * y + 4 * h;
+      if (ch >= d) continue;
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = o[ct][4 * y + i] * inv;
+      if (part) {
+        *reinterpret_cast<f32x4*>(a.part_o + po * d + ch) = f32x4{v[0], v[1], v[2], v[3]};
+      } else {
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<t4*>(static_cast<T*>(a.out) + ro * d + ch) =
+            t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+      }
+    }
 }
 
 // attention_join: the parts of a row, in order, a wavefront to a row.
