@@ -58,6 +58,21 @@ int quantise(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int c, int8_
   });
 }
 
+// ---------------------------------------------------------------- linear
+template <typename T, int BM, int BN, int WM, int WN>
+int linear_tiles(const cs::Q8Linear& a, hipStream_t s) {
+  cs::TileOrder o;
+  const int64_t tm = (a.rows + BM - 1) / BM, tn = ((int64_t)a.d_out + BN - 1) / BN;
+  if (tm * tn > kMaxCount) return CS_ERR_SHAPE;
+  o.tiles_m = (uint32_t)tm;
+  o.tiles_n = (uint32_t)tn;
+  o.per_xcd = (uint32_t)(tm * tn / 8);
+  o.more = (uint32_t)(tm * tn % 8);
+  hipLaunchKernelGGL((cs::linear_q8_tile<T, BM, BN, WM, WN>), dim3((unsigned)(tm * tn)),
+                     dim3(BM / WM * (BN / WN) * 64), 0, s, a, o);
+  return launched();
+}
+
 // ---------------------------------------------------------------- cache
 int cache_view(const cs_q8_cache* c, cs::CacheView* out) {
   if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return CS_ERR_ARG;
@@ -155,15 +170,24 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     if (st != CS_OK) return st;
     a.x = q; a.ldx = ld; a.sx = sq;
   }
-  const int64_t tiles_t = (rows + 63) / 64;
-  if (tiles_t > 65535) return CS_ERR_SHAPE;
-  const dim3 grid((unsigned)((d_out + 63) / 64), (unsigned)tiles_t), block(256);
-  const bool al = aligned(a.x, 16) && aligned(w, 16) && a.ldx % 16 == 0 && ldw % 16 == 0;
+  // whole 16-byte loads, offsets of a tile's rows in 32 bits
+  const bool al = aligned(a.x, 16) && aligned(w, 16) && a.ldx % 16 == 0 && ldw % 16 == 0 &&
+                  a.ldx < (1 << 23) && ldw < (1 << 23);
   return with_float(yt, [&](auto t) {
     using T = decltype(t);
-    if (al) hipLaunchKernelGGL((cs::linear_q8_tile<T, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((cs::linear_q8_tile<T, false>), grid, block, 0, s, a);
-    return launched();
+    if (!al) {
+      const int64_t tiles_t = (rows + 63) / 64;
+      if (tiles_t > 65535) return (int)CS_ERR_SHAPE;
+      hipLaunchKernelGGL((cs::linear_q8_any<T>),
+                         dim3((unsigned)((d_out + 63) / 64), (unsigned)tiles_t), dim3(256), 0, s, a);
+      return launched();
+    }
+    auto tiles = [&](int bm, int bn) {
+      return ((rows + bm - 1) / bm) * (((int64_t)d_out + bn - 1) / bn);
+    };
+    if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64>(a, s);
+    if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64>(a, s);
+    return linear_tiles<T, 64, 64, 32, 32>(a, s);
   });
 }
 

@@ -38,10 +38,12 @@ __device__ __forceinline__ i32x4 codes16(const int8_t* row, int e, int k) {
   return v;
 }
 
-// A 64 x 64 tile of y to a workgroup of four wavefronts, 32 x 32 each, 64
-// codes of k a step through LDS.
-template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(256) void linear_q8_tile(Q8Linear a) {
+// linear_q8_any: rows that start anywhere.  A 64 x 64 tile of y to a
+// workgroup of four wavefronts, 32 x 32 each, 64 codes of k a step through
+// registers and LDS, 16 bytes a thread and operand put together from single
+// ones.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
   constexpr int kLd = 64 + 16;                             // a row's bytes in LDS, padded
   __shared__ __align__(16) int8_t lx[64 * kLd], lw[64 * kLd];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
@@ -56,8 +58,8 @@ __global__ __launch_bounds__(256) void linear_q8_tile(Q8Linear a) {
   const int fr = lane % 32, fk = lane / 32 * 16;
   i32x16 acc = {};
   for (int k0 = 0; k0 < a.k; k0 += 64) {
-    const i32x4 vx = codes16<ALIGNED>(xr, k0 + sc, a.k);
-    const i32x4 vw = codes16<ALIGNED>(wr, k0 + sc, a.k);
+    const i32x4 vx = codes16<false>(xr, k0 + sc, a.k);
+    const i32x4 vw = codes16<false>(wr, k0 + sc, a.k);
     __syncthreads();
     *reinterpret_cast<i32x4*>(lx + sr * kLd + sc) = vx;
     *reinterpret_cast<i32x4*>(lw + sr * kLd + sc) = vw;
@@ -75,8 +77,165 @@ __global__ __launch_bounds__(256) void linear_q8_tile(Q8Linear a) {
   for (int i = 0; i < 16; ++i) {
     const int64_t t = t0 + tr + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
     if (t < a.rows)
-      static_cast<T*>(a.y)[t * a.ldy + n] = (T)((float)acc[i] * (a.sx[t] * s) + b);
+      static_cast<T*>(a.y)[t * a.ldy + n] = (T)fmaf((float)acc[i], a.sx[t] * s, b);
   }
+}
+
+// linear_q8_tile: a BM x BN tile of y to a workgroup, WM x WN of it to a
+// wavefront in 32 x 32 products, 128 codes of k a step.  Codes go from memory
+// straight into LDS, 16 bytes a lane, into the buffer that is not being
+// multiplied; one barrier a step.  A row's eight 16-byte chunks are permuted
+// (xor with its number's low bits) so that eight lanes reading a column of
+// chunks meet all banks; as LDS receives a wavefront's load in lane order, the
+// permutation is made in the addresses it loads from.  Rows past the end
+// repeat the last one and are not stored; the codes past the last whole 128 go
+// through registers, zeros after k.
+struct TileOrder {
+  uint32_t tiles_m, tiles_n, per_xcd, more;                // tiles / 8, tiles % 8
+};
+
+// The tile of a workgroup: workgroups go to the eight XCDs in turn, and each
+// XCD (its L2) takes consecutive tiles, in columns of four rows of tiles.
+__device__ __forceinline__ void place_tile(const TileOrder& o, uint32_t id, int* tm, int* tn) {
+  const uint32_t x = id % 8, i = id / 8;
+  const uint32_t tile = x * o.per_xcd + min(x, o.more) + i;
+  const uint32_t band = 4 * o.tiles_n;
+  const uint32_t b = tile / band, in = tile - b * band;
+  const uint32_t rows = min(4u, o.tiles_m - 4 * b);
+  *tn = (int)(in / rows);
+  *tm = (int)(4 * b + in - *tn * rows);
+}
+
+typedef __attribute__((address_space(1))) const void gvoid;
+typedef __attribute__((address_space(3))) void lvoid;
+
+template <int ROWS, int THREADS>
+__device__ __forceinline__ void codes_to_lds(const int8_t* base,
+                                             const uint32_t (&off)[ROWS * 8 / THREADS], int k0,
+                                             int8_t* lds) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+  for (int p = 0; p < ROWS * 8 / THREADS; ++p)
+    __builtin_amdgcn_global_load_lds((gvoid*)(base + k0 + off[p]),
+                                     (lvoid*)(lds + (p * THREADS + wave * 64) * 16), 16, 0, 0);
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8Linear a,
+                                                                             TileOrder order) {
+  constexpr int NW = BN / WN, THREADS = BM / WM * NW * 64;
+  constexpr int MT = WM / 32, NT = WN / 32;
+  constexpr int PX = BM * 8 / THREADS, PW = BN * 8 / THREADS;
+  __shared__ __align__(16) int8_t lx0[BM * 128], lx1[BM * 128], lw0[BN * 128], lw1[BN * 128];
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  int tm, tn;
+  place_tile(order, blockIdx.x, &tm, &tn);
+  const int64_t t0 = (int64_t)tm * BM;
+  const int n0 = tn * BN;
+  const int8_t* xb = a.x + t0 * a.ldx;
+  const int8_t* wb = a.w + (int64_t)n0 * a.ldw;
+  const int xrows = (int)min<int64_t>(BM, a.rows - t0), wrows = min(BN, a.d_out - n0);
+  // the 16-byte chunk `piece` of a buffer: row piece / 8, the row's chunk (piece % 8) ^ (row % 8)
+  uint32_t xo[PX], wo[PW];
+#pragma unroll
+  for (int p = 0; p < PX; ++p) {
+    const int piece = p * THREADS + tid, row = piece / 8;
+    xo[p] = (uint32_t)min(row, xrows - 1) * (uint32_t)a.ldx + ((piece ^ row) & 7) * 16;
+  }
+#pragma unroll
+  for (int p = 0; p < PW; ++p) {
+    const int piece = p * THREADS + tid, row = piece / 8;
+    wo[p] = (uint32_t)min(row, wrows - 1) * (uint32_t)a.ldw + ((piece ^ row) & 7) * 16;
+  }
+  const int mr = wave / NW * WM, nr = wave % NW * WN;
+  const int fr = lane % 32, fh = lane / 32;
+  i32x16 acc[MT][NT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[m][n][i] = 0;
+  auto multiply = [&](const int8_t* lx, const int8_t* lw) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int at = fr * 128 + ((2 * s + fh) ^ (fr & 7)) * 16;
+      i32x4 fx[MT], fw[NT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        fx[m] = *reinterpret_cast<const i32x4*>(lx + (mr + 32 * m) * 128 + at);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        fw[n] = *reinterpret_cast<const i32x4*>(lw + (nr + 32 * n) * 128 + at);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fx[m], fw[n], acc[m][n], 0, 0, 0);
+    }
+  };
+  const int whole = a.k / 128;
+  if (whole > 0) {
+    codes_to_lds<BM, THREADS>(xb, xo, 0, lx0);
+    codes_to_lds<BN, THREADS>(wb, wo, 0, lw0);
+  }
+  for (int s = 0; s < whole; s += 2) {
+    __syncthreads();                                       // this step's codes are there
+    if (s + 1 < whole) {
+      codes_to_lds<BM, THREADS>(xb, xo, (s + 1) * 128, lx1);
+      codes_to_lds<BN, THREADS>(wb, wo, (s + 1) * 128, lw1);
+    }
+    multiply(lx0, lw0);
+    if (s + 1 >= whole) break;
+    __syncthreads();
+    if (s + 2 < whole) {
+      codes_to_lds<BM, THREADS>(xb, xo, (s + 2) * 128, lx0);
+      codes_to_lds<BN, THREADS>(wb, wo, (s + 2) * 128, lw0);
+    }
+    multiply(lx1, lw1);
+  }
+  if (a.k % 128 != 0) {
+    const int k0 = whole * 128;
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < PX; ++p) {
+      const int piece = p * THREADS + tid, row = piece / 8;
+      *reinterpret_cast<i32x4*>(lx0 + piece * 16) =
+          codes16<true>(xb + (int64_t)min(row, xrows - 1) * a.ldx,
+                        k0 + ((piece ^ row) & 7) * 16, a.k);
+    }
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int piece = p * THREADS + tid, row = piece / 8;
+      *reinterpret_cast<i32x4*>(lw0 + piece * 16) =
+          codes16<true>(wb + (int64_t)min(row, wrows - 1) * a.ldw,
+                        k0 + ((piece ^ row) & 7) * 16, a.k);
+    }
+    __syncthreads();
+    multiply(lx0, lw0);
+  }
+  float sw[NT], bias[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int o = min(n0 + nr + 32 * n + fr, a.d_out - 1);
+    sw[n] = a.sw[o];
+    bias[n] = a.bias ? a.bias[o] : 0.0f;
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int64_t t = t0 + mr + 32 * m + 8 * (i / 4) + 4 * fh + i % 4;
+      if (t >= a.rows) continue;
+      const float sx = a.sx[t];
+      T* y = static_cast<T*>(a.y) + t * a.ldy;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int o = n0 + nr + 32 * n + fr;
+        if (o < a.d_out) y[o] = (T)fmaf((float)acc[m][n][i], sx * sw[n], bias[n]);
+      }
+    }
 }
 
 }  // namespace cs
