@@ -73,6 +73,17 @@ int linear_tiles(const cs::Q8Linear& a, hipStream_t s) {
   return launched();
 }
 
+constexpr int64_t kFusedElements = 8192;
+
+template <typename T, typename XT, int RT>
+int linear_few(const cs::Q8Linear& a, hipStream_t s) {
+  constexpr int NW = 8;
+  const size_t lds = sizeof(XT) > 1 ? (size_t)a.rows * round_up((size_t)a.k, 128) : 0;
+  hipLaunchKernelGGL((cs::linear_q8_few<T, XT, RT, NW>), dim3((unsigned)((a.d_out + 15) / 16)),
+                     dim3(NW * 64), lds, s, a);
+  return launched();
+}
+
 // ---------------------------------------------------------------- cache
 int cache_view(const cs_q8_cache* c, cs::CacheView* out) {
   if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return CS_ERR_ARG;
@@ -115,7 +126,7 @@ AttentionPlan attention_plan(const cs::CacheView& c, int tokens, int q_heads, in
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
   const int64_t items = (rows + per - 1) / per * c.heads;
-  int64_t splits = std::min<int64_t>({(p.many ? 512 : 1024) / items, (len + 127) / 128, 128});
+  int64_t splits = std::min<int64_t>({(p.many ? 512 : 1024) / items, (len + 127) / 128, cs::kMaxSplits});
   if (splits < 1) splits = 1;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
@@ -162,6 +173,14 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   cs::Q8Linear a{static_cast<const int8_t*>(x), ldx, sx, rows, k, w, ldw, sw, d_out, bias, y, ldy};
+  const bool w_al = aligned(w, 16) && ldw % 16 == 0 && ldw < (1 << 23);
+  // A few tokens are quantised by every workgroup of the product itself.
+  if (is_float(xt) && w_al && rows <= 16 && rows * k <= kFusedElements)
+    return with_float(yt, [&](auto ty) {
+      return with_float(xt, [&](auto tx) {
+        return linear_few<decltype(ty), decltype(tx), 1>(a, s);
+      });
+    });
   if (is_float(xt)) {
     const int64_t ld = (int64_t)round_up((size_t)k, 16);
     int8_t* q = static_cast<int8_t*>(ws);
@@ -171,8 +190,7 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     a.x = q; a.ldx = ld; a.sx = sq;
   }
   // whole 16-byte loads, offsets of a tile's rows in 32 bits
-  const bool al = aligned(a.x, 16) && aligned(w, 16) && a.ldx % 16 == 0 && ldw % 16 == 0 &&
-                  a.ldx < (1 << 23) && ldw < (1 << 23);
+  const bool al = w_al && aligned(a.x, 16) && a.ldx % 16 == 0 && a.ldx < (1 << 23);
   return with_float(yt, [&](auto t) {
     using T = decltype(t);
     if (!al) {
@@ -185,6 +203,9 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     auto tiles = [&](int bm, int bn) {
       return ((rows + bm - 1) / bm) * (((int64_t)d_out + bn - 1) / bn);
     };
+    if (rows <= 16) return linear_few<T, int8_t, 1>(a, s);
+    if (rows <= 32) return linear_few<T, int8_t, 2>(a, s);
+    if (rows <= 64) return linear_few<T, int8_t, 4>(a, s);
     if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64>(a, s);
     if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64>(a, s);
     return linear_tiles<T, 64, 64, 32, 32>(a, s);

@@ -767,34 +767,38 @@ __global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAt
     }
 }
 
-// attention_join: the parts of a row, in order, a wavefront to a row.
+// attention_join: the parts of a row, in order, a wavefront to a row.  Lane s
+// holds part s's weight, so the parts' loads wait for nothing but each other's
+// turn.
+constexpr int kMaxSplits = 64;
+
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
   const int lane = threadIdx.x % 64, d = a.c.d;
   const int64_t rows = (int64_t)a.tokens * a.q_heads;
   const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (row >= rows) return;
-  float top = kNegInf;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[s * rows + row].x);
+  float2 ml = float2{kNegInf, 0.0f};
+  if (lane < a.splits) ml = a.part_ml[lane * rows + row];
+  float top = ml.x;
+  for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
   const float base = top == kNegInf ? 0.0f : top;
-  float sum = 0.0f, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = a.part_ml[s * rows + row];
-    if (ml.y == 0.0f) continue;                            // a part without a key
-    const float f = exp2_fast(ml.x - base);
-    sum = fmaf(ml.y, f, sum);
-    const float* po = a.part_o + (s * rows + row) * d;
-    if (4 * lane < d) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(po + 4 * lane);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], f, y[i]);
-    }
-  }
+  const float f = exp2_fast(ml.x - base);                  // a part without a key: 0
+  float sum = ml.y * f;
+  for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+  const int ch = 4 * lane < d ? 4 * lane : 0;
+  const float* po = a.part_o + row * d + ch;
+  f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s)
+    y += *reinterpret_cast<const f32x4*>(po + s * rows * d) *
+         __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
   const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
   if (4 * lane < d) {
-    T* yp = static_cast<T*>(a.out) + row * d + 4 * lane;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) yp[i] = (T)(y[i] * inv);
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    y *= inv;
+    *reinterpret_cast<t4*>(static_cast<T*>(a.out) + row * d + ch) =
+        t4{(T)y[0], (T)y[1], (T)y[2], (T)y[3]};
   }
 }
 

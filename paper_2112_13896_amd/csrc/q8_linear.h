@@ -238,4 +238,121 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
     }
 }
 
+// linear_q8_few: few tokens, where reading w is the work.  16 output channels
+// to a workgroup of NW wavefronts, which take 128 codes of k in turn: a lane
+// loads 32 bytes of a row of w (the four lanes of a row 128 bytes together),
+// kept in flight four such steps deep, and multiplies them with RT tiles of 16
+// tokens, read the same way (the order of k inside a product only has to agree).
+// The wavefronts' int32 sums meet in LDS.  XT int8_t: tokens in codes.  A
+// float XT: every workgroup quantises the tokens itself, into LDS, while its
+// first loads of w are under way; that is one launch instead of two.
+constexpr int kFewSteps = 4;
+
+template <typename T, typename XT, int RT, int NW>
+__global__ __launch_bounds__(NW * 64) void linear_q8_few(Q8Linear a) {
+  constexpr bool kFloats = sizeof(XT) > 1;
+  extern __shared__ __align__(16) int8_t l_x[];            // floats: [rows][kpad] codes
+  __shared__ int l_sum[NW][RT][16][17];
+  __shared__ uint32_t l_max[16];
+  __shared__ float l_sx[16];
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int r = lane % 16, h = lane / 16;
+  const int n0 = blockIdx.x * 16, steps = (a.k + 127) / 128, kpad = steps * 128;
+  const int8_t* wr = a.w + (int64_t)min(n0 + r, a.d_out - 1) * a.ldw;
+  i32x4 w[kFewSteps][2];
+  auto load_w = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < kFewSteps; ++i) {
+      const int s = s0 + i * NW, e = s * 128 + 32 * h;
+      if (s >= steps) continue;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        w[i][y] = s + 1 < steps ? *reinterpret_cast<const i32x4*>(wr + e + 16 * y)
+                                : codes16<true>(wr, e + 16 * y, a.k);
+    }
+  };
+  load_w(wave);
+  if constexpr (kFloats) {
+    // quantise_rows' arithmetic; whole wavefronts share a row's vectors of eight
+    const XT* x = reinterpret_cast<const XT*>(a.x);
+    const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 &&
+                     (a.rows == 1 || a.ldx * sizeof(XT) % 16 == 0);
+    const int rows = (int)a.rows, nv = kpad / 8;
+    // rows below NW: NW / rows wavefronts to a row; else a wavefront to every NW-th row
+    const int per = max(1, NW / rows), first = wave / per, stride = NW / per;
+    auto fetch = [&](int row, int v, float (&f)[8]) {
+      const XT* p = x + row * a.ldx + 8 * v;
+      if (vec && 8 * v + 8 <= a.k) load8(p, f);
+      else load8_some(p, a.k - 8 * v, f);
+    };
+    const int l0 = wave % per * 64 + lane, lanes = per * 64;
+    if (tid < 16) l_max[tid] = 0;
+    __syncthreads();
+    for (int row = first; row < rows; row += stride) {
+      uint32_t top = 0;
+      for (int v = l0; v < nv; v += lanes) {
+        float f[8];
+        fetch(row, v, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, abs_bits(f[i]));
+      }
+      top = wave_max_u32(top);
+      if (lane == 0) atomicMax(&l_max[row], top);
+    }
+    __syncthreads();
+    for (int row = first; row < rows; row += stride) {
+      const RowScale rs = row_scale(l_max[row]);
+      if (l0 == 0) l_sx[row] = rs.s;
+      for (int v = l0; v < nv; v += lanes) {
+        float f[8];
+        fetch(row, v, f);
+        *reinterpret_cast<u32x2*>(l_x + row * kpad + 8 * v) = row_codes8(f, rs);
+      }
+    }
+    __syncthreads();
+  }
+  i32x4 acc[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+  for (int s0 = wave; s0 < steps; s0 += kFewSteps * NW) {
+    if (s0 != wave) load_w(s0);
+#pragma unroll
+    for (int i = 0; i < kFewSteps; ++i) {
+      const int s = s0 + i * NW, e = s * 128 + 32 * h;
+      if (s >= steps) continue;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const int row = min(16 * t + r, (int)a.rows - 1);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          i32x4 x;
+          if constexpr (kFloats)
+            x = *reinterpret_cast<const i32x4*>(l_x + row * kpad + e + 16 * y);
+          else if (s + 1 < steps)
+            x = *reinterpret_cast<const i32x4*>(a.x + row * a.ldx + e + 16 * y);
+          else
+            x = codes16<true>(a.x + row * a.ldx, e + 16 * y, a.k);
+          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][y], x, acc[t], 0, 0, 0);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) l_sum[wave][t][r][4 * h + i] = acc[t][i];
+  __syncthreads();
+  for (int i = tid; i < RT * 256; i += NW * 64) {
+    const int row = i / 16, n = i % 16, o = n0 + n;
+    if (row >= a.rows || o >= a.d_out) continue;
+    int sum = 0;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) sum += l_sum[v][row / 16][row % 16][n];
+    const float sx = kFloats ? l_sx[row % 16] : a.sx[row];
+    static_cast<T*>(a.y)[row * a.ldy + o] =
+        (T)fmaf((float)sum, sx * a.sw[o], a.bias ? a.bias[o] : 0.0f);
+  }
+}
+
 }  // namespace cs

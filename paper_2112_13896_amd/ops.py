@@ -845,15 +845,24 @@ def _float_dt(t: torch.dtype) -> int:
         raise TypeError(f"unsupported dtype {t}") from None
 
 
+def _stream_of(t: torch.Tensor) -> int:
+    """torch's current stream on the tensor's GPU, as _stream() without the Stream object (which
+    costs as much as a launch)."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
 def _rows(t: torch.Tensor, name: str):
-    """Device pointer and row stride of a GPU matrix whose rows are contiguous."""
+    """Device pointer, row stride and shape of a GPU matrix whose rows are contiguous."""
+    shape = t.shape
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.dim() != 2:
+    if len(shape) != 2:
         raise ValueError(f"{name} must be a matrix")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    ld, e = t.stride()
+    rows, c = shape
+    if e != 1 and c > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    return t.data_ptr(), ld if rows > 1 else max(ld, c), rows, c
 
 
 def _heads(t: torch.Tensor, name: str):
@@ -862,25 +871,28 @@ def _heads(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens][heads][d]")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    tokens, heads, d = t.shape
+    ts, hs, e = t.stride()
+    if e != 1 and d > 1:
         raise ValueError(f"{name}'s heads must be contiguous")
-    hs = t.stride(1) if t.shape[1] > 1 else t.shape[2]
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * hs, hs
+    if heads <= 1:
+        hs = d
+    return t.data_ptr(), ts if tokens > 1 else heads * hs, hs
 
 
 def _vector(t: torch.Tensor | None, name: str, dtype: torch.dtype, n: int):
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != (n,):
+    if t.dtype != dtype or t.shape != (n,):
         raise ValueError(f"{name} must be {dtype} [{n}]")
     return _dev(t, name)
 
 
-def _ws(ws: torch.Tensor | None, need: int, device):
-    """Pointer and size of a workspace, one made for the call where the caller keeps none
-    (torch's allocator orders its reuse on the stream)."""
+def _ws(ws: torch.Tensor | None, need, device):
+    """A workspace, its pointer and size; one of need() bytes made for the call where the caller
+    keeps none (torch's allocator orders its reuse on the stream)."""
     if ws is None:
-        ws = torch.empty((need,), dtype=torch.uint8, device=device)
+        ws = torch.empty((need(),), dtype=torch.uint8, device=device)
     return ws, _dev(ws, "ws"), ws.numel() * ws.element_size()
 
 
@@ -889,18 +901,17 @@ def quantise_rows(x: torch.Tensor, q: torch.Tensor | None = None,
     """Codes int8 [rows][c] and scales float32 [rows] of the rows of x (float32, float16 or
     bfloat16 [rows][c]): cs_quantise_rows.  Codes made here have a row stride that is a multiple
     of 16, which cs_linear_q8 reads fastest."""
-    px, ldx = _rows(x, "x")
-    rows, c = x.shape
+    px, ldx, rows, c = _rows(x, "x")
     if q is None:
         q = torch.empty((rows, (c + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :c]
     if q.dtype != torch.int8 or q.shape != x.shape:
         raise ValueError("q must be int8 of x's shape")
     if scale is None:
         scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
-    pq, ldq = _rows(q, "q")
+    pq, ldq, _, _ = _rows(q, "q")
     check("cs_quantise_rows", lib().cs_quantise_rows(
         _float_dt(x.dtype), px, ldx, rows, c, pq, ldq,
-        _vector(scale, "scale", torch.float32, rows), _stream()))
+        _vector(scale, "scale", torch.float32, rows), _stream_of(x)))
     return q, scale
 
 
@@ -919,29 +930,32 @@ def linear_q8(x: torch.Tensor, w: torch.Tensor, sw: torch.Tensor, sx: torch.Tens
     scales sw (quantise_rows of the weight matrix gives both).  x [rows][k] is int8 with scales
     sx, or a float tensor that the call quantises row by row.  out_dtype: x's by default, float32
     for int8 x."""
-    px, ldx = _rows(x, "x")
-    pw, ldw = _rows(w, "w")
-    rows, k = x.shape
-    d_out = w.shape[0]
-    if w.dtype != torch.int8 or w.shape[1] != k:
+    px, ldx, rows, k = _rows(x, "x")
+    pw, ldw, d_out, kw = _rows(w, "w")
+    xdt = x.dtype
+    if w.dtype != torch.int8 or kw != k:
         raise ValueError(f"w must be int8 [d_out][{k}]")
-    xt = CS_I8 if x.dtype == torch.int8 else _float_dt(x.dtype)
-    if (x.dtype == torch.int8) != (sx is not None):
+    codes = xdt == torch.int8
+    xt = CS_I8 if codes else _float_dt(xdt)
+    if codes != (sx is not None):
         raise ValueError("sx goes with int8 x")
     if out_dtype is None:
-        out_dtype = torch.float32 if x.dtype == torch.int8 else x.dtype
+        out_dtype = torch.float32 if codes else xdt
     if out is None:
-        out = torch.empty((rows, d_out), dtype=out_dtype, device=x.device)
-    if out.dtype != out_dtype or tuple(out.shape) != (rows, d_out):
-        raise ValueError(f"out must be {out_dtype} [{rows}][{d_out}]")
-    py, ldy = _rows(out, "out")
-    need = int(lib().cs_linear_q8_workspace_bytes(xt, rows, k, d_out))
-    ws, pws, nws = _ws(ws, need, x.device)
-    check("cs_linear_q8", lib().cs_linear_q8(
+        out = x.new_empty((rows, d_out), dtype=out_dtype)
+        py, ldy = out.data_ptr(), d_out
+    else:
+        py, ldy, yr, yc = _rows(out, "out")
+        if out.dtype != out_dtype or yr != rows or yc != d_out:
+            raise ValueError(f"out must be {out_dtype} [{rows}][{d_out}]")
+    L = lib()
+    ws, pws, nws = _ws(ws, lambda: L.cs_linear_q8_workspace_bytes(xt, rows, k, d_out), x.device)
+    st = L.cs_linear_q8(
         xt, px, ldx, _vector(sx, "sx", torch.float32, rows), rows, k, pw, ldw,
         _vector(sw, "sw", torch.float32, d_out), d_out,
         _vector(bias, "bias", torch.float32, d_out), _float_dt(out_dtype), py, ldy, pws, nws,
-        _stream()))
+        _stream_of(x))
+    check("cs_linear_q8", st)
     return out
 
 
@@ -968,6 +982,7 @@ class PagedCache:
         self.pages, self.heads, self.page, self.d = self.k.shape
         self._c = _lib.Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
                                self.v_scale.data_ptr(), *self.k.shape)
+        self._ref = ctypes.byref(self._c)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page: int, d: int, device="cuda") -> "PagedCache":
@@ -981,7 +996,7 @@ class PagedCache:
     def _ptr(self):
         if not self.k.is_cuda:
             raise ValueError("the cache must be on the GPU")
-        return ctypes.byref(self._c)
+        return self._ref
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
@@ -993,7 +1008,7 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torc
         raise ValueError(f"k and v must be of one type and [tokens][{cache.heads}][{cache.d}]")
     check("cs_cache_write", lib().cs_cache_write(
         cache._ptr(), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
-        _vector(slots, "slots", torch.int64, k.shape[0]), k.shape[0], _stream()))
+        _vector(slots, "slots", torch.int64, k.shape[0]), k.shape[0], _stream_of(k)))
 
 
 def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
@@ -1001,13 +1016,14 @@ def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
     """(k, v), each [tokens][heads][d] of `dtype`, of the slots' tokens: cs_cache_read."""
     shape = (slots.shape[0], cache.heads, cache.d)
     if out is None:
-        out = tuple(torch.empty(shape, dtype=dtype, device=slots.device) for _ in range(2))
-    for t in out:
-        if t.dtype != dtype or tuple(t.shape) != shape:
-            raise ValueError(f"out must be {dtype} {list(shape)}")
+        out = (slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype))
+    else:
+        for t in out:
+            if t.dtype != dtype or t.shape != shape:
+                raise ValueError(f"out must be {dtype} {list(shape)}")
     check("cs_cache_read", lib().cs_cache_read(
         cache._ptr(), _vector(slots, "slots", torch.int64, shape[0]), shape[0], _float_dt(dtype),
-        _dev(out[0], "out"), _dev(out[1], "out"), _stream()))
+        _dev(out[0], "out"), _dev(out[1], "out"), _stream_of(slots)))
     return out
 
 
@@ -1023,7 +1039,7 @@ def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.T
                               max_len: int | None = None) -> torch.Tensor:
     """Workspace of paged_attention for arguments of these shapes."""
     qt, ml = _attention_args(q, cache, table, max_len)
-    n = lib().cs_paged_attention_workspace_bytes(ctypes.byref(cache._c), qt, q.shape[0],
+    n = lib().cs_paged_attention_workspace_bytes(cache._ref, qt, q.shape[0],
                                                  q.shape[1], table.shape[0], table.shape[1], ml)
     return torch.empty((int(n),), dtype=torch.uint8, device=q.device)
 
@@ -1041,16 +1057,18 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
     pq, ldq, hsq = _heads(q, "q")
     b = table.shape[0]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if out.dtype != q.dtype or out.shape != q.shape:
+        out = q.new_empty(q.shape)
+    elif out.dtype != q.dtype or out.shape != q.shape:
         raise ValueError("out must be of q's type and shape")
-    need = int(lib().cs_paged_attention_workspace_bytes(
-        ctypes.byref(cache._c), qt, q.shape[0], q.shape[1], b, table.shape[1], ml))
-    ws, pws, nws = _ws(ws, need, q.device)
-    check("cs_paged_attention", lib().cs_paged_attention(
-        cache._ptr(), qt, pq, ldq, hsq, q.shape[0], q.shape[1], b, _dev(table, "table"),
-        table.shape[1], _vector(lens, "lens", torch.int32, b),
-        _vector(starts, "starts", torch.int32, b + 1), ml,
+    L = lib()
+    tokens, q_heads, _ = q.shape
+    width = table.shape[1]
+    ws, pws, nws = _ws(ws, lambda: L.cs_paged_attention_workspace_bytes(
+        cache._ref, qt, tokens, q_heads, b, width, ml), q.device)
+    st = L.cs_paged_attention(
+        cache._ptr(), qt, pq, ldq, hsq, tokens, q_heads, b, _dev(table, "table"), width,
+        _vector(lens, "lens", torch.int32, b), _vector(starts, "starts", torch.int32, b + 1), ml,
         1.0 / math.sqrt(cache.d) if scale is None else scale, window, _dev(out, "out"), pws, nws,
-        _stream()))
+        _stream_of(q))
+    check("cs_paged_attention", st)
     return out
