@@ -325,12 +325,14 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
       hipLaunchKernelGGL((cs::attention_few<T, decltype(dt)::value>), grid, block, 0, s, a);
     };
     auto many = [&](auto dt) {
-      constexpr int DT = decltype(dt)::value;
-      hipLaunchKernelGGL((cs::attention_many<T, DT>), grid, block, 2 * sizeof(cs::ManyLds<DT>), s,
+      constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
+      hipLaunchKernelGGL((cs::attention_many<T, W>), grid, block, 2 * sizeof(cs::ManyLds<DT>), s,
                          a);
     };
-    if (p.many) with_width(c.d, many);
-    else with_width(c.d, few);
+    if (!p.many) with_width(c.d, few);
+    else if (c.d > 64 && c.d <= 96) many(std::integral_constant<int, 96>{});
+    else if (c.d > 128 && c.d <= 192) many(std::integral_constant<int, 192>{});
+    else with_width(c.d, many);
     int r = launched();
     if (r == CS_OK && p.splits > 1) {
       hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, a);

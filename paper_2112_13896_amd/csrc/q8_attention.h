@@ -22,7 +22,9 @@
 //    maximum of x_j over the keys the row sees, w_j = a_j 2^(x_j - m + 12) is
 //    at most 2^13 and the denominator is the sum of 2^(x_j - m + 12) 2^-E_j.
 //    A token with large values that a row does not see, or hardly weighs,
-//    takes no precision from the others.
+//    takes no precision from the others.  m follows the maximum only when that
+//    is more than 4 (2^2) above it: halves have the room, and the sums so far
+//    are rescaled rarely.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -164,6 +166,15 @@ struct FAdd {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kHead = 12.0f;                             // weights are scaled by 2^12
+constexpr float kSlack = 2.0f;                             // and may be 2^2 times that
+
+// max(a, b, c), NaN ignored, as one instruction whatever the compiler knows of
+// its operands.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // A query row's power of two and what turns its products into log2 units.
 struct RowNorm {
@@ -384,11 +395,9 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
         }
       }
     }
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-    top = fmaxf(m, reduce_x16_x32(top, FMax{}));
-    if (__builtin_amdgcn_ballot_w64(top > m)) {
+    float top = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(m, x[6], x[7]));
+    top = reduce_x16_x32(top, FMax{});
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
       const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
       l *= f;
 #pragma unroll
@@ -481,26 +490,30 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
 // whose place in a row is permuted (xor) so that eight lanes that read or
 // write one column of chunks meet all banks; two buffers, the next step's
 // codes in flight in registers under this one's arithmetic, one barrier a
-// step.  Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y
-// = 0..3) of row r.  So a lane's eight weights of 16 keys are those at 4 h ..
+// step.  Two wavefronts bring the values, two the keys, a block of 16 keys (a
+// piece of one page, so its address is scalar) at a time.  W <= DT: channels
+// that are computed, d rounded up to 32.
+// Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y =
+// 0..3) of row r.  So a lane's eight weights of 16 keys are those at 4 h ..
 // and 8 + 4 h .., and the values' chunk g = 2 s + h of a channel holds just
 // the keys 16 s + 4 h .. +3 and 16 s + 8 + 4 h .. +3.
+// Here a = 1, E = log2(sv), taken once a step.
 template <int DT>
 struct ManyLds {
   _Float16 k[64][DT];
   _Float16 v[DT][64];
-  float ks[64], ls[64], rs[64];                            // ks, log2(vs), 1 / vs
+  float ks[64], ls[64], rs[64];                            // ks * c0, log2(vs), 1 / vs
 };
 
 __device__ __forceinline__ int value_chunk(int ch, int g) {
   return g ^ ((ch & 3) * 2) ^ ((ch >> 2) & 7);
 }
 
-template <typename T, int DT>
-__global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAttention a) {
+template <typename T, int W>
+__global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAttention a) {
+  constexpr int DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;
-  constexpr int KS = DT / 16, CT = DT / 32;
-  constexpr int KP = DT / 64;                              // key pieces of 16 codes a thread
+  constexpr int KS = W / 16, CT = W / 32;
   extern __shared__ __align__(16) unsigned char smem[];
   ManyLds<DT>* lds = reinterpret_cast<ManyLds<DT>*>(smem);
   const int tid = threadIdx.x, lane = tid % 64;
@@ -531,8 +544,12 @@ __global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAt
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
   const int steps = hi > j0 ? (hi - j0 + 63) / 64 : 0;
 
+  // Queries whose largest element lies in [1, 2^10) are taken as they are; c0
+  // is then all that turns a product into log2 units, and it is multiplied
+  // into the keys' scales.  Other rows get a power of two (row_mul undoes it).
+  const float c0 = a.scale * 1.4426950408889634f * kCodeScale;
   f16x8 q[NP][KS];
-  float c;
+  float row_mul = 1.0f;
   {
     const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
     uint32_t top = 0;
@@ -547,101 +564,131 @@ __global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAt
       }
     }
     const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    const RowNorm nm = row_norm(__uint_as_float(max(s32[0], s32[1])), a.scale);
-    c = nm.c;
+    const float big = __uint_as_float(max(s32[0], s32[1]));
+    const bool bad = !(big < __builtin_inff());
+    int shift = 0;
+    if (!bad && big > 0.0f && !(big >= 1.0f && big < 1024.0f))
+      shift = 9 - __builtin_amdgcn_frexp_expf(big);
+    row_mul = ldexpf(1.0f, -shift);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int ch = 16 * s + 8 * h;
       if (ch < d) load_q8(qp + ch, a.q_vec, f);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        f[e] = nm.bad ? __uint_as_float(0x7FC00000u) : ch < d ? ldexpf(f[e], nm.shift) : 0.0f;
+        f[e] = bad ? __uint_as_float(0x7FC00000u) : ch < d ? ldexpf(f[e], shift) : 0.0f;
       f16x8 p[NP];
       split_f16<NP>(f, p);
 #pragma unroll
       for (int n = 0; n < NP; ++n) q[n][s] = p[n];
     }
   }
+  const bool scaled = __builtin_amdgcn_ballot_w64(row_mul != 1.0f) != 0;
 
-  // staging: which codes this thread brings
+  // staging: this wavefront's blocks of 16 keys are 2 half and 2 half + 1
   const int32_t* table = a.table + (int64_t)t.b * a.table_width;
   const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
-  auto page_of = [&](int j) { return table[min(j, hi - 1) >> lg]; };
-  auto row_at = [&](int page, int j) {                     // a page outside the cache: any row
-    return (((int64_t)((uint32_t)page < (uint32_t)n_pages ? page : 0) * a.c.heads + head) << lg) +
-           (j & in_page);
-  };
-  constexpr int PR = DT / 16;                              // pieces of a key
-  const int k_key = tid / PR, k_ch = tid % PR * 16;        // + 256 / PR keys a piece
-  constexpr int VR = DT / 4;                               // dwords of a value
-  constexpr int VG = DT == 64 ? 8 : 256 / VR;              // groups of keys a round, of 8
-  constexpr int VN = 8 / VG;
-  const int v_ch = tid % VR * 4, v_g = tid / VR;           // DT 64: the second half has none
-  int kpage[KP], vpage[VN], spage = 0;
-  u32x4 kreg[KP];
-  uint32_t vreg[VN][8];
-  float ks_reg = 0.0f, vs_reg = 0.0f;
-  bool s_ok = false;
+  const bool brings_values = wave < 2;
+  const int half = wave % 2;
+  constexpr int KB = DT / 64;                              // key loads a block, 16 bytes a lane
+  constexpr int PR = DT / 16;                              // lanes to a key
+  const int k_key = lane / PR, k_ch = lane % PR * 16;      // + 64 / PR keys a load
+  constexpr int VD = DT == 256 ? 2 : 1;                    // dwords a lane and value row
+  constexpr int VR = DT / (4 * VD);                        // lanes to a value
+  const int v_g = lane / VR, v_ch = lane % VR * 4 * VD;    // (DT 64: lanes from 32 on have none)
+  const int k_off = k_key * d + (k_ch < d ? k_ch : 0);
+  const int v_off = 4 * (v_g & 1) * d + (v_ch < d ? v_ch : 0);
+  uint32_t reg[2][8 * VD];                                 // [block]: keys 4 KB dwords, values 8 VD
+  float meta = 0.0f;
+  int page[4];
   auto pages = [&](int j) {
 #pragma unroll
-    for (int p = 0; p < KP; ++p) kpage[p] = page_of(j + k_key + p * (256 / PR));
-#pragma unroll
-    for (int p = 0; p < VN; ++p) vpage[p] = page_of(j + (v_g + p * VG) / 2 * 16);
-    spage = page_of(j + lane);
+    for (int b = 0; b < 4; ++b)
+      page[b] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * b, hi - 1) >> lg]);
+  };
+  // first row of block b; a page outside the cache: any rows, hidden by `meta`
+  auto block_row = [&](int pg, int j, int b) {
+    return (((int64_t)((uint32_t)pg < (uint32_t)n_pages ? pg : 0) * a.c.heads + head) << lg) +
+           ((j + 16 * b) & in_page);
   };
   auto fetch = [&](int j) {
 #pragma unroll
-    for (int p = 0; p < KP; ++p) {
-      const int64_t at = row_at(kpage[p], j + k_key + p * (256 / PR));
-      kreg[p] = *reinterpret_cast<const u32x4*>(a.c.k + at * d + (k_ch < d ? k_ch : 0));
-    }
+    for (int x = 0; x < 2; ++x) {
+      const int b = 2 * half + x;
+      const int64_t at = block_row(half ? page[2 + x] : page[x], j, b) * d;
+      if (brings_values) {
+        const int8_t* vp = a.c.v + at;
 #pragma unroll
-    for (int p = 0; p < VN; ++p) {
-      if (DT == 64 && v_g >= 8) break;
-      const int g = v_g + p * VG, key = g / 2 * 16 + g % 2 * 4;
-      const int8_t* vp = a.c.v + row_at(vpage[p], j + key) * d + (v_ch < d ? v_ch : 0);
+        for (int i = 0; i < 8; ++i) {
+          uint32_t w[VD];
+          __builtin_memcpy(
+              w, __builtin_assume_aligned(vp + (i / 4 * 8 + i % 4) * d + (uint32_t)v_off, 4 * VD),
+              4 * VD);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        vreg[p][i] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)(i / 4 * 8 + i % 4) * d);
+          for (int y = 0; y < VD; ++y) reg[x][8 * y + i] = w[y];
+        }
+      } else {
+        const int8_t* kp = a.c.k + at;
+#pragma unroll
+        for (int p = 0; p < KB; ++p) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + p * (64 / PR) * d + (uint32_t)k_off);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) reg[x][4 * p + y] = w[y];
+        }
+      }
     }
-    if (wave == 0) {
-      const int64_t at = row_at(spage, j + lane);
-      s_ok = (uint32_t)spage < (uint32_t)n_pages;
-      ks_reg = a.c.ks[at];
-      vs_reg = a.c.vs[at];
+    if (!brings_values) {                                  // a lane has key `lane` of the step
+      const int b = lane / 16;
+      const int pg = b == 0 ? page[0] : b == 1 ? page[1] : b == 2 ? page[2] : page[3];
+      const int64_t at = block_row(pg, j, b) + lane % 16;
+      meta = (half ? a.c.vs : a.c.ks)[at];
+      // no page: weight 0
+      if ((uint32_t)pg >= (uint32_t)n_pages) meta = half ? -1.0f : 0.0f;
     }
   };
-  auto stage = [&](ManyLds<DT>& b) {
+  auto stage = [&](ManyLds<DT>& s) {
 #pragma unroll
-    for (int p = 0; p < KP; ++p) {
-      const int key = k_key + p * (256 / PR), ck = k_ch / 8;
-      *reinterpret_cast<f16x8*>(&b.k[key][((ck + 0) ^ (key & 7)) * 8]) =
-          codes_f16(kreg[p][0], kreg[p][1]);
-      *reinterpret_cast<f16x8*>(&b.k[key][((ck + 1) ^ (key & 7)) * 8]) =
-          codes_f16(kreg[p][2], kreg[p][3]);
+    for (int x = 0; x < 2; ++x) {
+      const int b = 2 * half + x;
+      if (brings_values) {
+        if (DT == 64 && v_g >= 2) continue;
+        const int g = 2 * b + v_g;
+#pragma unroll
+        for (int y = 0; y < VD; ++y) {
+          uint32_t w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = reg[x][8 * y + i] ^ kFlip;
+          const int ch = v_ch + 4 * y;
+          *reinterpret_cast<f16x8*>(&s.v[ch + 0][value_chunk(ch + 0, g) * 8]) =
+              codes_f16_across<0>(w);
+          *reinterpret_cast<f16x8*>(&s.v[ch + 1][value_chunk(ch + 1, g) * 8]) =
+              codes_f16_across<1>(w);
+          *reinterpret_cast<f16x8*>(&s.v[ch + 2][value_chunk(ch + 2, g) * 8]) =
+              codes_f16_across<2>(w);
+          *reinterpret_cast<f16x8*>(&s.v[ch + 3][value_chunk(ch + 3, g) * 8]) =
+              codes_f16_across<3>(w);
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < KB; ++p) {
+          const int key = 16 * b + p * (64 / PR) + k_key, ck = k_ch / 8;
+          *reinterpret_cast<f16x8*>(&s.k[key][((ck + 0) ^ (key & 7)) * 8]) =
+              codes_f16(reg[x][4 * p], reg[x][4 * p + 1]);
+          *reinterpret_cast<f16x8*>(&s.k[key][((ck + 1) ^ (key & 7)) * 8]) =
+              codes_f16(reg[x][4 * p + 2], reg[x][4 * p + 3]);
+        }
+      }
     }
-#pragma unroll
-    for (int p = 0; p < VN; ++p) {
-      if (DT == 64 && v_g >= 8) break;
-      const int g = v_g + p * VG;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) vreg[p][i] ^= kFlip;
-      *reinterpret_cast<f16x8*>(&b.v[v_ch + 0][value_chunk(v_ch + 0, g) * 8]) =
-          codes_f16_across<0>(vreg[p]);
-      *reinterpret_cast<f16x8*>(&b.v[v_ch + 1][value_chunk(v_ch + 1, g) * 8]) =
-          codes_f16_across<1>(vreg[p]);
-      *reinterpret_cast<f16x8*>(&b.v[v_ch + 2][value_chunk(v_ch + 2, g) * 8]) =
-          codes_f16_across<2>(vreg[p]);
-      *reinterpret_cast<f16x8*>(&b.v[v_ch + 3][value_chunk(v_ch + 3, g) * 8]) =
-          codes_f16_across<3>(vreg[p]);
-    }
-    if (wave == 0) {
-      // values all zero: a scale far below, their codes are 0; no page: weight 0
-      const float sv = vs_reg == 0.0f ? 0x1p-60f : fmaxf(vs_reg, 0x1p-120f);
-      const bool num = vs_reg == vs_reg;
-      b.ks[lane] = s_ok ? ks_reg : 0.0f;
-      b.ls[lane] = !s_ok ? kNegInf : num ? __builtin_amdgcn_logf(sv) : vs_reg;
-      b.rs[lane] = num ? 1.0f / sv : 1.0f;
+    if (!brings_values) {
+      if (half) {
+        // values all zero: a scale far below, their codes are 0
+        const float sv = meta == 0.0f ? 0x1p-60f : fmaxf(meta, 0x1p-120f);
+        const bool num = meta == meta;
+        s.ls[lane] = meta < 0.0f ? kNegInf : num ? __builtin_amdgcn_logf(sv) : meta;
+        s.rs[lane] = num ? 1.0f / sv : 1.0f;
+      } else {
+        s.ks[lane] = meta * c0;
+      }
     }
   };
 
@@ -667,42 +714,51 @@ __global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAt
       pages(j + 128);
     }
     if (j <= pos1 && j + 63 >= see0) {                     // some row sees a key of the step
-      float x[2][16];
-      float top = kNegInf;
+      f32x16 s[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x16 s;
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+        for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+      // 16-bit queries: the two products take turns; fp32's are one after the other, they are
+      // longer and leave fewer registers
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const f16x8 kf =
-              *reinterpret_cast<const f16x8*>(&b.k[32 * u + r][((2 * k + h) ^ (r & 7)) * 8]);
+      for (int i = 0; i < 2 * KS; ++i) {
+        const int u = NP == 1 ? i % 2 : i / KS, k = NP == 1 ? i / 2 : i % KS;
+        const f16x8 kf =
+            *reinterpret_cast<const f16x8*>(&b.k[32 * u + r][((2 * k + h) ^ (r & 7)) * 8]);
 #pragma unroll
-          for (int n = 0; n < NP; ++n)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s, 0, 0, 0);
-        }
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const f32x4 ks = *reinterpret_cast<const f32x4*>(&b.ks[32 * u + 8 * y + 4 * h]);
-          const f32x4 ls = *reinterpret_cast<const f32x4*>(&b.ls[32 * u + 8 * y + 4 * h]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[u][4 * y + i] = fmaf(s[4 * y + i] * ks[i], c, ls[i]);
-        }
+        for (int n = 0; n < NP; ++n)
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s[u], 0, 0, 0);
       }
-      if (j + 63 > pos0 || j < see1) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = j + 32 * u + 8 * (i / 4) + 4 * h + i % 4;
-            if (key > pos || key < see) x[u][i] = kNegInf;
-          }
+      if (scaled) {
+        s[0] *= row_mul;
+        s[1] *= row_mul;
       }
+      float x[32];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(x[0][i], x[1][i]));
-      top = fmaxf(m, reduce_x32(top, FMax{}));
-      if (__builtin_amdgcn_ballot_w64(top > m)) {
+      for (int y = 0; y < 8; ++y) {
+        const f32x4 ks = *reinterpret_cast<const f32x4*>(&b.ks[8 * y + 4 * h]);
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(&b.ls[8 * y + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * y + i] = fmaf(s[y / 4][y % 4 * 4 + i], ks[i], ls[i]);
+      }
+      if (j + 63 > pos0) {
+        const int last = pos - j - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (8 * (i / 4) + i % 4 > last) x[i] = kNegInf;
+      }
+      if (j < see1) {
+        const int first = see - j - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (8 * (i / 4) + i % 4 < first) x[i] = kNegInf;
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) top = max3(top, x[i], x[i + 1]);
+      top = reduce_x32(top, FMax{});
+      if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
         const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
         l *= f;
 #pragma unroll
@@ -711,32 +767,29 @@ __global__ __launch_bounds__(256, DT == 256 ? 1 : 2) void attention_many(PagedAt
       }
       const float base = m == kNegInf ? 0.0f : m - kHead;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int s = 0; s < 4; ++s) {
+        float w[8];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          float w[8];
+        for (int y = 0; y < 2; ++y) {
+          const f32x4 rs = *reinterpret_cast<const f32x4*>(&b.rs[16 * s + 8 * y + 4 * h]);
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const f32x4 rs =
-                *reinterpret_cast<const f32x4*>(&b.rs[32 * u + 16 * s + 8 * y + 4 * h]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              w[4 * y + i] = exp2_fast(x[u][8 * s + 4 * y + i] - base);
-              l = fmaf(w[4 * y + i], rs[i], l);
-            }
-          }
-          f16x8 p[NP];
-          split_f16<NP>(w, p);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            const int ch = 32 * ct + r;
-            const f16x8 vf = *reinterpret_cast<const f16x8*>(
-                &b.v[ch][value_chunk(ch, 4 * u + 2 * s + h) * 8]);
-#pragma unroll
-            for (int n = 0; n < NP; ++n)
-              o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);
+          for (int i = 0; i < 4; ++i) {
+            w[4 * y + i] = exp2_fast(x[8 * s + 4 * y + i] - base);
+            l = fmaf(w[4 * y + i], rs[i], l);
           }
         }
+        f16x8 p[NP];
+        split_f16<NP>(w, p);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const int ch = 32 * ct + r;
+          const f16x8 vf =
+              *reinterpret_cast<const f16x8*>(&b.v[ch][value_chunk(ch, 2 * s + h) * 8]);
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);
+        }
+      }
     }
     if (more) stage(lds[(step + 1) & 1]);
     __syncthreads();
