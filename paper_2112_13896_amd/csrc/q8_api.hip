@@ -326,7 +326,7 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
     };
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
-      hipLaunchKernelGGL((cs::attention_many<T, W>), grid, block, 2 * sizeof(cs::ManyLds<DT>), s,
+      hipLaunchKernelGGL((cs::attention_many<T, W>), grid, block, cs::ManyLds<DT>::bytes, s,
                          a);
     };
     if (!p.many) with_width(c.d, few);

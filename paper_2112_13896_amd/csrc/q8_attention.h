@@ -489,33 +489,38 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
 // all four: keys [64][DT], values transposed [DT][64], both in 16-byte chunks
 // whose place in a row is permuted (xor) so that eight lanes that read or
 // write one column of chunks meet all banks; two buffers, the next step's
-// codes in flight in registers under this one's arithmetic, one barrier a
-// step.  Two wavefronts bring the values, two the keys, a block of 16 keys (a
-// piece of one page, so its address is scalar) at a time.  W <= DT: channels
-// that are computed, d rounded up to 32.
+// codes are turned at the start of a step, beside its first products, and the
+// ones after that are then on their way in registers under all of its
+// arithmetic; one barrier a step.  Two wavefronts bring the values, two the
+// keys, a block of 16 keys (a piece of one page, so its address is scalar) at
+// a time.  W <= DT: channels that are computed, d rounded up to 32.
 // Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y =
 // 0..3) of row r.  So a lane's eight weights of 16 keys are those at 4 h ..
 // and 8 + 4 h .., and the values' chunk g = 2 s + h of a channel holds just
 // the keys 16 s + 4 h .. +3 and 16 s + 8 + 4 h .. +3.
 // Here a = 1, E = log2(sv), taken once a step.
+//
+// Where a chunk lies: key k's chunk i (channels 8 i ..) at byte (k DT 2) +
+// 16 (i ^ (k & 7)), channel c's chunk g of values at byte 128 c +
+// 16 (g ^ 2 (c & 3) ^ ((c >> 2) & 7)).
 template <int DT>
-struct ManyLds {
-  _Float16 k[64][DT];
-  _Float16 v[DT][64];
-  float ks[64], ls[64], rs[64];                            // ks * c0, log2(vs), 1 / vs
+struct ManyLds {                                           // bytes
+  static constexpr int k = 0;                              // [2][64][DT] halves
+  static constexpr int v = 2 * 64 * DT * 2;                // [2][DT][64] halves
+  static constexpr int ks = 2 * v;                         // [2][64] ks * c0
+  static constexpr int ls = ks + 512;                      // [2][64] log2(vs)
+  static constexpr int rs = ls + 512;                      // [2][64] 1 / vs
+  static constexpr int bytes = rs + 512;
+  static constexpr int buffer = 64 * DT * 2;               // one of two, keys or values
 };
-
-__device__ __forceinline__ int value_chunk(int ch, int g) {
-  return g ^ ((ch & 3) * 2) ^ ((ch >> 2) & 7);
-}
 
 template <typename T, int W>
 __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAttention a) {
   constexpr int DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;
   constexpr int KS = W / 16, CT = W / 32;
+  using At = ManyLds<DT>;
   extern __shared__ __align__(16) unsigned char smem[];
-  ManyLds<DT>* lds = reinterpret_cast<ManyLds<DT>*>(smem);
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int r = lane % 32, h = lane / 32, d = a.c.d;
@@ -534,11 +539,10 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   tile_keys(a, t, (int)fdiv((uint32_t)t.row0, a.by_group),
             (int)fdiv((uint32_t)(rows_end - 1), a.by_group), &lo, &hi);
   const int pos = back + tok, see = a.window > 0 ? pos - a.window + 1 : 0;
-  // the wavefront's rows: all see up to pos0 and from see1 on, none from pos1 + 1 on or before see0
+  // the wavefront's rows all see up to pos0 and from see1 on
   const int w0 = min(t.row0 + wave * 32, t.rows - 1), w1 = min(w0 + 31, t.rows - 1);
   const int pos0 = back + (int)fdiv((uint32_t)w0, a.by_group);
   const int pos1 = back + (int)fdiv((uint32_t)w1, a.by_group);
-  const int see0 = a.window > 0 ? pos0 - a.window + 1 : 0;
   const int see1 = a.window > 0 ? pos1 - a.window + 1 : 0;
   const int j0 = lo / 64 * 64 + split * a.chunk;
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
@@ -596,17 +600,19 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   constexpr int VD = DT == 256 ? 2 : 1;                    // dwords a lane and value row
   constexpr int VR = DT / (4 * VD);                        // lanes to a value
   const int v_g = lane / VR, v_ch = lane % VR * 4 * VD;    // (DT 64: lanes from 32 on have none)
-  const int k_off = k_key * d + (k_ch < d ? k_ch : 0);
-  const int v_off = 4 * (v_g & 1) * d + (v_ch < d ? v_ch : 0);
+  // byte of a block that this lane loads first (channels past d: any)
+  const uint32_t off = brings_values ? 4 * (v_g & 1) * d + (v_ch < d ? v_ch : 0)
+                                     : k_key * d + (k_ch < d ? k_ch : 0);
   uint32_t reg[2][8 * VD];                                 // [block]: keys 4 KB dwords, values 8 VD
   float meta = 0.0f;
+  bool meta_ok = false;
   int page[4];
   auto pages = [&](int j) {
 #pragma unroll
     for (int b = 0; b < 4; ++b)
       page[b] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * b, hi - 1) >> lg]);
   };
-  // first row of block b; a page outside the cache: any rows, hidden by `meta`
+  // first row of block b; a page outside the cache: any rows, hidden by `meta_ok`
   auto block_row = [&](int pg, int j, int b) {
     return (((int64_t)((uint32_t)pg < (uint32_t)n_pages ? pg : 0) * a.c.heads + head) << lg) +
            ((j + 16 * b) & in_page);
@@ -617,21 +623,19 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       const int b = 2 * half + x;
       const int64_t at = block_row(half ? page[2 + x] : page[x], j, b) * d;
       if (brings_values) {
-        const int8_t* vp = a.c.v + at;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+          const int8_t* vp = a.c.v + at + (i / 4 * 8 + i % 4) * d;
           uint32_t w[VD];
-          __builtin_memcpy(
-              w, __builtin_assume_aligned(vp + (i / 4 * 8 + i % 4) * d + (uint32_t)v_off, 4 * VD),
-              4 * VD);
+          __builtin_memcpy(w, __builtin_assume_aligned(vp + off, 4 * VD), 4 * VD);
 #pragma unroll
           for (int y = 0; y < VD; ++y) reg[x][8 * y + i] = w[y];
         }
       } else {
-        const int8_t* kp = a.c.k + at;
 #pragma unroll
         for (int p = 0; p < KB; ++p) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + p * (64 / PR) * d + (uint32_t)k_off);
+          const int8_t* kp = a.c.k + at + p * (64 / PR) * d;
+          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + off);
 #pragma unroll
           for (int y = 0; y < 4; ++y) reg[x][4 * p + y] = w[y];
         }
@@ -641,53 +645,56 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       const int b = lane / 16;
       const int pg = b == 0 ? page[0] : b == 1 ? page[1] : b == 2 ? page[2] : page[3];
       const int64_t at = block_row(pg, j, b) + lane % 16;
-      meta = (half ? a.c.vs : a.c.ks)[at];
-      // no page: weight 0
-      if ((uint32_t)pg >= (uint32_t)n_pages) meta = half ? -1.0f : 0.0f;
+      meta = (half ? a.c.vs : a.c.ks)[at];                 // (not touched here: that would wait)
+      meta_ok = (uint32_t)pg < (uint32_t)n_pages;
     }
   };
-  auto stage = [&](ManyLds<DT>& s) {
+  auto put = [&](int at, f16x8 v) { *reinterpret_cast<f16x8*>(smem + at) = v; };
+  // the lane's row in LDS and the place of its first chunk there; block and channel (values) or
+  // key (keys) below only turn its low bits
+  const int put_row = brings_values ? At::v + v_ch * 128 : At::k + (32 * half + k_key) * DT * 2;
+  const int put_bits = 16 * (brings_values ? (4 * half + (v_g & 1)) ^ ((v_ch >> 2) & 7)
+                                           : (k_ch / 8) ^ (k_key & 7));
+  auto stage = [&](auto par) {                             // buffer par
+    constexpr int P = decltype(par)::value, kBuf = P * At::buffer;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int b = 2 * half + x;
       if (brings_values) {
         if (DT == 64 && v_g >= 2) continue;
-        const int g = 2 * b + v_g;
 #pragma unroll
         for (int y = 0; y < VD; ++y) {
           uint32_t w[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) w[i] = reg[x][8 * y + i] ^ kFlip;
-          const int ch = v_ch + 4 * y;
-          *reinterpret_cast<f16x8*>(&s.v[ch + 0][value_chunk(ch + 0, g) * 8]) =
-              codes_f16_across<0>(w);
-          *reinterpret_cast<f16x8*>(&s.v[ch + 1][value_chunk(ch + 1, g) * 8]) =
-              codes_f16_across<1>(w);
-          *reinterpret_cast<f16x8*>(&s.v[ch + 2][value_chunk(ch + 2, g) * 8]) =
-              codes_f16_across<2>(w);
-          *reinterpret_cast<f16x8*>(&s.v[ch + 3][value_chunk(ch + 3, g) * 8]) =
-              codes_f16_across<3>(w);
+          auto at = [&](int c) {
+            return kBuf + put_row + (put_bits ^ 16 * ((2 * x) ^ (2 * c) ^ y)) + (4 * y + c) * 128;
+          };
+          put(at(0), codes_f16_across<0>(w));
+          put(at(1), codes_f16_across<1>(w));
+          put(at(2), codes_f16_across<2>(w));
+          put(at(3), codes_f16_across<3>(w));
         }
       } else {
 #pragma unroll
         for (int p = 0; p < KB; ++p) {
-          const int key = 16 * b + p * (64 / PR) + k_key, ck = k_ch / 8;
-          *reinterpret_cast<f16x8*>(&s.k[key][((ck + 0) ^ (key & 7)) * 8]) =
-              codes_f16(reg[x][4 * p], reg[x][4 * p + 1]);
-          *reinterpret_cast<f16x8*>(&s.k[key][((ck + 1) ^ (key & 7)) * 8]) =
-              codes_f16(reg[x][4 * p + 2], reg[x][4 * p + 3]);
+          const int first = p * (64 / PR), turn = 16 * (first & 7);
+          const int at = kBuf + put_row + (16 * x + first) * DT * 2;
+          put(at + (put_bits ^ turn), codes_f16(reg[x][4 * p], reg[x][4 * p + 1]));
+          put(at + (put_bits ^ turn ^ 16), codes_f16(reg[x][4 * p + 2], reg[x][4 * p + 3]));
         }
       }
     }
     if (!brings_values) {
+      float* to = reinterpret_cast<float*>(smem + At::ks + P * 256) + lane;
       if (half) {
         // values all zero: a scale far below, their codes are 0
         const float sv = meta == 0.0f ? 0x1p-60f : fmaxf(meta, 0x1p-120f);
         const bool num = meta == meta;
-        s.ls[lane] = meta < 0.0f ? kNegInf : num ? __builtin_amdgcn_logf(sv) : meta;
-        s.rs[lane] = num ? 1.0f / sv : 1.0f;
+        to[(At::ls - At::ks) / 4] =            // no page: weight 0
+            !meta_ok ? kNegInf : num ? __builtin_amdgcn_logf(sv) : meta;
+        to[(At::rs - At::ks) / 4] = num ? 1.0f / sv : 1.0f;
       } else {
-        s.ks[lane] = meta * c0;
+        to[0] = meta_ok ? meta * c0 : 0.0f;
       }
     }
   };
@@ -698,101 +705,118 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[x][i] = 0.0f;
   float m = kNegInf, l = 0.0f;
+  // the chunks that a lane reads: of key r (its even and odd chunks, four by four), of channel r
+  int k_at[4], v_at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    k_at[i] = At::k + r * DT * 2 + ((2 * i + h) ^ (r & 7)) * 16;
+    v_at[i] = At::v + r * 128 + ((2 * i + h) ^ (2 * (r & 3)) ^ ((r >> 2) & 7)) * 16;
+  }
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
   if (steps > 0) {
     pages(j0);
     fetch(j0);
-    stage(lds[0]);
+    stage(Even{});
     pages(j0 + 64);
+    if (steps > 1) fetch(j0 + 64);
+    pages(j0 + 128);
   }
   __syncthreads();
-  for (int step = 0; step < steps; ++step) {
+  auto advance = [&](auto par, auto other, int step) {
+    constexpr int P = decltype(par)::value;
     const int j = j0 + 64 * step;
-    const ManyLds<DT>& b = lds[step & 1];
-    const bool more = step + 1 < steps;
-    if (more) {
-      fetch(j + 64);
-      pages(j + 128);
+    if (step + 1 < steps) stage(other);
+    if (step + 2 < steps) {
+      fetch(j + 128);
+      pages(j + 192);
     }
-    if (j <= pos1 && j + 63 >= see0) {                     // some row sees a key of the step
-      f32x16 s[2];
+    f32x16 s[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
-      // 16-bit queries: the two products take turns; fp32's are one after the other, they are
-      // longer and leave fewer registers
+      for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+    // the halves of the keys in turn; fp32's products one after the other: they are longer and
+    // leave fewer registers
 #pragma unroll
-      for (int i = 0; i < 2 * KS; ++i) {
-        const int u = NP == 1 ? i % 2 : i / KS, k = NP == 1 ? i / 2 : i % KS;
-        const f16x8 kf =
-            *reinterpret_cast<const f16x8*>(&b.k[32 * u + r][((2 * k + h) ^ (r & 7)) * 8]);
+    for (int i = 0; i < 2 * KS; ++i) {
+      const int u = NP == 1 ? i % 2 : i / KS, k = NP == 1 ? i / 2 : i % KS;
+      const f16x8 kf = *reinterpret_cast<const f16x8*>(smem + k_at[k % 4] + P * At::buffer +
+                                                       32 * u * DT * 2 + k / 4 * 128);
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s[u], 0, 0, 0);
+    }
+    if (scaled) {
+      asm volatile("");                                    // a branch, not selects
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i / 16][i % 16] *= row_mul;
+    }
+    const unsigned char* meta_at = smem + At::ks + P * 256 + 16 * h;
+    auto meta4 = [&](int which, int y) {                   // keys 8 y + 4 h ..
+      return *reinterpret_cast<const f32x4*>(meta_at + (which - At::ks) + 32 * y);
+    };
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const f32x4 ks = meta4(At::ks, y), ls = meta4(At::ls, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s[y / 4][y % 4 * 4 + i] = fmaf(s[y / 4][y % 4 * 4 + i], ks[i], ls[i]);
+    }
+    if (j + 63 > pos0) {
+      const int last = pos - j - 4 * h;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (8 * (i / 4) + i % 4 > last) s[i / 16][i % 16] = kNegInf;
+    }
+    if (j < see1) {
+      const int first = see - j - 4 * h;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (8 * (i / 4) + i % 4 < first) s[i / 16][i % 16] = kNegInf;
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) top = max3(top, s[i / 16][i % 16], s[i / 16][i % 16 + 1]);
+    top = reduce_x32(top, FMax{});
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
+      l *= f;
+#pragma unroll
+      for (int y = 0; y < CT; ++y)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[y][i] *= f;
+      m = top;
+    }
+    const float base = m == kNegInf ? 0.0f : m - kHead;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      float w[8];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const f32x4 rs = meta4(At::rs, 2 * v + y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[4 * y + i] = exp2_fast(s[v / 2][v % 2 * 8 + 4 * y + i] - base);
+          l = fmaf(w[4 * y + i], rs[i], l);
+        }
+      }
+      f16x8 p[NP];
+      split_f16<NP>(w, p);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const f16x8 vf = *reinterpret_cast<const f16x8*>(smem + v_at[v] + P * At::buffer +
+                                                         ct * 32 * 128);
 #pragma unroll
         for (int n = 0; n < NP; ++n)
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s[u], 0, 0, 0);
-      }
-      if (scaled) {
-        s[0] *= row_mul;
-        s[1] *= row_mul;
-      }
-      float x[32];
-#pragma unroll
-      for (int y = 0; y < 8; ++y) {
-        const f32x4 ks = *reinterpret_cast<const f32x4*>(&b.ks[8 * y + 4 * h]);
-        const f32x4 ls = *reinterpret_cast<const f32x4*>(&b.ls[8 * y + 4 * h]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * y + i] = fmaf(s[y / 4][y % 4 * 4 + i], ks[i], ls[i]);
-      }
-      if (j + 63 > pos0) {
-        const int last = pos - j - 4 * h;
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (8 * (i / 4) + i % 4 > last) x[i] = kNegInf;
-      }
-      if (j < see1) {
-        const int first = see - j - 4 * h;
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (8 * (i / 4) + i % 4 < first) x[i] = kNegInf;
-      }
-      float top = m;
-#pragma unroll
-      for (int i = 0; i < 32; i += 2) top = max3(top, x[i], x[i + 1]);
-      top = reduce_x32(top, FMax{});
-      if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-        const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
-        l *= f;
-#pragma unroll
-        for (int y = 0; y < CT; ++y) o[y] *= f;
-        m = top;
-      }
-      const float base = m == kNegInf ? 0.0f : m - kHead;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        float w[8];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const f32x4 rs = *reinterpret_cast<const f32x4*>(&b.rs[16 * s + 8 * y + 4 * h]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[4 * y + i] = exp2_fast(x[8 * s + 4 * y + i] - base);
-            l = fmaf(w[4 * y + i], rs[i], l);
-          }
-        }
-        f16x8 p[NP];
-        split_f16<NP>(w, p);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const int ch = 32 * ct + r;
-          const f16x8 vf =
-              *reinterpret_cast<const f16x8*>(&b.v[ch][value_chunk(ch, 2 * s + h) * 8]);
-#pragma unroll
-          for (int n = 0; n < NP; ++n)
-            o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);
-        }
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);
       }
     }
-    if (more) stage(lds[(step + 1) & 1]);
     __syncthreads();
+  };
+  for (int step = 0; step < steps; step += 2) {
+    advance(Even{}, Odd{}, step);
+    if (step + 1 < steps) advance(Odd{}, Even{}, step + 1);
   }
   l = reduce_x32(l, FAdd{});
   if (row >= rows_end) return;
