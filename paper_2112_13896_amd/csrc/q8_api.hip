@@ -110,7 +110,7 @@ void with_width(int d, F f) {
 }
 
 struct AttentionPlan {
-  bool many;           // attention_many, else attention_few
+  int per;             // rows of a workgroup: 128 (attention_many), 16 or 32 (attention_few)
   int64_t tiles;       // numbers of row tiles (find_tile)
   int splits, chunk;
 };
@@ -119,14 +119,13 @@ AttentionPlan attention_plan(const cs::CacheView& c, int tokens, int q_heads, in
                              int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
-  p.many = rows > 32 * (int64_t)batch;
-  const int per = p.many ? 128 : 16;
-  p.tiles = rows / per + batch + 1;
+  p.per = rows > 32 * (int64_t)batch ? 128 : rows > 16 * (int64_t)batch ? 32 : 16;
+  p.tiles = rows / p.per + batch + 1;
   int64_t len = (int64_t)table_width << c.page_log;
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
-  const int64_t items = (rows + per - 1) / per * c.heads;
-  int64_t splits = std::min<int64_t>({(p.many ? 512 : 1024) / items, (len + 127) / 128, cs::kMaxSplits});
+  const int64_t items = (rows + p.per - 1) / p.per * c.heads;
+  int64_t splits = std::min<int64_t>({(p.per == 128 ? 512 : 1024) / items, (len + 127) / 128, cs::kMaxSplits});
   if (splits < 1) splits = 1;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
@@ -322,14 +321,16 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
     using T = decltype(t);
     const dim3 grid((unsigned)blocks), block(256);
     auto few = [&](auto dt) {
-      hipLaunchKernelGGL((cs::attention_few<T, decltype(dt)::value>), grid, block, 0, s, a);
+      constexpr int DT = decltype(dt)::value;
+      if (p.per == 16) hipLaunchKernelGGL((cs::attention_few<T, DT, 1>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((cs::attention_few<T, DT, 2>), grid, block, 0, s, a);
     };
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
       hipLaunchKernelGGL((cs::attention_many<T, W>), grid, block, cs::ManyLds<DT>::bytes, s,
                          a);
     };
-    if (!p.many) with_width(c.d, few);
+    if (p.per < 128) with_width(c.d, few);
     else if (c.d > 64 && c.d <= 96) many(std::integral_constant<int, 96>{});
     else if (c.d > 128 && c.d <= 192) many(std::integral_constant<int, 192>{});
     else with_width(c.d, many);

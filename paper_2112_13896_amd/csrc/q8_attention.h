@@ -69,11 +69,12 @@ __device__ __forceinline__ void place(const PagedAttention& a, int* head, int* t
   *split = (int)s;
 }
 
-// A tile of `rows` rows of one sequence.  Sequence b's tiles have the numbers
-// from starts[b] * group / rows + b on, which leaves room for its last,
-// partial one: a tile number gives its sequence by a binary search, and the
-// few numbers without rows leave at once.  Tokens past the last sequence are
-// a sequence of length 0.
+// A tile of `per` rows of one sequence.  Sequence b's tiles have the numbers
+// from starts[b] * group / per + b on, which leaves room for its last, partial
+// one; the sequence of a tile is the number of sequences b >= 1 whose first
+// tile is not past it, counted 64 at a time (one load's latency, where a
+// binary search has one per level).  The few numbers without rows leave at
+// once.  Tokens past the last sequence are a sequence of length 0.
 struct RowTile {
   int b, token0, n;    // sequence, its first new token, its new tokens
   int row0, rows;      // first row of the tile in the sequence, the sequence's rows
@@ -81,23 +82,24 @@ struct RowTile {
 };
 
 __device__ __forceinline__ bool find_tile(const PagedAttention& a, int tile, int per, RowTile* t) {
-  auto base = [&](int b) {
-    const int s = b > a.batch ? a.tokens : a.starts[b];
-    return (int)((int64_t)s * a.group / per) + b;
-  };
-  int lo = 0, hi = a.batch;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (base(mid) <= tile) lo = mid;
-    else hi = mid - 1;
+  auto base = [&](int b, int start) { return (int)((int64_t)start * a.group / per) + b; };
+  const int lane = threadIdx.x % 64;
+  int b = 0;
+  for (int b0 = 1; b0 <= a.batch; b0 += 64) {
+    const int i = min(b0 + lane, a.batch);
+    const bool past = b0 + lane > a.batch || base(i, a.starts[i]) > tile;
+    const uint64_t later = __builtin_amdgcn_ballot_w64(past);
+    b += later ? __builtin_ctzll(later) : 64;
+    if (later) break;
   }
-  t->b = lo;
-  t->token0 = min(max(a.starts[lo], 0), a.tokens);
-  const int end = lo == a.batch ? a.tokens : min(max(a.starts[lo + 1], 0), a.tokens);
+  const int start = a.starts[b];
+  t->b = b;
+  t->token0 = min(max(start, 0), a.tokens);
+  const int end = b == a.batch ? a.tokens : min(max(a.starts[b + 1], 0), a.tokens);
   t->n = max(end - t->token0, 0);
   t->rows = t->n * a.group;
-  t->row0 = (tile - base(lo)) * per;
-  t->len = lo == a.batch ? 0 : min(max(a.lens[lo], 0), a.table_width << a.c.page_log);
+  t->row0 = (tile - base(b, start)) * per;
+  t->len = b == a.batch ? 0 : min(max(a.lens[b], 0), a.table_width << a.c.page_log);
   return t->row0 >= 0 && t->row0 < t->rows;
 }
 
@@ -229,54 +231,52 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 }
 
 // ---------------------------------------------------------------- few rows
-// attention_few: up to 16 rows of a cache head (a decoding token's query
+// attention_few: up to 16 RT rows of a cache head (a decoding token's query
 // heads, a few drafted tokens) to a workgroup of four wavefronts, the keys
 // read once.  A wavefront takes 32 keys a step, every fourth step of the
 // workgroup's part of the key axis: keys and values go from memory to
-// registers (no LDS), the next step's loads in flight under this one's
-// arithmetic.  Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles
-// of 16, channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels
-// r DT/16 .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
-template <int DT>
-struct FewStep {
-  u32x4 k[2][DT / 64];
-  uint32_t v[DT / 64][8];
-  f32x4 ks[2], vs[2];
-};
-
-template <typename T, int DT>
-__global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAttention a) {
+// registers (no LDS) and are turned to halves there.  What hides the loads is
+// other wavefronts: registers for a step in flight ahead would halve their
+// number.  Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of
+// 16, channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels
+// r DT/16 .. ; logits: keys 4h .. 4h+3 of both tiles for rows r, 16 + r.
+template <typename T, int DT, int RT>
+__global__ __launch_bounds__(256, DT * RT == 512 ? 1 : DT * RT == 256 ? 2 : sizeof(T) == 4 ? 3 : 4)
+void attention_few(PagedAttention a) {
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;
   constexpr int KS = DT / 32, CT = DT / 16;
   __shared__ float l_o[4][16][DT + 4];
-  __shared__ float l_m[4][16], l_l[4][16];
+  __shared__ float l_m[4][16 * RT], l_l[4][16 * RT];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, h = lane / 16, d = a.c.d;
   int head, tile, split;
   place(a, &head, &tile, &split);
   RowTile t;
-  if (!find_tile(a, tile, 16, &t)) return;
-  const int row = t.row0 + r, rows_end = min(t.rows, t.row0 + 16);
-  const int tok = (int)fdiv((uint32_t)min(row, t.rows - 1), a.by_group);
+  if (!find_tile(a, tile, 16 * RT, &t)) return;
+  const int rows_end = min(t.rows, t.row0 + 16 * RT);
   const int tok0 = (int)fdiv((uint32_t)t.row0, a.by_group);
   const int tok1 = (int)fdiv((uint32_t)(rows_end - 1), a.by_group);
-  const int qh = head * a.group + min(row, t.rows - 1) - tok * a.group;
+  const int back = t.len - t.n;                            // position of new token 0
   int lo, hi;
   tile_keys(a, t, tok0, tok1, &lo, &hi);
-  const int pos = t.len - t.n + tok;                       // the row sees [see, pos]
-  const int see = a.window > 0 ? pos - a.window + 1 : 0;
-  const int pos0 = t.len - t.n + tok0;                     // every row sees up to pos0 ...
-  const int see1 = a.window > 0 ? t.len - t.n + tok1 - a.window + 1 : 0;   // ... from see1 on
+  const int pos0 = back + tok0;                            // every row sees up to pos0 ...
+  const int see1 = a.window > 0 ? back + tok1 - a.window + 1 : 0;   // ... from see1 on
   // this workgroup's part
-  int j0 = lo / 32 * 32 + split * a.chunk;
+  const int j0 = lo / 32 * 32 + split * a.chunk;
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
   const int steps = hi > j0 ? (hi - j0 + 31) / 32 : 0;
 
   // the query rows' operand
-  f16x8 q[NP][KS];
-  float c;
-  {
-    const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
+  f16x8 q[RT][NP][KS];
+  float c[RT];
+  int pos[RT];                                             // row y sees up to pos[y]
+#pragma unroll
+  for (int y = 0; y < RT; ++y) {
+    const int row = min(t.row0 + 16 * y + r, t.rows - 1);
+    const int tok = (int)fdiv((uint32_t)row, a.by_group);
+    pos[y] = back + tok;
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq +
+                  (head * a.group + row - tok * a.group) * a.hsq;
     float f[KS][8];
     uint32_t top = 0;
 #pragma unroll
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
     top = max(s16[0], s16[1]);
     const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     const RowNorm nm = row_norm(__uint_as_float(max(s32[0], s32[1])), a.scale);
-    c = nm.c;
+    c[y] = nm.c;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
 #pragma unroll
@@ -303,183 +303,195 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void attention_few(PagedAtte
       f16x8 p[NP];
       split_f16<NP>(f[s], p);
 #pragma unroll
-      for (int n = 0; n < NP; ++n) q[n][s] = p[n];
+      for (int n = 0; n < NP; ++n) q[y][n][s] = p[n];
     }
   }
 
   const int32_t* table = a.table + (int64_t)t.b * a.table_width;
   const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
-  // rows (of codes) of the two tiles of 16 keys of a step; -1: no such page
-  auto rows_of = [&](int j, int64_t (&at)[2]) {
+  int page[2];                                             // of the two tiles of 16 keys
+  auto pages = [&](int j) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int k0 = min(j + 16 * u, hi - 1);
-      const int page = __builtin_amdgcn_readfirstlane(table[k0 >> lg]);
-      at[u] = (uint32_t)page < (uint32_t)n_pages
-                  ? (((int64_t)page * a.c.heads + head) << lg) + ((j + 16 * u) & in_page)
-                  : -1;
-    }
+    for (int u = 0; u < 2; ++u)
+      page[u] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * u, hi - 1) >> lg]);
   };
-  FewStep<DT> st;
-  int64_t at[2];
-  auto fetch = [&](FewStep<DT>& s, const int64_t (&at)[2]) {
+  f32x4 o[RT][CT];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int y = 0; y < RT; ++y) {
+    m[y] = kNegInf;
+    l[y] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < CT; ++x) o[y][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  if (wave < steps) pages(j0 + 32 * wave);
+  for (int step = wave; step < steps; step += 4) {
+    const int j = j0 + 32 * step;
+    u32x4 kr[2][DT / 64];
+    uint32_t vr[DT / 64][8];
+    f32x4 ks[2], vs[2];
+    bool ok[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int64_t row0 = at[u] < 0 ? 0 : at[u];          // any rows: hidden ones are masked
-      const int8_t* kp = a.c.k + (row0 + r) * d;
+      ok[u] = (uint32_t)page[u] < (uint32_t)n_pages;
+      // no page: any rows, which are masked
+      const int64_t row0 = (((int64_t)(ok[u] ? page[u] : 0) * a.c.heads + head) << lg) +
+                           ((j + 16 * u) & in_page);
+      const int8_t* kp = a.c.k + row0 * d;
 #pragma unroll
       for (int p = 0; p < DT / 64; ++p) {
         const int ch = h * (DT / 4) + 16 * p;              // channels past d meet zeros in q
-        s.k[u][p] = *reinterpret_cast<const u32x4*>(kp + (ch < d ? ch : 0));
+        kr[u][p] = *reinterpret_cast<const u32x4*>(kp + (uint32_t)(r * d + (ch < d ? ch : 0)));
       }
-      s.ks[u] = *reinterpret_cast<const f32x4*>(a.c.ks + row0 + 4 * h);
-      s.vs[u] = *reinterpret_cast<const f32x4*>(a.c.vs + row0 + 4 * h);
+      ks[u] = *reinterpret_cast<const f32x4*>(a.c.ks + row0 + 4 * h);
+      vs[u] = *reinterpret_cast<const f32x4*>(a.c.vs + row0 + 4 * h);
       const int ch = r * (DT / 16);                        // channels past d are not stored
-      const int8_t* vp = a.c.v + (row0 + 4 * h) * d + (ch < d ? ch : 0);
+      const int8_t* vp = a.c.v + row0 * d;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t w[DT / 64];
-        __builtin_memcpy(w, __builtin_assume_aligned(vp + (int64_t)i * d, DT / 16), DT / 16);
+        __builtin_memcpy(w,
+                         __builtin_assume_aligned(
+                             vp + i * d + (uint32_t)(4 * h * d + (ch < d ? ch : 0)), DT / 16),
+                         DT / 16);
 #pragma unroll
-        for (int x = 0; x < DT / 64; ++x) s.v[x][4 * u + i] = w[x];
+        for (int x = 0; x < DT / 64; ++x) vr[x][4 * u + i] = w[x];
       }
     }
-  };
-
-  f32x4 o[CT];
-#pragma unroll
-  for (int x = 0; x < CT; ++x) o[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = kNegInf, l = 0.0f;
-  int step = wave;
-  if (step < steps) {
-    rows_of(j0 + 32 * step, at);
-    fetch(st, at);
-  }
-#pragma unroll 2
-  for (; step < steps; step += 4) {
-    const int j = j0 + 32 * step;
-    const bool ok0 = at[0] >= 0, ok1 = at[1] >= 0;
-    FewStep<DT> nx;
-    if (step + 4 < steps) {
-      rows_of(j + 128, at);
-      fetch(nx, at);
-    }
-    // logits in log2 units, plus E
-    float x[8], av[8], rv[8];
+    if (step + 4 < steps) pages(j + 128);
+    f32x4 s[RT][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int y = 0; y < RT; ++y) s[y][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const f16x8 kf = codes_f16(st.k[u][k / 2][k % 2 * 2], st.k[u][k / 2][k % 2 * 2 + 1]);
+        const f16x8 kf = codes_f16(kr[u][k / 2][k % 2 * 2], kr[u][k / 2][k % 2 * 2 + 1]);
 #pragma unroll
-        for (int n = 0; n < NP; ++n)
-          s = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][k], s, 0, 0, 0);
-      }
+        for (int y = 0; y < RT; ++y)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const ValueScale sv = value_scale(st.vs[u][i]);
-        av[4 * u + i] = sv.a;
-        rv[4 * u + i] = sv.r;
-        x[4 * u + i] = fmaf(s[i] * st.ks[u][i], c, sv.e);
+          for (int n = 0; n < NP; ++n)
+            s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[y][n][k], s[y][u], 0, 0, 0);
       }
     }
-    // hidden keys: past the row's position (the last part's end), before its window, no page
-    if (j + 31 > pos0 || j < see1 || !ok0 || !ok1) {
+    ValueScale sv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sv[i] = value_scale(vs[i / 4][i % 4]);
+    f16x8 p[RT][NP];
+#pragma unroll
+    for (int y = 0; y < RT; ++y) {
+      // logits in log2 units, plus E
+      float x[8], av[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int key = j + 16 * (i / 4) + 4 * h + i % 4;
-        if (key > pos || key < see || !(i < 4 ? ok0 : ok1)) {
-          x[i] = kNegInf;
-          av[i] = 0.0f;
+        av[i] = sv[i].a;
+        x[i] = fmaf(s[y][i / 4][i % 4] * ks[i / 4][i % 4], c[y], sv[i].e);
+      }
+      // hidden keys: past the row's position (the last part's end), before its window, no page
+      if (j + 31 > pos0 || j < see1 || !ok[0] || !ok[1]) {
+        const int see = a.window > 0 ? pos[y] - a.window + 1 : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = j + 16 * (i / 4) + 4 * h + i % 4;
+          if (key > pos[y] || key < see || !ok[i / 4]) {
+            x[i] = kNegInf;
+            av[i] = 0.0f;
+          }
         }
       }
-    }
-    float top = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(m, x[6], x[7]));
-    top = reduce_x16_x32(top, FMax{});
-    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-      const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
-      l *= f;
+      float top = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(m[y], x[6], x[7]));
+      top = reduce_x16_x32(top, FMax{});
+      if (__builtin_amdgcn_ballot_w64(top > m[y] + kSlack)) {
+        const float f = top == kNegInf ? 1.0f : exp2_fast(m[y] - top);
+        l[y] *= f;
 #pragma unroll
-      for (int y = 0; y < CT; ++y) o[y] *= f;
-      m = top;
-    }
-    const float base = m == kNegInf ? 0.0f : m - kHead;
-    float w[8];
+        for (int z = 0; z < CT; ++z) o[y][z] *= f;
+        m[y] = top;
+      }
+      const float base = m[y] == kNegInf ? 0.0f : m[y] - kHead;
+      float w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float e = exp2_fast(x[i] - base);
-      l = fmaf(e, rv[i], l);
-      w[i] = e * av[i];
+      for (int i = 0; i < 8; ++i) {
+        const float e = exp2_fast(x[i] - base);
+        l[y] = fmaf(e, sv[i].r, l[y]);
+        w[i] = e * av[i];
+      }
+      split_f16<NP>(w, p[y]);
     }
-    f16x8 p[NP];
-    split_f16<NP>(w, p);
     auto values = [&](auto cc, int xw) {
       constexpr int C = decltype(cc)::value;
-      const f16x8 vf = codes_f16_across<C>(st.v[xw]);
+      const f16x8 vf = codes_f16_across<C>(vr[xw]);
 #pragma unroll
-      for (int n = 0; n < NP; ++n)
-        o[4 * xw + C] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[n], o[4 * xw + C], 0, 0, 0);
+      for (int y = 0; y < RT; ++y)
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+          o[y][4 * xw + C] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[y][n], o[y][4 * xw + C], 0, 0, 0);
     };
 #pragma unroll
     for (int xw = 0; xw < DT / 64; ++xw) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) st.v[xw][i] ^= kFlip;
+      for (int i = 0; i < 8; ++i) vr[xw][i] ^= kFlip;
       values(std::integral_constant<int, 0>{}, xw);
       values(std::integral_constant<int, 1>{}, xw);
       values(std::integral_constant<int, 2>{}, xw);
       values(std::integral_constant<int, 3>{}, xw);
     }
-    st = nx;
   }
-  l = reduce_x16_x32(l, FAdd{});
 
-  // the four wavefronts' sums, joined in order
-  if (h == 0) {
-    l_m[wave][r] = m;
-    l_l[wave][r] = l;
-  }
+  // the four wavefronts' sums, joined in order, 16 rows at a time
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int x = 0; x < CT; x += 4)
-      *reinterpret_cast<f32x4*>(&l_o[wave][r][(4 * h + i) * CT + x]) =
-          f32x4{o[x][i], o[x + 1][i], o[x + 2][i], o[x + 3][i]};
-  __syncthreads();
-  // 16 lanes to a row
-  const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16;
-  if (t.row0 + rr >= rows_end) return;
-  float top = kNegInf;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, l_m[w][rr]);
-  const float base = top == kNegInf ? 0.0f : top;
-  float f[4], sum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    f[w] = exp2_fast(l_m[w][rr] - base);
-    // a wavefront without a key has l = 0; one with a NaN among its keys alone has m = -inf
-    sum += l_l[w][rr] == 0.0f ? 0.0f : l_l[w][rr] * f[w];
-  }
-  const int orow = t.row0 + rr;
-  const int otok = (int)fdiv((uint32_t)orow, a.by_group);
-  const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
-                     otok * a.group;
-  if (a.splits > 1 && x0 == 0) a.part_ml[(int64_t)split * a.tokens * a.q_heads + ro] =
-      float2{top, sum};
-  const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
-  for (int x = 8 * x0; x < d; x += 128) {
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
-      y[i] = a.splits > 1 ? s : s * inv;
+  for (int y = 0; y < RT; ++y) {
+    l[y] = reduce_x16_x32(l[y], FAdd{});
+    if (h == 0) {
+      l_m[wave][16 * y + r] = m[y];
+      l_l[wave][16 * y + r] = l[y];
     }
-    if (a.splits > 1)
-      store8(a.part_o + ((int64_t)split * a.tokens * a.q_heads + ro) * d + x, y);
-    else
-      store8(static_cast<T*>(a.out) + ro * d + x, y);
+  }
+#pragma unroll
+  for (int y = 0; y < RT; ++y) {
+    if (y > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < CT; x += 4)
+        *reinterpret_cast<f32x4*>(&l_o[wave][r][(4 * h + i) * CT + x]) =
+            f32x4{o[y][x][i], o[y][x + 1][i], o[y][x + 2][i], o[y][x + 3][i]};
+    __syncthreads();
+    // 16 lanes to a row
+    const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16, lr = 16 * y + rr;
+    if (t.row0 + lr < rows_end) {
+      float top = kNegInf;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, l_m[w][lr]);
+      const float base = top == kNegInf ? 0.0f : top;
+      float f[4], sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        // a wavefront without a key has sums of 0; one with NaN alone among its keys m = -inf
+        f[w] = exp2_fast(l_m[w][lr] - base);
+        sum = fmaf(l_l[w][lr], f[w], sum);
+      }
+      const int orow = t.row0 + lr;
+      const int otok = (int)fdiv((uint32_t)orow, a.by_group);
+      const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
+                         otok * a.group;
+      const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
+      if (a.splits > 1 && x0 == 0) a.part_ml[po] = float2{top, sum};
+      const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
+      for (int x = 8 * x0; x < d; x += 128) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float s = 0.0f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
+          v[i] = a.splits > 1 ? s : s * inv;
+        }
+        if (a.splits > 1) store8(a.part_o + po * d + x, v);
+        else store8(static_cast<T*>(a.out) + ro * d + x, v);
+      }
+    }
   }
 }
 
