@@ -110,23 +110,33 @@ void with_width(int d, F f) {
 }
 
 struct AttentionPlan {
-  int per;             // rows of a workgroup: 128 (attention_many), 16 or 32 (attention_few)
+  int per;             // rows of a workgroup: 128 (attention_many) or 16 (attention_few)
   int64_t tiles;       // numbers of row tiles (find_tile)
   int splits, chunk;
 };
 
-AttentionPlan attention_plan(const cs::CacheView& c, int tokens, int q_heads, int batch,
-                             int table_width, int max_len, int window) {
+AttentionPlan attention_plan(const cs::CacheView& c, cs_dtype qt, int tokens, int q_heads,
+                             int batch, int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
-  p.per = rows > 32 * (int64_t)batch ? 128 : rows > 16 * (int64_t)batch ? 32 : 16;
+  // 128 rows a workgroup from 65 rows a sequence on (bf16, d 128, eight heads; few | many):
+  // 64 rows 32 | 50 us (1 x 32,768 keys), 71 | 65 (8 x 8,192), 54 | 76 (32 x 2,048), 14 | 17
+  // (32 x 200); 96 rows 48 | 53, 115 | 70, 82 | 95, 20 | 20; 128 rows 49 | 40, 119 | 76
+  p.per = rows > 64 * (int64_t)batch ? 128 : 16;
   p.tiles = rows / p.per + batch + 1;
   int64_t len = (int64_t)table_width << c.page_log;
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
-  const int64_t items = (rows + p.per - 1) / p.per * c.heads;
-  int64_t splits = std::min<int64_t>({(p.per == 128 ? 512 : 1024) / items, (len + 127) / 128, cs::kMaxSplits});
-  if (splits < 1) splits = 1;
+  // As many parts as fill the card: few rows twice, at four workgroups a compute unit (three and
+  // two where fp32 queries and wide heads take more registers), so that sequences of unequal
+  // length even out (64 sequences of up to 8,192 keys: 151 us filled once, 141 twice or four
+  // times); many rows, whose parts cost more to join, once at one.  Keys that four wavefronts
+  // pass in ten microseconds or so stay whole.
+  const int64_t per_seq = (rows + batch - 1) / batch;
+  const int64_t items = batch * ((per_seq + p.per - 1) / p.per) * c.heads;
+  const int wgs = p.per == 128 ? 1 : 2 * (c.d > 128 ? 2 : c.d > 64 && qt == CS_F32 ? 3 : 4);
+  int64_t splits = std::min<int64_t>({256 * wgs / items, len / 256, cs::kMaxSplits});
+  if (splits < 1 || len <= 1024) splits = 1;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
   return p;
@@ -275,7 +285,7 @@ size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt,
   if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0) return 0;
   if (q_heads % c.heads != 0) return 0;
   // the split without a window is the finest: it serves any window
-  const AttentionPlan p = attention_plan(c, tokens, q_heads, batch, table_width, max_len, 0);
+  const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len, 0);
   return attention_part_bytes(p, (int64_t)tokens * q_heads, c.d);
 }
 
@@ -301,7 +311,8 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
   const size_t need = cs_paged_attention_workspace_bytes(cache, qt, tokens, q_heads, batch,
                                                          table_width, max_len);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
-  const AttentionPlan p = attention_plan(c, tokens, q_heads, batch, table_width, max_len, window);
+  const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len,
+                                          window);
   const int group = q_heads / c.heads;
   const int64_t rows = (int64_t)tokens * q_heads;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -322,21 +333,20 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
     const dim3 grid((unsigned)blocks), block(256);
     auto few = [&](auto dt) {
       constexpr int DT = decltype(dt)::value;
-      if (p.per == 16) hipLaunchKernelGGL((cs::attention_few<T, DT, 1>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((cs::attention_few<T, DT, 2>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((cs::attention_few<T, DT>), grid, block, 0, s, a);
     };
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
       hipLaunchKernelGGL((cs::attention_many<T, W>), grid, block, cs::ManyLds<DT>::bytes, s,
                          a);
     };
-    if (p.per < 128) with_width(c.d, few);
+    if (p.per == 16) with_width(c.d, few);
     else if (c.d > 64 && c.d <= 96) many(std::integral_constant<int, 96>{});
     else if (c.d > 128 && c.d <= 192) many(std::integral_constant<int, 192>{});
     else with_width(c.d, many);
     int r = launched();
     if (r == CS_OK && p.splits > 1) {
-      hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, a);
+      hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)rows), block, 0, s, a);
       r = launched();
     }
     return r;

@@ -231,29 +231,31 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 }
 
 // ---------------------------------------------------------------- few rows
-// attention_few: up to 16 RT rows of a cache head (a decoding token's query
+// attention_few: up to 16 rows of a cache head (a decoding token's query
 // heads, a few drafted tokens) to a workgroup of four wavefronts, the keys
 // read once.  A wavefront takes 32 keys a step, every fourth step of the
 // workgroup's part of the key axis: keys and values go from memory to
 // registers (no LDS) and are turned to halves there.  What hides the loads is
-// other wavefronts: registers for a step in flight ahead would halve their
-// number.  Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of
+// other wavefronts: registers for a step in flight ahead, or for a second
+// tile of rows, would halve their number (two long sequences of 20 rows a
+// head: 70 us with two tiles that both read the keys, the second out of the
+// L2, 88 us with one of 32 rows).  Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of
 // 16, channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels
-// r DT/16 .. ; logits: keys 4h .. 4h+3 of both tiles for rows r, 16 + r.
-template <typename T, int DT, int RT>
-__global__ __launch_bounds__(256, DT * RT == 512 ? 1 : DT * RT == 256 ? 2 : sizeof(T) == 4 ? 3 : 4)
+// r DT/16 .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
+template <typename T, int DT>
+__global__ __launch_bounds__(256, DT == 256 ? 2 : DT == 128 && sizeof(T) == 4 ? 3 : 4)
 void attention_few(PagedAttention a) {
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;
   constexpr int KS = DT / 32, CT = DT / 16;
   __shared__ float l_o[4][16][DT + 4];
-  __shared__ float l_m[4][16 * RT], l_l[4][16 * RT];
+  __shared__ float l_m[4][16], l_l[4][16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, h = lane / 16, d = a.c.d;
   int head, tile, split;
   place(a, &head, &tile, &split);
   RowTile t;
-  if (!find_tile(a, tile, 16 * RT, &t)) return;
-  const int rows_end = min(t.rows, t.row0 + 16 * RT);
+  if (!find_tile(a, tile, 16, &t)) return;
+  const int rows_end = min(t.rows, t.row0 + 16);
   const int tok0 = (int)fdiv((uint32_t)t.row0, a.by_group);
   const int tok1 = (int)fdiv((uint32_t)(rows_end - 1), a.by_group);
   const int back = t.len - t.n;                            // position of new token 0
@@ -267,14 +269,12 @@ void attention_few(PagedAttention a) {
   const int steps = hi > j0 ? (hi - j0 + 31) / 32 : 0;
 
   // the query rows' operand
-  f16x8 q[RT][NP][KS];
-  float c[RT];
-  int pos[RT];                                             // row y sees up to pos[y]
-#pragma unroll
-  for (int y = 0; y < RT; ++y) {
-    const int row = min(t.row0 + 16 * y + r, t.rows - 1);
-    const int tok = (int)fdiv((uint32_t)row, a.by_group);
-    pos[y] = back + tok;
+  const int row = min(t.row0 + r, t.rows - 1);
+  const int tok = (int)fdiv((uint32_t)row, a.by_group);
+  const int pos = back + tok;                              // the row sees up to pos
+  f16x8 q[NP][KS];
+  float c;
+  {
     const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq +
                   (head * a.group + row - tok * a.group) * a.hsq;
     float f[KS][8];
@@ -294,7 +294,7 @@ void attention_few(PagedAttention a) {
     top = max(s16[0], s16[1]);
     const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     const RowNorm nm = row_norm(__uint_as_float(max(s32[0], s32[1])), a.scale);
-    c[y] = nm.c;
+    c = nm.c;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
 #pragma unroll
@@ -303,7 +303,7 @@ void attention_few(PagedAttention a) {
       f16x8 p[NP];
       split_f16<NP>(f[s], p);
 #pragma unroll
-      for (int n = 0; n < NP; ++n) q[y][n][s] = p[n];
+      for (int n = 0; n < NP; ++n) q[n][s] = p[n];
     }
   }
 
@@ -315,15 +315,10 @@ void attention_few(PagedAttention a) {
     for (int u = 0; u < 2; ++u)
       page[u] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * u, hi - 1) >> lg]);
   };
-  f32x4 o[RT][CT];
-  float m[RT], l[RT];
+  f32x4 o[CT];
 #pragma unroll
-  for (int y = 0; y < RT; ++y) {
-    m[y] = kNegInf;
-    l[y] = 0.0f;
-#pragma unroll
-    for (int x = 0; x < CT; ++x) o[y][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  for (int x = 0; x < CT; ++x) o[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = kNegInf, l = 0.0f;
   if (wave < steps) pages(j0 + 32 * wave);
   for (int step = wave; step < steps; step += 4) {
     const int j = j0 + 32 * step;
@@ -359,74 +354,64 @@ void attention_few(PagedAttention a) {
       }
     }
     if (step + 4 < steps) pages(j + 128);
-    f32x4 s[RT][2];
+    f32x4 s[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int y = 0; y < RT; ++y) s[y][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      s[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const f16x8 kf = codes_f16(kr[u][k / 2][k % 2 * 2], kr[u][k / 2][k % 2 * 2 + 1]);
 #pragma unroll
-        for (int y = 0; y < RT; ++y)
-#pragma unroll
-          for (int n = 0; n < NP; ++n)
-            s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[y][n][k], s[y][u], 0, 0, 0);
+        for (int n = 0; n < NP; ++n)
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][k], s[u], 0, 0, 0);
       }
     }
-    ValueScale sv[8];
+    // logits in log2 units, plus E
+    float x[8], av[8], rv[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sv[i] = value_scale(vs[i / 4][i % 4]);
-    f16x8 p[RT][NP];
-#pragma unroll
-    for (int y = 0; y < RT; ++y) {
-      // logits in log2 units, plus E
-      float x[8], av[8];
+    for (int i = 0; i < 8; ++i) {
+      const ValueScale sv = value_scale(vs[i / 4][i % 4]);
+      av[i] = sv.a;
+      rv[i] = sv.r;
+      x[i] = fmaf(s[i / 4][i % 4] * ks[i / 4][i % 4], c, sv.e);
+    }
+    // hidden keys: past the row's position (the last part's end), before its window, no page
+    if (j + 31 > pos0 || j < see1 || !ok[0] || !ok[1]) {
+      const int see = a.window > 0 ? pos - a.window + 1 : 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        av[i] = sv[i].a;
-        x[i] = fmaf(s[y][i / 4][i % 4] * ks[i / 4][i % 4], c[y], sv[i].e);
-      }
-      // hidden keys: past the row's position (the last part's end), before its window, no page
-      if (j + 31 > pos0 || j < see1 || !ok[0] || !ok[1]) {
-        const int see = a.window > 0 ? pos[y] - a.window + 1 : 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = j + 16 * (i / 4) + 4 * h + i % 4;
-          if (key > pos[y] || key < see || !ok[i / 4]) {
-            x[i] = kNegInf;
-            av[i] = 0.0f;
-          }
+        const int key = j + 16 * (i / 4) + 4 * h + i % 4;
+        if (key > pos || key < see || !ok[i / 4]) {
+          x[i] = kNegInf;
+          av[i] = 0.0f;
         }
       }
-      float top = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(m[y], x[6], x[7]));
-      top = reduce_x16_x32(top, FMax{});
-      if (__builtin_amdgcn_ballot_w64(top > m[y] + kSlack)) {
-        const float f = top == kNegInf ? 1.0f : exp2_fast(m[y] - top);
-        l[y] *= f;
-#pragma unroll
-        for (int z = 0; z < CT; ++z) o[y][z] *= f;
-        m[y] = top;
-      }
-      const float base = m[y] == kNegInf ? 0.0f : m[y] - kHead;
-      float w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float e = exp2_fast(x[i] - base);
-        l[y] = fmaf(e, sv[i].r, l[y]);
-        w[i] = e * av[i];
-      }
-      split_f16<NP>(w, p[y]);
     }
+    float top = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(m, x[6], x[7]));
+    top = reduce_x16_x32(top, FMax{});
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
+      l *= f;
+#pragma unroll
+      for (int z = 0; z < CT; ++z) o[z] *= f;
+      m = top;
+    }
+    const float base = m == kNegInf ? 0.0f : m - kHead;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float e = exp2_fast(x[i] - base);
+      l = fmaf(e, rv[i], l);
+      w[i] = e * av[i];
+    }
+    f16x8 p[NP];
+    split_f16<NP>(w, p);
     auto values = [&](auto cc, int xw) {
       constexpr int C = decltype(cc)::value;
       const f16x8 vf = codes_f16_across<C>(vr[xw]);
 #pragma unroll
-      for (int y = 0; y < RT; ++y)
-#pragma unroll
-        for (int n = 0; n < NP; ++n)
-          o[y][4 * xw + C] =
-              __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[y][n], o[y][4 * xw + C], 0, 0, 0);
+      for (int n = 0; n < NP; ++n)
+        o[4 * xw + C] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[n], o[4 * xw + C], 0, 0, 0);
     };
 #pragma unroll
     for (int xw = 0; xw < DT / 64; ++xw) {
@@ -439,59 +424,51 @@ void attention_few(PagedAttention a) {
     }
   }
 
-  // the four wavefronts' sums, joined in order, 16 rows at a time
-#pragma unroll
-  for (int y = 0; y < RT; ++y) {
-    l[y] = reduce_x16_x32(l[y], FAdd{});
-    if (h == 0) {
-      l_m[wave][16 * y + r] = m[y];
-      l_l[wave][16 * y + r] = l[y];
-    }
+  // the four wavefronts' sums, joined in order
+  l = reduce_x16_x32(l, FAdd{});
+  if (h == 0) {
+    l_m[wave][r] = m;
+    l_l[wave][r] = l;
   }
 #pragma unroll
-  for (int y = 0; y < RT; ++y) {
-    if (y > 0) __syncthreads();
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int x = 0; x < CT; x += 4)
+      *reinterpret_cast<f32x4*>(&l_o[wave][r][(4 * h + i) * CT + x]) =
+          f32x4{o[x][i], o[x + 1][i], o[x + 2][i], o[x + 3][i]};
+  __syncthreads();
+  // 16 lanes to a row
+  const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16;
+  if (t.row0 + rr >= rows_end) return;
+  float top = kNegInf;
 #pragma unroll
-      for (int x = 0; x < CT; x += 4)
-        *reinterpret_cast<f32x4*>(&l_o[wave][r][(4 * h + i) * CT + x]) =
-            f32x4{o[y][x][i], o[y][x + 1][i], o[y][x + 2][i], o[y][x + 3][i]};
-    __syncthreads();
-    // 16 lanes to a row
-    const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16, lr = 16 * y + rr;
-    if (t.row0 + lr < rows_end) {
-      float top = kNegInf;
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, l_m[w][rr]);
+  const float base = top == kNegInf ? 0.0f : top;
+  float f[4], sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) top = fmaxf(top, l_m[w][lr]);
-      const float base = top == kNegInf ? 0.0f : top;
-      float f[4], sum = 0.0f;
+  for (int w = 0; w < 4; ++w) {
+    // a wavefront without a key has sums of 0; one with NaN alone among its keys m = -inf
+    f[w] = exp2_fast(l_m[w][rr] - base);
+    sum = fmaf(l_l[w][rr], f[w], sum);
+  }
+  const int orow = t.row0 + rr;
+  const int otok = (int)fdiv((uint32_t)orow, a.by_group);
+  const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
+                     otok * a.group;
+  const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
+  if (a.splits > 1 && x0 == 0) a.part_ml[po] = float2{top, sum};
+  const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
+  for (int x = 8 * x0; x < d; x += 128) {
+    float v[8];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        // a wavefront without a key has sums of 0; one with NaN alone among its keys m = -inf
-        f[w] = exp2_fast(l_m[w][lr] - base);
-        sum = fmaf(l_l[w][lr], f[w], sum);
-      }
-      const int orow = t.row0 + lr;
-      const int otok = (int)fdiv((uint32_t)orow, a.by_group);
-      const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
-                         otok * a.group;
-      const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
-      if (a.splits > 1 && x0 == 0) a.part_ml[po] = float2{top, sum};
-      const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
-      for (int x = 8 * x0; x < d; x += 128) {
-        float v[8];
+    for (int i = 0; i < 8; ++i) {
+      float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float s = 0.0f;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
-          v[i] = a.splits > 1 ? s : s * inv;
-        }
-        if (a.splits > 1) store8(a.part_o + po * d + x, v);
-        else store8(static_cast<T*>(a.out) + ro * d + x, v);
-      }
+      for (int w = 0; w < 4; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
+      v[i] = a.splits > 1 ? s : s * inv;
     }
+    if (a.splits > 1) store8(a.part_o + po * d + x, v);
+    else store8(static_cast<T*>(a.out) + ro * d + x, v);
   }
 }
 
@@ -568,17 +545,20 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   float row_mul = 1.0f;
   {
     const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
-    uint32_t top = 0;
-    float f[8];
+    float f[KS][8];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int ch = 16 * s + 8 * h;
-      if (ch < d) {
-        load_q8(qp + ch, a.q_vec, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
-      }
+      load_q8(qp + (ch < d ? ch : 0), a.q_vec, f[s]);      // all loads before the first use
     }
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (16 * s + 8 * h >= d) f[s][e] = 0.0f;
+        top = max(top, abs_bits(f[s][e]));
+      }
     const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     const float big = __uint_as_float(max(s32[0], s32[1]));
     const bool bad = !(big < __builtin_inff());
@@ -588,13 +568,11 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     row_mul = ldexpf(1.0f, -shift);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const int ch = 16 * s + 8 * h;
-      if (ch < d) load_q8(qp + ch, a.q_vec, f);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        f[e] = bad ? __uint_as_float(0x7FC00000u) : ch < d ? ldexpf(f[e], shift) : 0.0f;
+        f[s][e] = bad ? __uint_as_float(0x7FC00000u) : ldexpf(f[s][e], shift);
       f16x8 p[NP];
-      split_f16<NP>(f, p);
+      split_f16<NP>(f[s], p);
 #pragma unroll
       for (int n = 0; n < NP; ++n) q[n][s] = p[n];
     }
@@ -856,39 +834,46 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     }
 }
 
-// attention_join: the parts of a row, in order, a wavefront to a row.  Lane s
-// holds part s's weight, so the parts' loads wait for nothing but each other's
-// turn.
+// attention_join: the parts of a row, in a fixed order, a workgroup to a row.
+// Lane s of each wavefront has part s's weight; a wavefront adds up every
+// fourth part, so their loads wait for nothing but each other's turn, and the
+// four sums meet in LDS.
 constexpr int kMaxSplits = 64;
 
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
+  __shared__ f32x4 l_y[4][64];
   const int lane = threadIdx.x % 64, d = a.c.d;
-  const int64_t rows = (int64_t)a.tokens * a.q_heads;
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (row >= rows) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t rows = (int64_t)a.tokens * a.q_heads, row = blockIdx.x;
   float2 ml = float2{kNegInf, 0.0f};
   if (lane < a.splits) ml = a.part_ml[lane * rows + row];
   float top = ml.x;
   for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
   const float base = top == kNegInf ? 0.0f : top;
   const float f = exp2_fast(ml.x - base);                  // a part without a key: 0
-  float sum = ml.y * f;
-  for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
   const int ch = 4 * lane < d ? 4 * lane : 0;
   const float* po = a.part_o + row * d + ch;
   f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
+  for (int s0 = wave; s0 < a.splits; s0 += 32)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int s = s0 + 4 * i;
+      if (s < a.splits)
+        y += *reinterpret_cast<const f32x4*>(po + s * rows * d) *
+             __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+    }
+  l_y[wave][lane] = y;
+  __syncthreads();
+  if (wave > 0 || 4 * lane >= d) return;
+  y = l_y[0][lane] + l_y[1][lane] + l_y[2][lane] + l_y[3][lane];
+  float sum = 0.0f;
   for (int s = 0; s < a.splits; ++s)
-    y += *reinterpret_cast<const f32x4*>(po + s * rows * d) *
-         __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
-  const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
-  if (4 * lane < d) {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    y *= inv;
-    *reinterpret_cast<t4*>(static_cast<T*>(a.out) + row * d + ch) =
-        t4{(T)y[0], (T)y[1], (T)y[2], (T)y[3]};
-  }
+    sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ml.y * f), s));
+  y *= sum == 0.0f ? 0.0f : kCodeScale / sum;
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<t4*>(static_cast<T*>(a.out) + row * d + ch) =
+      t4{(T)y[0], (T)y[1], (T)y[2], (T)y[3]};
 }
 
 }  // namespace cs

@@ -157,22 +157,39 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[m][n][i] = 0;
+  // The next 32 codes' operands are read under this 32's products, one read to a product: left
+  // to itself the compiler reads all of them just before their use.
   auto multiply = [&](const int8_t* lx, const int8_t* lw) {
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    i32x4 fx[2][MT], fw[2][NT];
+    auto read = [&](int s) {
       const int at = fr * 128 + ((2 * s + fh) ^ (fr & 7)) * 16;
-      i32x4 fx[MT], fw[NT];
 #pragma unroll
       for (int m = 0; m < MT; ++m)
-        fx[m] = *reinterpret_cast<const i32x4*>(lx + (mr + 32 * m) * 128 + at);
+        fx[s & 1][m] = *reinterpret_cast<const i32x4*>(lx + (mr + 32 * m) * 128 + at);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        fw[n] = *reinterpret_cast<const i32x4*>(lw + (nr + 32 * n) * 128 + at);
+        fw[s & 1][n] = *reinterpret_cast<const i32x4*>(lw + (nr + 32 * n) * 128 + at);
+    };
+    read(0);
+    __builtin_amdgcn_sched_group_barrier(0x100, MT + NT, 0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) read(s + 1);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fx[m], fw[n], acc[m][n], 0, 0, 0);
+          acc[m][n] =
+              __builtin_amdgcn_mfma_i32_32x32x32_i8(fx[s & 1][m], fw[s & 1][n], acc[m][n], 0, 0, 0);
+      if (s < 3) {
+#pragma unroll
+        for (int i = 0; i < MT * NT; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (i < MT + NT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+      } else {
+        __builtin_amdgcn_sched_group_barrier(0x008, MT * NT, 0);
+      }
     }
   };
   const int whole = a.k / 128;
