@@ -476,8 +476,8 @@ void attention_few(PagedAttention a) {
 // attention_many: 128 rows of a cache head to a workgroup of four wavefronts,
 // 32 rows each, 64 keys a step.  A step's codes are turned to halves once for
 // all four: keys [64][DT], values transposed [DT][64], both in 16-byte chunks
-// whose place in a row is permuted (xor) so that eight lanes that read or
-// write one column of chunks meet all banks; two buffers, the next step's
+// whose place in a row is permuted (xor) so that the lanes that read a column
+// of chunks together meet all banks; two buffers, the next step's
 // codes are turned at the start of a step, beside its first products, and the
 // ones after that are then on their way in registers under all of its
 // arithmetic; one barrier a step.  Two wavefronts bring the values, two the
@@ -490,8 +490,8 @@ void attention_few(PagedAttention a) {
 // Here a = 1, E = log2(sv), taken once a step.
 //
 // Where a chunk lies: key k's chunk i (channels 8 i ..) at byte (k DT 2) +
-// 16 (i ^ (k & 7)), channel c's chunk g of values at byte 128 c +
-// 16 (g ^ 2 (c & 3) ^ ((c >> 2) & 7)).
+// 16 (i ^ key_turn(k)), channel c's chunk g of values at byte 128 c +
+// 16 (g ^ chunk_turn(c)).
 template <int DT>
 struct ManyLds {                                           // bytes
   static constexpr int k = 0;                              // [2][64][DT] halves
@@ -584,16 +584,17 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
   const bool brings_values = wave < 2;
   const int half = wave % 2;
-  constexpr int KB = DT / 64;                              // key loads a block, 16 bytes a lane
+  auto key_turn = [](int key) { return DT == 64 ? chunk_turn(key) : key & 15; };
+  constexpr int KB = DT / 64;                              // keys: loads a block, 16 bytes a lane
   constexpr int PR = DT / 16;                              // lanes to a key
   const int k_key = lane / PR, k_ch = lane % PR * 16;      // + 64 / PR keys a load
-  constexpr int VD = DT == 256 ? 2 : 1;                    // dwords a lane and value row
-  constexpr int VR = DT / (4 * VD);                        // lanes to a value
-  const int v_g = lane / VR, v_ch = lane % VR * 4 * VD;    // (DT 64: lanes from 32 on have none)
+  // values: 32 lanes to a block, 16 to each half of its keys (chunk of LDS), DT / 16 channels a lane
+  constexpr int VD = DT / 64;                              // dwords a lane and value row
+  const int v_ch = lane % 16 * 4 * VD;
   // byte of a block that this lane loads first (channels past d: any)
-  const uint32_t off = brings_values ? 4 * (v_g & 1) * d + (v_ch < d ? v_ch : 0)
+  const uint32_t off = brings_values ? 4 * (lane / 16 % 2) * d + (v_ch < d ? v_ch : 0)
                                      : k_key * d + (k_ch < d ? k_ch : 0);
-  uint32_t reg[2][8 * VD];                                 // [block]: keys 4 KB dwords, values 8 VD
+  uint32_t reg[8 * VD];                                    // both blocks' keys; one's values
   float meta = 0.0f;
   bool meta_ok = false;
   int page[4];
@@ -608,27 +609,25 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
            ((j + 16 * b) & in_page);
   };
   auto fetch = [&](int j) {
+    const int64_t at0 = block_row(half ? page[2] : page[0], j, 2 * half) * d;
+    const int64_t at1 = block_row(half ? page[3] : page[1], j, 2 * half + 1) * d;
+    if (brings_values) {
+      const int8_t* vp = a.c.v + (lane < 32 ? at0 : at1) + off;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int b = 2 * half + x;
-      const int64_t at = block_row(half ? page[2 + x] : page[x], j, b) * d;
-      if (brings_values) {
+      for (int i = 0; i < 8; ++i) {
+        uint32_t w[VD];
+        __builtin_memcpy(
+            w, __builtin_assume_aligned(vp + (int64_t)(i / 4 * 8 + i % 4) * d, 4 * VD), 4 * VD);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int8_t* vp = a.c.v + at + (i / 4 * 8 + i % 4) * d;
-          uint32_t w[VD];
-          __builtin_memcpy(w, __builtin_assume_aligned(vp + off, 4 * VD), 4 * VD);
+        for (int y = 0; y < VD; ++y) reg[8 * y + i] = w[y];
+      }
+    } else {
 #pragma unroll
-          for (int y = 0; y < VD; ++y) reg[x][8 * y + i] = w[y];
-        }
-      } else {
+      for (int p = 0; p < 2 * KB; ++p) {
+        const int8_t* kp = a.c.k + (p < KB ? at0 : at1) + p % KB * (64 / PR) * d;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(kp + off);
 #pragma unroll
-        for (int p = 0; p < KB; ++p) {
-          const int8_t* kp = a.c.k + at + p * (64 / PR) * d;
-          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + off);
-#pragma unroll
-          for (int y = 0; y < 4; ++y) reg[x][4 * p + y] = w[y];
-        }
+        for (int y = 0; y < 4; ++y) reg[4 * p + y] = w[y];
       }
     }
     if (!brings_values) {                                  // a lane has key `lane` of the step
@@ -640,38 +639,33 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     }
   };
   auto put = [&](int at, f16x8 v) { *reinterpret_cast<f16x8*>(smem + at) = v; };
-  // the lane's row in LDS and the place of its first chunk there; block and channel (values) or
-  // key (keys) below only turn its low bits
+  // the lane's first row in LDS and the place of its chunk there (which the rows' numbers turn)
   const int put_row = brings_values ? At::v + v_ch * 128 : At::k + (32 * half + k_key) * DT * 2;
-  const int put_bits = 16 * (brings_values ? (4 * half + (v_g & 1)) ^ ((v_ch >> 2) & 7)
-                                           : (k_ch / 8) ^ (k_key & 7));
+  const int put_bits = 16 * (brings_values ? (4 * half + lane / 16) ^ chunk_turn(v_ch)
+                                           : k_ch / 8 ^ key_turn(32 * half + k_key));
   auto stage = [&](auto par) {                             // buffer par
     constexpr int P = decltype(par)::value, kBuf = P * At::buffer;
+    if (brings_values) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      if (brings_values) {
-        if (DT == 64 && v_g >= 2) continue;
+      for (int y = 0; y < VD; ++y) {
+        uint32_t w[8];
 #pragma unroll
-        for (int y = 0; y < VD; ++y) {
-          uint32_t w[8];
+        for (int i = 0; i < 8; ++i) w[i] = reg[8 * y + i] ^ kFlip;
+        auto at = [&](int c) {                             // channel v_ch + 4 y + c
+          return kBuf + put_row + (4 * y + c) * 128 + (put_bits ^ 16 * chunk_turn(4 * y + c));
+        };
+        put(at(0), codes_f16_across<0>(w));
+        put(at(1), codes_f16_across<1>(w));
+        put(at(2), codes_f16_across<2>(w));
+        put(at(3), codes_f16_across<3>(w));
+      }
+    } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = reg[x][8 * y + i] ^ kFlip;
-          auto at = [&](int c) {
-            return kBuf + put_row + (put_bits ^ 16 * ((2 * x) ^ (2 * c) ^ y)) + (4 * y + c) * 128;
-          };
-          put(at(0), codes_f16_across<0>(w));
-          put(at(1), codes_f16_across<1>(w));
-          put(at(2), codes_f16_across<2>(w));
-          put(at(3), codes_f16_across<3>(w));
-        }
-      } else {
-#pragma unroll
-        for (int p = 0; p < KB; ++p) {
-          const int first = p * (64 / PR), turn = 16 * (first & 7);
-          const int at = kBuf + put_row + (16 * x + first) * DT * 2;
-          put(at + (put_bits ^ turn), codes_f16(reg[x][4 * p], reg[x][4 * p + 1]));
-          put(at + (put_bits ^ turn ^ 16), codes_f16(reg[x][4 * p + 2], reg[x][4 * p + 3]));
-        }
+      for (int p = 0; p < 2 * KB; ++p) {
+        const int key = p / KB * 16 + p % KB * (64 / PR);  // + 32 half + k_key
+        const int at = kBuf + put_row + key * DT * 2, turn = 16 * key_turn(key);
+        put(at + (put_bits ^ turn), codes_f16(reg[4 * p], reg[4 * p + 1]));
+        put(at + (put_bits ^ turn ^ 16), codes_f16(reg[4 * p + 2], reg[4 * p + 3]));
       }
     }
     if (!brings_values) {
@@ -696,12 +690,12 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     for (int i = 0; i < 16; ++i) o[x][i] = 0.0f;
   float m = kNegInf, l = 0.0f;
   // the chunks that a lane reads: of key r (its even and odd chunks, four by four), of channel r
-  int k_at[4], v_at[4];
+  constexpr int KA = DT == 64 ? 4 : 8;                     // columns of chunks that turn together
+  int k_at[KA], v_at[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    k_at[i] = At::k + r * DT * 2 + ((2 * i + h) ^ (r & 7)) * 16;
-    v_at[i] = At::v + r * 128 + ((2 * i + h) ^ (2 * (r & 3)) ^ ((r >> 2) & 7)) * 16;
-  }
+  for (int i = 0; i < KA; ++i) k_at[i] = At::k + r * DT * 2 + ((2 * i + h) ^ key_turn(r)) * 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v_at[i] = At::v + r * 128 + ((2 * i + h) ^ chunk_turn(r)) * 16;
   typedef std::integral_constant<int, 0> Even;
   typedef std::integral_constant<int, 1> Odd;
   if (steps > 0) {
@@ -731,8 +725,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 #pragma unroll
     for (int i = 0; i < 2 * KS; ++i) {
       const int u = NP == 1 ? i % 2 : i / KS, k = NP == 1 ? i / 2 : i % KS;
-      const f16x8 kf = *reinterpret_cast<const f16x8*>(smem + k_at[k % 4] + P * At::buffer +
-                                                       32 * u * DT * 2 + k / 4 * 128);
+      const f16x8 kf = *reinterpret_cast<const f16x8*>(smem + k_at[k % KA] + P * At::buffer +
+                                                       32 * u * DT * 2 + k / KA * 256);
 #pragma unroll
       for (int n = 0; n < NP; ++n)
         s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s[u], 0, 0, 0);

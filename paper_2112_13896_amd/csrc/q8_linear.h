@@ -85,8 +85,9 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
 // wavefront in 32 x 32 products, 128 codes of k a step.  Codes go from memory
 // straight into LDS, 16 bytes a lane, into the buffer that is not being
 // multiplied; one barrier a step.  A row's eight 16-byte chunks are permuted
-// (xor with its number's low bits) so that eight lanes reading a column of
-// chunks meet all banks; as LDS receives a wavefront's load in lane order, the
+// (chunk_turn) so that the sixteen lanes served together when a column of
+// chunks is read meet all 64 banks (with row % 8 alone, every such read took
+// half as long again); as LDS receives a wavefront's load in lane order, the
 // permutation is made in the addresses it loads from.  Rows past the end
 // repeat the last one and are not stored; the codes past the last whole 128 go
 // through registers, zeros after k.
@@ -136,17 +137,17 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   const int8_t* xb = a.x + t0 * a.ldx;
   const int8_t* wb = a.w + (int64_t)n0 * a.ldw;
   const int xrows = (int)min<int64_t>(BM, a.rows - t0), wrows = min(BN, a.d_out - n0);
-  // the 16-byte chunk `piece` of a buffer: row piece / 8, the row's chunk (piece % 8) ^ (row % 8)
+  // the 16-byte chunk `piece` of a buffer: row piece / 8, the row's chunk (piece % 8) ^ chunk_turn(row)
   uint32_t xo[PX], wo[PW];
 #pragma unroll
   for (int p = 0; p < PX; ++p) {
     const int piece = p * THREADS + tid, row = piece / 8;
-    xo[p] = (uint32_t)min(row, xrows - 1) * (uint32_t)a.ldx + ((piece ^ row) & 7) * 16;
+    xo[p] = (uint32_t)min(row, xrows - 1) * (uint32_t)a.ldx + ((piece ^ chunk_turn(row)) & 7) * 16;
   }
 #pragma unroll
   for (int p = 0; p < PW; ++p) {
     const int piece = p * THREADS + tid, row = piece / 8;
-    wo[p] = (uint32_t)min(row, wrows - 1) * (uint32_t)a.ldw + ((piece ^ row) & 7) * 16;
+    wo[p] = (uint32_t)min(row, wrows - 1) * (uint32_t)a.ldw + ((piece ^ chunk_turn(row)) & 7) * 16;
   }
   const int mr = wave / NW * WM, nr = wave % NW * WN;
   const int fr = lane % 32, fh = lane / 32;
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   auto multiply = [&](const int8_t* lx, const int8_t* lw) {
     i32x4 fx[2][MT], fw[2][NT];
     auto read = [&](int s) {
-      const int at = fr * 128 + ((2 * s + fh) ^ (fr & 7)) * 16;
+      const int at = fr * 128 + ((2 * s + fh) ^ chunk_turn(fr)) * 16;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
         fx[s & 1][m] = *reinterpret_cast<const i32x4*>(lx + (mr + 32 * m) * 128 + at);
@@ -220,14 +221,14 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
       const int piece = p * THREADS + tid, row = piece / 8;
       *reinterpret_cast<i32x4*>(lx0 + piece * 16) =
           codes16<true>(xb + (int64_t)min(row, xrows - 1) * a.ldx,
-                        k0 + ((piece ^ row) & 7) * 16, a.k);
+                        k0 + ((piece ^ chunk_turn(row)) & 7) * 16, a.k);
     }
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
       const int piece = p * THREADS + tid, row = piece / 8;
       *reinterpret_cast<i32x4*>(lw0 + piece * 16) =
           codes16<true>(wb + (int64_t)min(row, wrows - 1) * a.ldw,
-                        k0 + ((piece ^ row) & 7) * 16, a.k);
+                        k0 + ((piece ^ chunk_turn(row)) & 7) * 16, a.k);
     }
     __syncthreads();
     multiply(lx0, lw0);
