@@ -181,7 +181,9 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
   const size_t need = cs_linear_q8_workspace_bytes(xt, rows, k, d_out);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  cs::Q8Linear a{static_cast<const int8_t*>(x), ldx, sx, rows, k, w, ldw, sw, d_out, bias, y, ldy};
+  const int y_vec = aligned(y, 16) && ldy * (int64_t)float_size(yt) % 16 == 0;
+  cs::Q8Linear a{static_cast<const int8_t*>(x), ldx, sx, rows, k, w, ldw, sw, d_out, bias, y, ldy,
+                 y_vec};
   const bool w_al = aligned(w, 16) && ldw % 16 == 0 && ldw < (1 << 23);
   // A few tokens are quantised by every workgroup of the product itself.
   if (is_float(xt) && w_al && rows <= 16 && rows * k <= kFusedElements)

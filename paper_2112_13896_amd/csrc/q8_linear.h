@@ -24,6 +24,7 @@ struct Q8Linear {
   const float* bias;
   void* y;
   int64_t ldy;
+  int y_vec;           // rows of y start on 16 bytes
 };
 
 // 16 codes of a row from element e on; those past k read as 0.  ALIGNED: rows
@@ -91,6 +92,9 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
 // permutation is made in the addresses it loads from.  Rows past the end
 // repeat the last one and are not stored; the codes past the last whole 128 go
 // through registers, zeros after k.
+// The products are w times x: a lane then holds four neighbouring channels of
+// one token, which go through LDS (free by then), 32 tokens of a wavefront at a
+// time, to be stored as whole rows of its tile, 16 bytes a lane.
 struct TileOrder {
   uint32_t tiles_m, tiles_n, per_xcd, more;                // tiles / 8, tiles % 8
 };
@@ -128,6 +132,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   constexpr int MT = WM / 32, NT = WN / 32;
   constexpr int PX = BM * 8 / THREADS, PW = BN * 8 / THREADS;
   __shared__ __align__(16) int8_t lx0[BM * 128], lx1[BM * 128], lw0[BN * 128], lw1[BN * 128];
+  __shared__ __align__(16) float l_sw[BN], l_bias[BN];
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   int tm, tn;
@@ -181,7 +186,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
 #pragma unroll
         for (int n = 0; n < NT; ++n)
           acc[m][n] =
-              __builtin_amdgcn_mfma_i32_32x32x32_i8(fx[s & 1][m], fw[s & 1][n], acc[m][n], 0, 0, 0);
+              __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[s & 1][n], fx[s & 1][m], acc[m][n], 0, 0, 0);
       if (s < 3) {
 #pragma unroll
         for (int i = 0; i < MT * NT; ++i) {
@@ -193,6 +198,14 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
       }
     }
   };
+  for (int i = tid; i < BN; i += THREADS) {
+    const int o = min(n0 + i, a.d_out - 1);
+    l_sw[i] = a.sw[o];
+    l_bias[i] = a.bias ? a.bias[o] : 0.0f;
+  }
+  float sx[MT];                                            // of the lane's tokens
+#pragma unroll
+  for (int m = 0; m < MT; ++m) sx[m] = a.sx[min<int64_t>(t0 + mr + 32 * m + fr, a.rows - 1)];
   const int whole = a.k / 128;
   if (whole > 0) {
     codes_to_lds<BM, THREADS>(xb, xo, 0, lx0);
@@ -233,27 +246,50 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
     __syncthreads();
     multiply(lx0, lw0);
   }
-  float sw[NT], bias[NT];
+  __syncthreads();                                         // the last operands have been read
+  constexpr int kRow = WN * (int)sizeof(T) + 16;           // a token's bytes in LDS, padded
+  constexpr int kShare = THREADS / 64 / 4;                 // wavefronts to a buffer
+  static_assert(kShare * 32 * kRow <= BM * 128 && kShare * 32 * kRow <= BN * 128, "");
+  const int buf = wave / kShare;
+  int8_t* out = (buf == 0 ? lx0 : buf == 1 ? lx1 : buf == 2 ? lw0 : lw1) + wave % kShare * 32 * kRow;
+  constexpr int E = 16 / sizeof(T), kPieces = WN / E;      // elements of 16 bytes, pieces of a row
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const int nvalid = a.d_out - n0 - nr;                    // channels of the wavefront's tile
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int o = min(n0 + nr + 32 * n + fr, a.d_out - 1);
-    sw[n] = a.sw[o];
-    bias[n] = a.bias ? a.bias[o] : 0.0f;
-  }
+  for (int m = 0; m < MT; ++m) {
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t t = t0 + mr + 32 * m + 8 * (i / 4) + 4 * fh + i % 4;
+      for (int y = 0; y < 4; ++y) {
+        const int ch = 32 * n + 8 * y + 4 * fh;
+        const f32x4 sw = *reinterpret_cast<const f32x4*>(l_sw + nr + ch);
+        const f32x4 bias = *reinterpret_cast<const f32x4*>(l_bias + nr + ch);
+        t4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[i] = (T)fmaf((float)acc[m][n][4 * y + i], sx[m] * sw[i], bias[i]);
+        *reinterpret_cast<t4*>(out + fr * kRow + ch * sizeof(T)) = v;
+      }
+    wave_lds_order();
+#pragma unroll
+    for (int p = lane; p < 32 * kPieces; p += 64) {
+      const int tok = p / kPieces, e = p % kPieces * E;
+      const int64_t t = t0 + mr + 32 * m + tok;
       if (t >= a.rows) continue;
-      const float sx = a.sx[t];
-      T* y = static_cast<T*>(a.y) + t * a.ldy;
+      T* y = static_cast<T*>(a.y) + t * a.ldy + n0 + nr + e;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(out + tok * kRow + e * sizeof(T));
+      if (a.y_vec && e + E <= nvalid) {
+        *reinterpret_cast<u32x4*>(y) = v;
+      } else {
+        T el[E];
+        __builtin_memcpy(el, &v, 16);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int o = n0 + nr + 32 * n + fr;
-        if (o < a.d_out) y[o] = (T)fmaf((float)acc[m][n][i], sx * sw[n], bias[n]);
+        for (int i = 0; i < E; ++i)
+          if (e + i < nvalid) y[i] = el[i];
       }
     }
+    wave_lds_order();
+  }
 }
 
 // linear_q8_few: few tokens, where reading w is the work.  16 output channels
