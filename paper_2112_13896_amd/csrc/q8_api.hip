@@ -37,12 +37,16 @@ template <typename T, int WPR>
 int quantise_launch(const T* x, int64_t ldx, int64_t rows, int c, int8_t* q, int64_t ldq,
                     float* scale, hipStream_t s) {
   const dim3 grid((unsigned)((rows * WPR + 3) / 4)), block(256);
-  if (aligned(x, 16) && (rows == 1 || ldx * sizeof(T) % 16 == 0))
-    hipLaunchKernelGGL((cs::quantise_rows<T, true, WPR>), grid, block, 0, s, x, ldx, rows, c, q,
+  auto starts_on = [&](size_t n) { return aligned(x, n) && (rows == 1 || ldx * sizeof(T) % n == 0); };
+  if (starts_on(16))
+    hipLaunchKernelGGL((cs::quantise_rows<T, 16, WPR>), grid, block, 0, s, x, ldx, rows, c, q,
                        ldq, scale);
+  else if (sizeof(T) == 4 || starts_on(4))
+    hipLaunchKernelGGL((cs::quantise_rows<T, 4, WPR>), grid, block, 0, s, x, ldx, rows, c, q, ldq,
+                       scale);
   else
-    hipLaunchKernelGGL((cs::quantise_rows<T, false, WPR>), grid, block, 0, s, x, ldx, rows, c, q,
-                       ldq, scale);
+    hipLaunchKernelGGL((cs::quantise_rows<T, (int)sizeof(T), WPR>), grid, block, 0, s, x, ldx,
+                       rows, c, q, ldq, scale);
   return launched();
 }
 
@@ -59,7 +63,7 @@ int quantise(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int c, int8_
 }
 
 // ---------------------------------------------------------------- linear
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int NB>
 int linear_tiles(const cs::Q8Linear& a, hipStream_t s) {
   cs::TileOrder o;
   const int64_t tm = (a.rows + BM - 1) / BM, tn = ((int64_t)a.d_out + BN - 1) / BN;
@@ -68,12 +72,17 @@ int linear_tiles(const cs::Q8Linear& a, hipStream_t s) {
   o.tiles_n = (uint32_t)tn;
   o.per_xcd = (uint32_t)(tm * tn / 8);
   o.more = (uint32_t)(tm * tn % 8);
-  hipLaunchKernelGGL((cs::linear_q8_tile<T, BM, BN, WM, WN>), dim3((unsigned)(tm * tn)),
+  hipLaunchKernelGGL((cs::linear_q8_tile<T, BM, BN, WM, WN, NB>), dim3((unsigned)(tm * tn)),
                      dim3(BM / WM * (BN / WN) * 64), 0, s, a, o);
   return launched();
 }
 
-constexpr int64_t kFusedElements = 8192;
+// Elements of up to 16 tokens that every workgroup of the product quantises itself, instead of a
+// launch that does it once (a recorded graph of the call, bf16, k x d_out as given): 1 x 2,048 4.8
+// against 7.8 us, 1 x 16,384 19.5 | 26.0, 4 x 4,096 9.3 | 9.4, 8 x 2,048 7.4 | 8.4, 16 x 1,024 7.5 |
+// 6.8; beyond, 8 x 4,096 16.2 | 12.6, 16 x 2,048 10.9 | 8.9.  Calls that are not recorded save
+// 2.7 us of the host's time on top.
+constexpr int64_t kFusedElements = 16384;
 
 template <typename T, typename XT, int RT>
 int linear_few(const cs::Q8Linear& a, hipStream_t s) {
@@ -217,9 +226,9 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     if (rows <= 16) return linear_few<T, int8_t, 1>(a, s);
     if (rows <= 32) return linear_few<T, int8_t, 2>(a, s);
     if (rows <= 64) return linear_few<T, int8_t, 4>(a, s);
-    if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64>(a, s);
-    if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64>(a, s);
-    return linear_tiles<T, 64, 64, 32, 32>(a, s);
+    if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64, 2>(a, s);
+    if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64, 2>(a, s);
+    return linear_tiles<T, 64, 64, 32, 32, 4>(a, s);
   });
 }
 

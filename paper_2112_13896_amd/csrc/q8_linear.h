@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "q8_rows.h"
 
 namespace cs {
@@ -27,11 +29,29 @@ struct Q8Linear {
   int y_vec;           // rows of y start on 16 bytes
 };
 
-// 16 codes of a row from element e on; those past k read as 0.  ALIGNED: rows
-// start on 16 bytes, so whole pieces are one load.
-template <bool ALIGNED>
-__device__ __forceinline__ i32x4 codes16(const int8_t* row, int e, int k) {
-  if (ALIGNED && e + 16 <= k) return *reinterpret_cast<const i32x4*>(row + e);
+// 16 codes of a row from element e on; those past k read as 0.  The row starts
+// on 16 bytes.  `inner`: it is not the matrix's last, so that its bytes up to a
+// multiple of 16 are the matrix's own and can be loaded.
+__device__ __forceinline__ i32x4 codes16(const int8_t* row, int e, int k, bool inner) {
+  i32x4 v = {0, 0, 0, 0};
+  if (e >= k) return v;
+  if (inner || e + 16 <= k) {
+    v = *reinterpret_cast<const i32x4*>(row + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int keep = k - e - 4 * i;                      // bytes of the dword before k
+      if (keep < 4) v[i] = keep <= 0 ? 0 : v[i] & (int)((1u << (8 * keep)) - 1);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (e + i < k) v[i / 4] |= (int)((uint32_t)(uint8_t)row[e + i] << (8 * (i % 4)));
+  }
+  return v;
+}
+
+// The same of a row that starts anywhere.
+__device__ __forceinline__ i32x4 codes16_any(const int8_t* row, int e, int k) {
   i32x4 v = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 16; ++i)
@@ -59,8 +79,8 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
   const int fr = lane % 32, fk = lane / 32 * 16;
   i32x16 acc = {};
   for (int k0 = 0; k0 < a.k; k0 += 64) {
-    const i32x4 vx = codes16<false>(xr, k0 + sc, a.k);
-    const i32x4 vw = codes16<false>(wr, k0 + sc, a.k);
+    const i32x4 vx = codes16_any(xr, k0 + sc, a.k);
+    const i32x4 vw = codes16_any(wr, k0 + sc, a.k);
     __syncthreads();
     *reinterpret_cast<i32x4*>(lx + sr * kLd + sc) = vx;
     *reinterpret_cast<i32x4*>(lw + sr * kLd + sc) = vw;
@@ -84,8 +104,8 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
 
 // linear_q8_tile: a BM x BN tile of y to a workgroup, WM x WN of it to a
 // wavefront in 32 x 32 products, 128 codes of k a step.  Codes go from memory
-// straight into LDS, 16 bytes a lane, into the buffer that is not being
-// multiplied; one barrier a step.  A row's eight 16-byte chunks are permuted
+// straight into LDS, 16 bytes a lane, NB - 1 steps ahead of the products, with
+// NB buffers and one barrier a step.  A row's eight 16-byte chunks are permuted
 // (chunk_turn) so that the sixteen lanes served together when a column of
 // chunks is read meet all 64 banks (with row % 8 alone, every such read took
 // half as long again); as LDS receives a wavefront's load in lane order, the
@@ -125,13 +145,26 @@ __device__ __forceinline__ void codes_to_lds(const int8_t* base,
                                      (lvoid*)(lds + (p * THREADS + wave * 64) * 16), 16, 0, 0);
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+// All but the last N of this wavefront's loads have landed, its LDS reads are
+// done, and so are the other wavefronts'.
+template <int N>
+__device__ __forceinline__ void landed() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int NB>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8Linear a,
                                                                              TileOrder order) {
   constexpr int NW = BN / WN, THREADS = BM / WM * NW * 64;
   constexpr int MT = WM / 32, NT = WN / 32;
   constexpr int PX = BM * 8 / THREADS, PW = BN * 8 / THREADS;
+  // (variables of their own: the compiler then knows that a load into one is not read in another)
   __shared__ __align__(16) int8_t lx0[BM * 128], lx1[BM * 128], lw0[BN * 128], lw1[BN * 128];
+  __shared__ __align__(16) int8_t lx2[NB > 2 ? BM * 128 : 16], lw2[NB > 2 ? BN * 128 : 16];
+  __shared__ __align__(16) int8_t lx3[NB > 2 ? BM * 128 : 16], lw3[NB > 2 ? BN * 128 : 16];
+  static_assert(NB == 2 || NB == 4, "");
   __shared__ __align__(16) float l_sw[BN], l_bias[BN];
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -207,41 +240,55 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
 #pragma unroll
   for (int m = 0; m < MT; ++m) sx[m] = a.sx[min<int64_t>(t0 + mr + 32 * m + fr, a.rows - 1)];
   const int whole = a.k / 128;
+  // step s's codes into buffer B; past the last step its codes again, into a buffer that nobody
+  // reads any more, so that every step counts as many loads
+  auto fetch = [&](auto buffer, int s) {
+    constexpr int B = decltype(buffer)::value;
+    const int k0 = min(s, whole - 1) * 128;
+    codes_to_lds<BM, THREADS>(xb, xo, k0, B == 0 ? lx0 : B == 1 ? lx1 : B == 2 ? lx2 : lx3);
+    codes_to_lds<BN, THREADS>(wb, wo, k0, B == 0 ? lw0 : B == 1 ? lw1 : B == 2 ? lw2 : lw3);
+  };
+  auto step = [&](auto buffer, int s) {
+    constexpr int B = decltype(buffer)::value;
+    landed<(NB - 2) * (PX + PW)>();
+    fetch(std::integral_constant<int, (B + NB - 1) % NB>{}, s + NB - 1);
+    multiply(B == 0 ? lx0 : B == 1 ? lx1 : B == 2 ? lx2 : lx3,
+             B == 0 ? lw0 : B == 1 ? lw1 : B == 2 ? lw2 : lw3);
+  };
   if (whole > 0) {
-    codes_to_lds<BM, THREADS>(xb, xo, 0, lx0);
-    codes_to_lds<BN, THREADS>(wb, wo, 0, lw0);
-  }
-  for (int s = 0; s < whole; s += 2) {
-    __syncthreads();                                       // this step's codes are there
-    if (s + 1 < whole) {
-      codes_to_lds<BM, THREADS>(xb, xo, (s + 1) * 128, lx1);
-      codes_to_lds<BN, THREADS>(wb, wo, (s + 1) * 128, lw1);
+    fetch(std::integral_constant<int, 0>{}, 0);
+    if constexpr (NB > 2) {
+      fetch(std::integral_constant<int, 1>{}, 1);
+      fetch(std::integral_constant<int, 2>{}, 2);
     }
-    multiply(lx0, lw0);
+  }
+  for (int s = 0; s < whole; s += NB) {
+    step(std::integral_constant<int, 0>{}, s);
     if (s + 1 >= whole) break;
-    __syncthreads();
-    if (s + 2 < whole) {
-      codes_to_lds<BM, THREADS>(xb, xo, (s + 2) * 128, lx0);
-      codes_to_lds<BN, THREADS>(wb, wo, (s + 2) * 128, lw0);
+    step(std::integral_constant<int, 1>{}, s + 1);
+    if constexpr (NB > 2) {
+      if (s + 2 >= whole) break;
+      step(std::integral_constant<int, 2>{}, s + 2);
+      if (s + 3 >= whole) break;
+      step(std::integral_constant<int, 3>{}, s + 3);
     }
-    multiply(lx1, lw1);
   }
+  landed<0>();
   if (a.k % 128 != 0) {
     const int k0 = whole * 128;
-    __syncthreads();
 #pragma unroll
     for (int p = 0; p < PX; ++p) {
-      const int piece = p * THREADS + tid, row = piece / 8;
+      const int piece = p * THREADS + tid, row = min(piece / 8, xrows - 1);
       *reinterpret_cast<i32x4*>(lx0 + piece * 16) =
-          codes16<true>(xb + (int64_t)min(row, xrows - 1) * a.ldx,
-                        k0 + ((piece ^ chunk_turn(row)) & 7) * 16, a.k);
+          codes16(xb + (int64_t)row * a.ldx, k0 + ((piece ^ chunk_turn(piece / 8)) & 7) * 16, a.k,
+                  t0 + row + 1 < a.rows);
     }
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
-      const int piece = p * THREADS + tid, row = piece / 8;
+      const int piece = p * THREADS + tid, row = min(piece / 8, wrows - 1);
       *reinterpret_cast<i32x4*>(lw0 + piece * 16) =
-          codes16<true>(wb + (int64_t)min(row, wrows - 1) * a.ldw,
-                        k0 + ((piece ^ chunk_turn(row)) & 7) * 16, a.k);
+          codes16(wb + (int64_t)row * a.ldw, k0 + ((piece ^ chunk_turn(piece / 8)) & 7) * 16, a.k,
+                  n0 + row + 1 < a.d_out);
     }
     __syncthreads();
     multiply(lx0, lw0);
@@ -314,6 +361,7 @@ __global__ __launch_bounds__(NW * 64) void linear_q8_few(Q8Linear a) {
   const int r = lane % 16, h = lane / 16;
   const int n0 = blockIdx.x * 16, steps = (a.k + 127) / 128, kpad = steps * 128;
   const int8_t* wr = a.w + (int64_t)min(n0 + r, a.d_out - 1) * a.ldw;
+  const bool w_inner = n0 + r + 1 < a.d_out;
   i32x4 w[kFewSteps][2];
   auto load_w = [&](int s0) {
 #pragma unroll
@@ -323,7 +371,7 @@ __global__ __launch_bounds__(NW * 64) void linear_q8_few(Q8Linear a) {
 #pragma unroll
       for (int y = 0; y < 2; ++y)
         w[i][y] = s + 1 < steps ? *reinterpret_cast<const i32x4*>(wr + e + 16 * y)
-                                : codes16<true>(wr, e + 16 * y, a.k);
+                                : codes16(wr, e + 16 * y, a.k, w_inner);
     }
   };
   load_w(wave);
@@ -386,7 +434,7 @@ __global__ __launch_bounds__(NW * 64) void linear_q8_few(Q8Linear a) {
           else if (s + 1 < steps)
             x = *reinterpret_cast<const i32x4*>(a.x + row * a.ldx + e + 16 * y);
           else
-            x = codes16<true>(a.x + row * a.ldx, e + 16 * y, a.k);
+            x = codes16(a.x + row * a.ldx, e + 16 * y, a.k, row + 1 < a.rows);
           acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][y], x, acc[t], 0, 0, 0);
         }
       }

@@ -40,6 +40,14 @@ __device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
     for (int i = 0; i < 8; ++i) f[i] = to_f32(a[i]);
   }
 }
+// The same where p is aligned to ALIGN bytes only.
+template <int ALIGN, typename T>
+__device__ __forceinline__ void load8_at(const T* p, float (&f)[8]) {
+  T t[8];
+  __builtin_memcpy(t, __builtin_assume_aligned(p, ALIGN), sizeof(t));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = to_f32(t[i]);
+}
 template <typename T>
 __device__ __forceinline__ void load8_some(const T* p, int n, float (&f)[8]) {
 #pragma unroll
@@ -103,7 +111,8 @@ __device__ __forceinline__ u32x2 row_codes8(const float (&f)[8], const RowScale&
 // and 8,192 (WPR 4) elements are read once; longer rows' rest is read twice.
 constexpr int kRowHeld = 4;
 
-template <typename T, bool VEC, int WPR>
+// ALIGN: rows start on 16 bytes, on 4, or anywhere.
+template <typename T, int ALIGN, int WPR>
 __global__ __launch_bounds__(256) void quantise_rows(const T* __restrict__ x, int64_t ldx,
                                                      int64_t rows, int c, int8_t* __restrict__ q,
                                                      int64_t ldq, float* __restrict__ scale) {
@@ -115,7 +124,7 @@ __global__ __launch_bounds__(256) void quantise_rows(const T* __restrict__ x, in
   const T* xr = x + (live ? row : 0) * ldx;
   const int nv = live ? (c + 7) / 8 : 0;
   auto fetch = [&](int v, float (&f)[8]) {
-    if (VEC && 8 * v + 8 <= c) load8(xr + 8 * (int64_t)v, f);
+    if (8 * v + 8 <= c) load8_at<ALIGN>(xr + 8 * (int64_t)v, f);
     else load8_some(xr + 8 * (int64_t)v, c - 8 * v, f);
   };
   float f[kRowHeld][8];
