@@ -846,6 +846,8 @@ __global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
   for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
   const float base = top == kNegInf ? 0.0f : top;
   const float f = exp2_fast(ml.x - base);                  // a part without a key: 0
+  float sum = ml.y * f;                                    // (while all lanes are there)
+  for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
   const int ch = 4 * lane < d ? 4 * lane : 0;
   const float* po = a.part_o + row * d + ch;
   f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -861,9 +863,6 @@ __global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
   __syncthreads();
   if (wave > 0 || 4 * lane >= d) return;
   y = l_y[0][lane] + l_y[1][lane] + l_y[2][lane] + l_y[3][lane];
-  float sum = 0.0f;
-  for (int s = 0; s < a.splits; ++s)
-    sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ml.y * f), s));
   y *= sum == 0.0f ? 0.0f : kCodeScale / sum;
   typedef T t4 __attribute__((ext_vector_type(4)));
   *reinterpret_cast<t4*>(static_cast<T*>(a.out) + row * d + ch) =

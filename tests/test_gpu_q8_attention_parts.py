@@ -1,0 +1,32 @@
+"""Rows whose key axis is split into more parts than the join has lanes for a row's channels."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2112_13896_amd import ops
+from tests.q8_util import DTYPES, Sequences
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [16, 64, 80, 128, 256])
+@pytest.mark.parametrize("seqs", [[(1, 20000)], [(1, 17000), (2, 600), (1, 9000)]])
+def test_many_parts(dtype, d, seqs):
+    s = Sequences(d, seqs, 1, 2, d, 64, DTYPES[dtype])
+    s.check(ops.paged_attention(*s.args()))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_parts_of_many_rows(dtype):
+    s = Sequences(3, [(70, 20000)], 1, 1, 64, 64, DTYPES[dtype])
+    s.check(ops.paged_attention(*s.args()))
+
+
+def test_nan_in_one_part():
+    """A key that is not a number, alone in its part, reaches the row that sees it."""
+    s = Sequences(4, [(1, 20000), (1, 19000)], 1, 1, 32, 64, torch.bfloat16)
+    pg, off = divmod(s.slot(0, 12345), 64)
+    s.ks[pg, 0, off] = float("nan")
+    s.check(ops.paged_attention(*s.args()))
