@@ -42,11 +42,12 @@ def sources() -> list:
 
 
 def source_digest() -> str:
-    """SHA-256 over every native source and header the library is built from."""
+    """SHA-256 over every source and header the layer kernels (csrc/cs_api.hip, csrc/cs_pack.cpp)
+    are built from: the native sources but those of the 8-bit attention-layer operators."""
     import hashlib
     h = hashlib.sha256()
     files = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)
-                   if f.endswith((".hip", ".cpp", ".h")))
+                   if f.endswith((".hip", ".cpp", ".h")) and not f.startswith("q8_"))
     files.append(os.path.join(INCLUDE, "cs.h"))
     for f in files:
         h.update(os.path.basename(f).encode())
