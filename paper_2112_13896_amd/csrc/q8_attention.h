@@ -20,7 +20,7 @@
 //    To round it to f16 it is kept relative to the row's own largest: with
 //    sv_j = a_j 2^E_j (1 <= a_j < 2), x_j = log2(e_j) + E_j and m the running
 //    maximum of x_j over the keys the row sees, w_j = a_j 2^(x_j - m + 12) is
-//    at most 2^13 and the denominator is the sum of 2^(x_j - m + 12) 2^-E_j.
+//    at most 2^13 and the denominator is the sum of w_j / sv_j.
 //    A token with large values that a row does not see, or hardly weighs,
 //    takes no precision from the others.  m follows the maximum only when that
 //    is more than 4 (2^2) above it: halves have the room, and the sums so far
@@ -194,17 +194,37 @@ __device__ __forceinline__ RowNorm row_norm(float amax, float scale) {
   return r;
 }
 
-// How a token's values enter: sv = a 2^E (zero values: any E far below).
+// How a token's values enter: sv = a 2^E.  Where all of a token's values are
+// zero, so are its codes, and any scale does that leaves the others room.
 struct ValueScale {
-  float e, a, r;                                           // E, a, 2^-E
+  float e, a, r;                                           // E, a, 1 / sv
 };
 __device__ __forceinline__ ValueScale value_scale(float sv) {
   ValueScale v;
-  const int ex = fabsf(sv) > 0.0f ? max(__builtin_amdgcn_frexp_expf(sv) - 1, -120) : -60;
+  if (sv == 0.0f) sv = 0x1p-60f;
+  const int ex = max(__builtin_amdgcn_frexp_expf(sv) - 1, -120);
   v.e = (float)ex;
   v.a = ldexpf(sv, -ex);                                   // NaN stays
-  v.r = ldexpf(1.0f, -ex);
+  v.r = ldexpf(__builtin_amdgcn_rcpf(v.a), -ex);
   return v;
+}
+
+// Adds eight weights' share to a row's denominator (r: 1 / sv).  f16 outputs
+// are as fine as the rounded weights, whose errors would show: there the sum
+// takes the weights as rounded, so that their quotients still sum to 1 and a
+// row that one key rules has no error from its rounding (but not those that
+// are too small for a half to hold: their keys' values may be small, not their
+// part in the sum).
+template <typename T, int NP>
+__device__ __forceinline__ float add_weights(float l, const float (&w)[8], const f16x8 (&p)[NP],
+                                             const float (&r)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float t = w[i];
+    if (std::is_same<T, _Float16>::value && t > 0x1p-13f) t = (float)p[0][i];
+    l = fmaf(t, r[i], l);
+  }
+  return l;
 }
 
 template <typename T>
@@ -383,7 +403,7 @@ void attention_few(PagedAttention a) {
         const int key = j + 16 * (i / 4) + 4 * h + i % 4;
         if (key > pos || key < see || !ok[i / 4]) {
           x[i] = kNegInf;
-          av[i] = 0.0f;
+          av[i] = rv[i] = 0.0f;                            // (they may be NaN)
         }
       }
     }
@@ -399,13 +419,10 @@ void attention_few(PagedAttention a) {
     const float base = m == kNegInf ? 0.0f : m - kHead;
     float w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float e = exp2_fast(x[i] - base);
-      l = fmaf(e, rv[i], l);
-      w[i] = e * av[i];
-    }
+    for (int i = 0; i < 8; ++i) w[i] = exp2_fast(x[i] - base) * av[i];
     f16x8 p[NP];
     split_f16<NP>(w, p);
+    l = add_weights<T, NP>(l, w, p, rv);
     auto values = [&](auto cc, int xw) {
       constexpr int C = decltype(cc)::value;
       const f16x8 vf = codes_f16_across<C>(vr[xw]);
@@ -775,18 +792,19 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     const float base = m == kNegInf ? 0.0f : m - kHead;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      float w[8];
+      float w[8], rv[8];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         const f32x4 rs = meta4(At::rs, 2 * v + y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           w[4 * y + i] = exp2_fast(s[v / 2][v % 2 * 8 + 4 * y + i] - base);
-          l = fmaf(w[4 * y + i], rs[i], l);
+          rv[4 * y + i] = rs[i];
         }
       }
       f16x8 p[NP];
       split_f16<NP>(w, p);
+      l = add_weights<T, NP>(l, w, p, rv);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         const f16x8 vf = *reinterpret_cast<const f16x8*>(smem + v_at[v] + P * At::buffer +
