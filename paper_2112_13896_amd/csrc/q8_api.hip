@@ -223,9 +223,13 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     auto tiles = [&](int bm, int bn) {
       return ((rows + bm - 1) / bm) * (((int64_t)d_out + bn - 1) / bn);
     };
+    // tokens x k x d_out in us, registers alone | 64 x 64 tiles: 16 x 2,048 x 1,000 4.3 | 6.0, 16 x
+    // 8,192 x 8,192 19.2 | 19.1; 32 x 2,048 x 1,000 5.4 | 6.2, 32 x 8,192 x 1,024 12.9 | 15.3, 32 x
+    // 1,024 x 8,192 5.6 | 4.8, 32 x 8,192 x 8,192 26.6 | 19.2; 48 x 512 x 512 4.9 | 3.8
     if (rows <= 16) return linear_few<T, int8_t, 1>(a, s);
-    if (rows <= 32) return linear_few<T, int8_t, 2>(a, s);
-    if (rows <= 64) return linear_few<T, int8_t, 4>(a, s);
+    if (rows <= 32 && d_out <= 2048) return linear_few<T, int8_t, 2>(a, s);
+    // the largest tile of which there are enough to keep most compute units busy: 2,048 x 4,096 x
+    // 4,096 40 us in 128 x 128, 59 in 64 x 64; 8,192 x 4,096 x 8,192 245 in 256 x 256, 290 in 128 x 128
     if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64, 2>(a, s);
     if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64, 2>(a, s);
     return linear_tiles<T, 64, 64, 32, 32, 4>(a, s);
