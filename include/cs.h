@@ -731,6 +731,7 @@ size_t cs_workspace_bytes(int op, cs_dtype xt, int64_t rows, int c_in);
  */
 
 #define CS_MAX_Q8_K 131072      /* k of cs_linear_q8: that many products of two codes fit int32 */
+#define CS_MAX_Q8_OUT (1 << 22) /* d_out of cs_linear_q8                                        */
 #define CS_MAX_Q8_LEN (1 << 30) /* positions that a row of cs_paged_attention's table holds     */
 
 /*
@@ -763,7 +764,7 @@ int cs_quantise_rows(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int 
  *  Rows of x and w that start on 16 bytes are staged 16 bytes at a time; pad
  *  the row stride of an odd k to a multiple of 16 to have that.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (a stride below its row,
- *  k > CS_MAX_Q8_K, more than 2^31 - 1 rows), CS_ERR_WORKSPACE, CS_ERR_DEVICE.
+ *  k > CS_MAX_Q8_K, d_out > CS_MAX_Q8_OUT, more than 2^31 - 1 rows), CS_ERR_WORKSPACE, CS_ERR_DEVICE.
  */
 int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64_t rows, int k,
                  const int8_t* w, int64_t ldw, const float* sw, int d_out, const float* bias,
@@ -779,7 +780,8 @@ size_t cs_linear_q8_workspace_bytes(cs_dtype xt, int64_t rows, int k, int d_out)
  * s / page.  Every array is the caller's device memory, codes 16-byte aligned.
  *  page    tokens of a page: a power of two from 16 to 1024.
  *  d       channels of a head: a multiple of 16 up to 256.
- *  pages * page is at most 2^31 - 1.
+ *  pages * page is at most 2^31 - 1.  Scales are >= 0 or NaN, and a row of
+ *  scale 0 has codes 0, as cs_cache_write leaves them.
  */
 typedef struct {
   int8_t* k;       /* [pages][heads][page][d] */

@@ -170,7 +170,9 @@ int cs_quantise_rows(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int 
 }
 
 size_t cs_linear_q8_workspace_bytes(cs_dtype xt, int64_t rows, int k, int d_out) {
-  if (rows < 1 || rows > kMaxCount || k < 1 || k > CS_MAX_Q8_K || d_out < 1) return 0;
+  if (rows < 1 || rows > kMaxCount || k < 1 || k > CS_MAX_Q8_K || d_out < 1 ||
+      d_out > CS_MAX_Q8_OUT)
+    return 0;
   if (!is_float(xt)) return 0;
   return round_up((size_t)rows * round_up((size_t)k, 16) + (size_t)rows * 4, 256);
 }
@@ -187,6 +189,7 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     return CS_ERR_ARG;
   if (k > CS_MAX_Q8_K || rows > kMaxCount || ldx < k || ldw < k || ldy < d_out)
     return CS_ERR_SHAPE;
+  if (d_out > CS_MAX_Q8_OUT) return CS_ERR_SHAPE;
   const size_t need = cs_linear_q8_workspace_bytes(xt, rows, k, d_out);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -214,10 +217,9 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
   return with_float(yt, [&](auto t) {
     using T = decltype(t);
     if (!al) {
-      const int64_t tiles_t = (rows + 63) / 64;
-      if (tiles_t > 65535) return (int)CS_ERR_SHAPE;
       hipLaunchKernelGGL((cs::linear_q8_any<T>),
-                         dim3((unsigned)((d_out + 63) / 64), (unsigned)tiles_t), dim3(256), 0, s, a);
+                         dim3((unsigned)((rows + 63) / 64), (unsigned)(((int64_t)d_out + 63) / 64)),
+                         dim3(256), 0, s, a);
       return launched();
     }
     auto tiles = [&](int bm, int bn) {
@@ -336,7 +338,7 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
   cs::PagedAttention a{c, q, ldq, hsq, vec, tokens, q_heads, group, batch,
                        cs::make_fastdiv((uint32_t)group), cs::make_fastdiv((uint32_t)c.heads),
                        cs::make_fastdiv((uint32_t)p.tiles), table, table_width, lens, starts, scale,
-                       window, out, p.splits, p.chunk, nullptr, nullptr};
+                       std::min(window, CS_MAX_Q8_LEN), out, p.splits, p.chunk, nullptr, nullptr};
   if (p.splits > 1) {
     a.part_o = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)p.splits * rows * c.d);

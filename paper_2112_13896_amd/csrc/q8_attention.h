@@ -103,11 +103,17 @@ __device__ __forceinline__ bool find_tile(const PagedAttention& a, int tile, int
   return t->row0 >= 0 && t->row0 < t->rows;
 }
 
+// Position of a sequence's new token; those before the sequence's first
+// position see nothing, wherever they are.
+__device__ __forceinline__ int position(const RowTile& t, int token) {
+  return max(t.len - t.n + token, -1);
+}
+
 // Positions [lo, hi) that some row of tokens t0 .. t1 of the tile sees.
 __device__ __forceinline__ void tile_keys(const PagedAttention& a, const RowTile& t, int t0,
                                           int t1, int* lo, int* hi) {
-  const int p0 = t.len - t.n + t0, p1 = t.len - t.n + t1;
-  *hi = max(p1 + 1, 0);
+  const int p0 = position(t, t0), p1 = position(t, t1);
+  *hi = p1 + 1;
   *lo = a.window > 0 ? max(p0 - a.window + 1, 0) : 0;
 }
 
@@ -278,11 +284,10 @@ void attention_few(PagedAttention a) {
   const int rows_end = min(t.rows, t.row0 + 16);
   const int tok0 = (int)fdiv((uint32_t)t.row0, a.by_group);
   const int tok1 = (int)fdiv((uint32_t)(rows_end - 1), a.by_group);
-  const int back = t.len - t.n;                            // position of new token 0
   int lo, hi;
   tile_keys(a, t, tok0, tok1, &lo, &hi);
-  const int pos0 = back + tok0;                            // every row sees up to pos0 ...
-  const int see1 = a.window > 0 ? back + tok1 - a.window + 1 : 0;   // ... from see1 on
+  const int pos0 = position(t, tok0);                      // every row sees up to pos0 ...
+  const int see1 = a.window > 0 ? position(t, tok1) - a.window + 1 : 0;   // ... from see1 on
   // this workgroup's part
   const int j0 = lo / 32 * 32 + split * a.chunk;
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
@@ -291,7 +296,7 @@ void attention_few(PagedAttention a) {
   // the query rows' operand
   const int row = min(t.row0 + r, t.rows - 1);
   const int tok = (int)fdiv((uint32_t)row, a.by_group);
-  const int pos = back + tok;                              // the row sees up to pos
+  const int pos = position(t, tok);                        // the row sees up to pos
   f16x8 q[NP][KS];
   float c;
   {
@@ -498,8 +503,8 @@ void attention_few(PagedAttention a) {
 // codes are turned at the start of a step, beside its first products, and the
 // ones after that are then on their way in registers under all of its
 // arithmetic; one barrier a step.  Two wavefronts bring the values, two the
-// keys, a block of 16 keys (a piece of one page, so its address is scalar) at
-// a time.  W <= DT: channels that are computed, d rounded up to 32.
+// keys, by blocks of 16 (a piece of one page, so their addresses are scalar).
+// W <= DT: channels that are computed, d rounded up to 32.
 // Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y =
 // 0..3) of row r.  So a lane's eight weights of 16 keys are those at 4 h ..
 // and 8 + 4 h .., and the values' chunk g = 2 s + h of a channel holds just
@@ -540,15 +545,14 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   const int row_c = min(row, t.rows - 1);
   const int tok = (int)fdiv((uint32_t)row_c, a.by_group);
   const int qh = head * a.group + row_c - tok * a.group;
-  const int back = t.len - t.n;                            // position of new token 0
   int lo, hi;
   tile_keys(a, t, (int)fdiv((uint32_t)t.row0, a.by_group),
             (int)fdiv((uint32_t)(rows_end - 1), a.by_group), &lo, &hi);
-  const int pos = back + tok, see = a.window > 0 ? pos - a.window + 1 : 0;
+  const int pos = position(t, tok), see = a.window > 0 ? pos - a.window + 1 : 0;
   // the wavefront's rows all see up to pos0 and from see1 on
   const int w0 = min(t.row0 + wave * 32, t.rows - 1), w1 = min(w0 + 31, t.rows - 1);
-  const int pos0 = back + (int)fdiv((uint32_t)w0, a.by_group);
-  const int pos1 = back + (int)fdiv((uint32_t)w1, a.by_group);
+  const int pos0 = position(t, (int)fdiv((uint32_t)w0, a.by_group));
+  const int pos1 = position(t, (int)fdiv((uint32_t)w1, a.by_group));
   const int see1 = a.window > 0 ? pos1 - a.window + 1 : 0;
   const int j0 = lo / 64 * 64 + split * a.chunk;
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
@@ -706,7 +710,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[x][i] = 0.0f;
   float m = kNegInf, l = 0.0f;
-  // the chunks that a lane reads: of key r (its even and odd chunks, four by four), of channel r
+  // the chunks that a lane reads: of key r, of channel r
   constexpr int KA = DT == 64 ? 4 : 8;                     // columns of chunks that turn together
   int k_at[KA], v_at[4];
 #pragma unroll

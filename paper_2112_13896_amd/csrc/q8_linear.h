@@ -68,8 +68,8 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
   constexpr int kLd = 64 + 16;                             // a row's bytes in LDS, padded
   __shared__ __align__(16) int8_t lx[64 * kLd], lw[64 * kLd];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int64_t t0 = (int64_t)blockIdx.y * 64;
-  const int n0 = blockIdx.x * 64;
+  const int64_t t0 = (int64_t)blockIdx.x * 64;
+  const int n0 = blockIdx.y * 64;
   const int sr = tid / 4, sc = tid % 4 * 16;               // the piece this thread stages
   const int64_t xt = min(t0 + sr, a.rows - 1);
   const int wn = min(n0 + sr, a.d_out - 1);

@@ -959,7 +959,7 @@ def linear_q8(x: torch.Tensor, w: torch.Tensor, sw: torch.Tensor, sx: torch.Tens
     return out
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedCache:
     """Keys and values of many sequences in 8 bits (cs_q8_cache): codes int8
     [pages][heads][page][d], scales float32 [pages][heads][page]."""
@@ -979,10 +979,11 @@ class PagedCache:
                 raise ValueError(f"{name} must be {dt} {list(shape)}")
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
-        self.pages, self.heads, self.page, self.d = self.k.shape
-        self._c = _lib.Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
-                               self.v_scale.data_ptr(), *self.k.shape)
-        self._ref = ctypes.byref(self._c)
+        c = _lib.Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                         self.v_scale.data_ptr(), *self.k.shape)
+        for name, value in (("_c", c), ("_ref", ctypes.byref(c)),
+                            *zip(("pages", "heads", "page", "d"), self.k.shape)):
+            object.__setattr__(self, name, value)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page: int, d: int, device="cuda") -> "PagedCache":

@@ -30,3 +30,14 @@ def test_nan_in_one_part():
     pg, off = divmod(s.slot(0, 12345), 64)
     s.ks[pg, 0, off] = float("nan")
     s.check(ops.paged_attention(*s.args()))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_windows_past_every_length(new):
+    """A window up to the largest int is no window, also for tokens that see nothing."""
+    s = Sequences(5, [(new, 70), (new, max(1, new - 30)), (new, 0)], 2, 2, 64, 16, torch.float16)
+    args = s.args()
+    want = ops.paged_attention(*args)
+    s.check(want)
+    for window in (71, 2 ** 30, 2 ** 31 - 1):
+        assert torch.equal(ops.paged_attention(*args, window=window), want)

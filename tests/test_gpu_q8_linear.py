@@ -138,3 +138,38 @@ def test_other_stream_and_graph():
             torch.cuda.synchronize()
             assert torch.equal(out, ref)
             assert torch.equal(ops.linear_q8(x, w, sw), ref)
+
+
+@pytest.mark.parametrize("m,k,n", [(1, 8192, 40), (1, 16384, 17), (2, 8192, 33), (3, 2731, 50),
+                                   (5, 3276, 16), (16, 1024, 64), (16, 1025, 64), (20, 8192, 2048),
+                                   (20, 900, 2064), (64, 8192, 128), (130, 8200, 70)])
+def test_few_and_many_tokens_at_the_rules_edges(m, k, n):
+    """Sizes on both sides of what is quantised in the product's launch, and of the tiles."""
+    r = np.random.default_rng(m + k + n)
+    x = rand(r, (m, k), torch.bfloat16)
+    w = rand(r, (n, k), torch.float32, 0.05)
+    qw, sw = ops.quantise_rows(w.cuda())
+    qx, sx = o8.quantise(f64(x))
+    y = ops.linear_q8(x.cuda(), qw, sw)
+    _check(y, qx, sx, qw.cpu().numpy(), sw.cpu().numpy(), None, torch.bfloat16)
+    shifted = torch.zeros((m, k + 3), dtype=torch.bfloat16).cuda()[:, 3:]
+    shifted.copy_(x)
+    assert torch.equal(ops.linear_q8(shifted, qw, sw), y)
+
+
+def test_last_rows_end_with_their_storage():
+    """k that is no multiple of 16 in storage that ends with the last code."""
+    r = np.random.default_rng(8)
+    for m, k, n in ((3, 100, 20), (70, 1500, 65), (300, 129, 300)):
+        qx, qw = _codes(r, (m, k)), _codes(r, (n, k))
+        ld = (k + 15) // 16 * 16
+
+        def tight(a):
+            buf = torch.full(((a.shape[0] - 1) * ld + k,), 99, dtype=torch.int8)
+            view = buf.as_strided(a.shape, (ld, 1))
+            view.copy_(torch.from_numpy(a))
+            return buf.cuda().as_strided(a.shape, (ld, 1))
+        sx, sw = np.ones(m, np.float32), np.ones(n, np.float32)
+        y = ops.linear_q8(tight(qx), tight(qw), torch.from_numpy(sw).cuda(),
+                          sx=torch.from_numpy(sx).cuda())
+        _check(y, qx, sx, qw, sw, None, torch.float32)
