@@ -35,8 +35,9 @@
  *  - Integer path: int8 activations and weights, int32 accumulation and bias
  *    (Section 4: weights and activations quantised to 8 bits).  Float path:
  *    fp32 throughout (CS_F16 and CS_BF16 are types of the 8-bit attention
- *    operators alone; every other call refuses them).  Integer sums wrap modulo 2^32 on overflow (the
- *    configurations used stay below 2^31 by a wide margin).
+ *    operators alone; every other call refuses them).  Integer sums wrap
+ *    modulo 2^32 on overflow (the configurations used stay below 2^31 by a
+ *    wide margin).
  */
 #ifndef CS_H_
 #define CS_H_
@@ -764,7 +765,8 @@ int cs_quantise_rows(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int 
  *  Rows of x and w that start on 16 bytes are staged 16 bytes at a time; pad
  *  the row stride of an odd k to a multiple of 16 to have that.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (a stride below its row,
- *  k > CS_MAX_Q8_K, d_out > CS_MAX_Q8_OUT, more than 2^31 - 1 rows), CS_ERR_WORKSPACE, CS_ERR_DEVICE.
+ *  k > CS_MAX_Q8_K, d_out > CS_MAX_Q8_OUT, more than 2^31 - 1 rows),
+ *  CS_ERR_WORKSPACE, CS_ERR_DEVICE.
  */
 int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64_t rows, int k,
                  const int8_t* w, int64_t ldw, const float* sw, int d_out, const float* bias,

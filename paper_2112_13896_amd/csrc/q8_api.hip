@@ -37,7 +37,9 @@ template <typename T, int WPR>
 int quantise_launch(const T* x, int64_t ldx, int64_t rows, int c, int8_t* q, int64_t ldq,
                     float* scale, hipStream_t s) {
   const dim3 grid((unsigned)((rows * WPR + 3) / 4)), block(256);
-  auto starts_on = [&](size_t n) { return aligned(x, n) && (rows == 1 || ldx * sizeof(T) % n == 0); };
+  auto starts_on = [&](size_t n) {
+    return aligned(x, n) && (rows == 1 || ldx * sizeof(T) % n == 0);
+  };
   if (starts_on(16))
     hipLaunchKernelGGL((cs::quantise_rows<T, 16, WPR>), grid, block, 0, s, x, ldx, rows, c, q,
                        ldq, scale);
@@ -78,10 +80,10 @@ int linear_tiles(const cs::Q8Linear& a, hipStream_t s) {
 }
 
 // Elements of up to 16 tokens that every workgroup of the product quantises itself, instead of a
-// launch that does it once (a recorded graph of the call, bf16, k x d_out as given): 1 x 2,048 4.8
-// against 7.8 us, 1 x 16,384 19.5 | 26.0, 4 x 4,096 9.3 | 9.4, 8 x 2,048 7.4 | 8.4, 16 x 1,024 7.5 |
-// 6.8; beyond, 8 x 4,096 16.2 | 12.6, 16 x 2,048 10.9 | 8.9.  Calls that are not recorded save
-// 2.7 us of the host's time on top.
+// launch that does it once (recorded in a graph, bf16, tokens x k): 1 x 2,048 4.8 us against 7.8,
+// 1 x 16,384 19.5 | 26.0, 4 x 4,096 9.3 | 9.4, 8 x 2,048 7.4 | 8.4, 16 x 1,024 7.5 | 6.8; beyond,
+// 8 x 4,096 16.2 | 12.6, 16 x 2,048 10.9 | 8.9.  Calls that are not recorded save 2.7 us of the
+// host's time on top.
 constexpr int64_t kFusedElements = 16384;
 
 template <typename T, typename XT, int RT>
@@ -231,7 +233,8 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     if (rows <= 16) return linear_few<T, int8_t, 1>(a, s);
     if (rows <= 32 && d_out <= 2048) return linear_few<T, int8_t, 2>(a, s);
     // the largest tile of which there are enough to keep most compute units busy: 2,048 x 4,096 x
-    // 4,096 40 us in 128 x 128, 59 in 64 x 64; 8,192 x 4,096 x 8,192 245 in 256 x 256, 290 in 128 x 128
+    // 4,096 40 us in 128 x 128, 59 in 64 x 64; 8,192 x 4,096 x 8,192 with its tokens quantised 321
+    // in 256 x 256, 361 in 128 x 128 (before both stored whole rows; 268 now)
     if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64, 2>(a, s);
     if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64, 2>(a, s);
     return linear_tiles<T, 64, 64, 32, 32, 4>(a, s);

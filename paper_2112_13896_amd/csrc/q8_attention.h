@@ -261,13 +261,17 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 // heads, a few drafted tokens) to a workgroup of four wavefronts, the keys
 // read once.  A wavefront takes 32 keys a step, every fourth step of the
 // workgroup's part of the key axis: keys and values go from memory to
-// registers (no LDS) and are turned to halves there.  What hides the loads is
-// other wavefronts: registers for a step in flight ahead, or for a second
-// tile of rows, would halve their number (two long sequences of 20 rows a
-// head: 70 us with two tiles that both read the keys, the second out of the
-// L2, 88 us with one of 32 rows).  Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of
-// 16, channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels
-// r DT/16 .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
+// registers (no LDS) and are turned to halves there.
+// Bound by memory: 64 sequences of up to 8,192 keys, 32 query and 8 cache
+// heads of 128 (623 MB), take 135 us and 6.7 to join their parts, 4.6 TB/s of
+// the 5.1 of a large copy; the vector units are busy a third of the time.
+// What hides the loads is other wavefronts: registers for a step in flight
+// ahead (157 us), or for a second tile of rows, would halve their number (two
+// long sequences of 20 rows a head: 70 us with two tiles that both read the
+// keys, the second out of the L2, 88 us with one of 32 rows).
+// Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of 16,
+// channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels r DT/16
+// .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
 template <typename T, int DT>
 __global__ __launch_bounds__(256, DT == 256 ? 2 : DT == 128 && sizeof(T) == 4 ? 3 : 4)
 void attention_few(PagedAttention a) {
@@ -499,12 +503,21 @@ void attention_few(PagedAttention a) {
 // 32 rows each, 64 keys a step.  A step's codes are turned to halves once for
 // all four: keys [64][DT], values transposed [DT][64], both in 16-byte chunks
 // whose place in a row is permuted (xor) so that the lanes that read a column
-// of chunks together meet all banks; two buffers, the next step's
-// codes are turned at the start of a step, beside its first products, and the
-// ones after that are then on their way in registers under all of its
-// arithmetic; one barrier a step.  Two wavefronts bring the values, two the
-// keys, by blocks of 16 (a piece of one page, so their addresses are scalar).
-// W <= DT: channels that are computed, d rounded up to 32.
+// of chunks together meet all banks; two buffers.  The next step's codes are
+// turned at the start of a step, beside its first products, and the ones after
+// that are then on their way in registers under all of its arithmetic; one
+// barrier a step.  Two wavefronts bring the values, two the keys, by blocks of
+// 16 (a piece of one page, so their addresses are scalar).  W <= DT: channels
+// that are computed, d rounded up to 32.
+// Four prompts of 2,048 after up to 4,096 positions, 32 query and 8 cache heads
+// of 128, bf16 (409 GFLOP): 545-590 us, 700-750 TFLOP/s.  Bound by each
+// wavefront's own stream of some 700 instructions a step: the registers allow
+// two wavefronts a SIMD, and with matrix units busy for 30 % and vector units
+// for 50 % of the time neither is full.  Measured by leaving work out: loads 18 %
+// of the time, the first product 20, the second 15, exponentials 7, turning
+// codes 4.  Slower: 32 keys a step (720 us: twice the barriers; with three
+// wavefronts a SIMD registers spill, 808), the next half step's logits among
+// this one's exponentials (613: spills).  fp32 queries take twice the products.
 // Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y =
 // 0..3) of row r.  So a lane's eight weights of 16 keys are those at 4 h ..
 // and 8 + 4 h .., and the values' chunk g = 2 s + h of a channel holds just
@@ -609,7 +622,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   constexpr int KB = DT / 64;                              // keys: loads a block, 16 bytes a lane
   constexpr int PR = DT / 16;                              // lanes to a key
   const int k_key = lane / PR, k_ch = lane % PR * 16;      // + 64 / PR keys a load
-  // values: 32 lanes to a block, 16 to each half of its keys (chunk of LDS), DT / 16 channels a lane
+  // values: 32 lanes to a block, 16 to each half of its keys (a chunk of LDS), DT / 16 channels each
   constexpr int VD = DT / 64;                              // dwords a lane and value row
   const int v_ch = lane % 16 * 4 * VD;
   // byte of a block that this lane loads first (channels past d: any)

@@ -62,7 +62,8 @@ __device__ __forceinline__ i32x4 codes16_any(const int8_t* row, int e, int k) {
 // linear_q8_any: rows that start anywhere.  A 64 x 64 tile of y to a
 // workgroup of four wavefronts, 32 x 32 each, 64 codes of k a step through
 // registers and LDS, 16 bytes a thread and operand put together from single
-// ones.
+// ones, which is what bounds it (the simplest kernel that is right for any row;
+// padding rows to 16 bytes, as quantise_rows does, avoids it).
 template <typename T>
 __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
   constexpr int kLd = 64 + 16;                             // a row's bytes in LDS, padded
@@ -114,7 +115,15 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
 // through registers, zeros after k.
 // The products are w times x: a lane then holds four neighbouring channels of
 // one token, which go through LDS (free by then), 32 tokens of a wavefront at a
-// time, to be stored as whole rows of its tile, 16 bytes a lane.
+// time, to be stored as whole rows of its tile, 16 bytes a lane (with two-byte
+// stores and each row's scale loaded beside them, a tile's end took as long as
+// a third of its products: 315 us for the case below).
+// 256 x 256 with eight wavefronts, two buffers (128 KB): 8,192 x 4,096 x 8,192
+// in 250-280 us, 2.0-2.2 POP/s (a library int8 product of that size: 2.5).  Matrix
+// instructions issue half of the time; of a step of 128 codes a fifth is the
+// wait for its loads, and a tile's start and end, which nothing overlaps, are a
+// fifth of the whole.  64 x 64, four wavefronts, four buffers: 777 x 1,500 x 1,001 in
+// 10 us, 0.3 us a step, which is the latency of twelve dependent steps.
 struct TileOrder {
   uint32_t tiles_m, tiles_n, per_xcd, more;                // tiles / 8, tiles % 8
 };
@@ -175,7 +184,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   const int8_t* xb = a.x + t0 * a.ldx;
   const int8_t* wb = a.w + (int64_t)n0 * a.ldw;
   const int xrows = (int)min<int64_t>(BM, a.rows - t0), wrows = min(BN, a.d_out - n0);
-  // the 16-byte chunk `piece` of a buffer: row piece / 8, the row's chunk (piece % 8) ^ chunk_turn(row)
+  // the 16-byte chunk `piece` of a buffer: row piece / 8, its chunk (piece % 8) ^ chunk_turn(row)
   uint32_t xo[PX], wo[PW];
 #pragma unroll
   for (int p = 0; p < PX; ++p) {
@@ -298,7 +307,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   constexpr int kShare = THREADS / 64 / 4;                 // wavefronts to a buffer
   static_assert(kShare * 32 * kRow <= BM * 128 && kShare * 32 * kRow <= BN * 128, "");
   const int buf = wave / kShare;
-  int8_t* out = (buf == 0 ? lx0 : buf == 1 ? lx1 : buf == 2 ? lw0 : lw1) + wave % kShare * 32 * kRow;
+  int8_t* out =
+      (buf == 0 ? lx0 : buf == 1 ? lx1 : buf == 2 ? lw0 : lw1) + wave % kShare * 32 * kRow;
   constexpr int E = 16 / sizeof(T), kPieces = WN / E;      // elements of 16 bytes, pieces of a row
   typedef T t4 __attribute__((ext_vector_type(4)));
   const int nvalid = a.d_out - n0 - nr;                    // channels of the wavefront's tile
@@ -347,6 +357,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
 // The wavefronts' int32 sums meet in LDS.  XT int8_t: tokens in codes.  A
 // float XT: every workgroup quantises the tokens itself, into LDS, while its
 // first loads of w are under way; that is one launch instead of two.
+// Bound by latency where w is small (1 x 512 x 512, quantised here: 4.4 us) and by
+// reading w where it is not (1 x 8,192 x 8,192: 15.6 us, 4.3 TB/s).
 constexpr int kFewSteps = 4;
 
 template <typename T, typename XT, int RT, int NW>

@@ -52,14 +52,15 @@ def test_linear_refusals(L):
                dict(sw=P + 2), dict(bias=P + 3), dict(sx=P + 2)):
         assert call(**kw) == CS_ERR_ARG, kw
     for kw in (dict(ldx=63), dict(ldw=63), dict(ldy=31), dict(rows=1 << 31),
-               dict(k=131073, ldx=131073, ldw=131073)):
+               dict(k=131073, ldx=131073, ldw=131073), dict(d_out=(1 << 22) + 1, ldy=1 << 23)):
         assert call(**kw) == CS_ERR_SHAPE, kw
     need = L.cs_linear_q8_workspace_bytes(CS_F32, 4, 64, 32)
     assert need >= 4 * 64 + 4 * 4
     for kw in (dict(ws=0), dict(n=need - 1), dict(ws=P + 8)):
         assert call(xt=CS_F32, sx=0, **kw) == CS_ERR_WORKSPACE, kw
     assert call(rows=0, x=0, w=0) == CS_OK
-    for args in ((CS_F32, 0, 64, 32), (CS_F32, 4, 0, 32), (CS_F32, 4, 131073, 32), (CS_I32, 4, 4, 4)):
+    for args in ((CS_F32, 0, 64, 32), (CS_F32, 4, 0, 32), (CS_F32, 4, 131073, 32), (CS_I32, 4, 4, 4),
+                 (CS_F32, 4, 64, (1 << 22) + 1)):
         assert L.cs_linear_q8_workspace_bytes(*args) == 0
 
 
