@@ -124,6 +124,7 @@ struct AttentionPlan {
   int per;             // rows of a workgroup: 128 (attention_many) or 16 (attention_few)
   int64_t tiles;       // numbers of row tiles (find_tile)
   int splits, chunk;
+  int waves;           // wavefronts of a workgroup (attention_few)
 };
 
 AttentionPlan attention_plan(const cs::CacheView& c, cs_dtype qt, int tokens, int q_heads,
@@ -150,6 +151,12 @@ AttentionPlan attention_plan(const cs::CacheView& c, cs_dtype qt, int tokens, in
   if (splits < 1 || len <= 1024) splits = 1;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
+  // a workgroup or fewer a compute unit, keys whole: eight wavefronts halve its chain of steps
+  // (four | eight, one new token, 8 cache heads of 128: 1 x 700 keys 11.1 | 9.7 us, 8 x 900 13.5 |
+  // 11.6, fp32 32 x 1,000 26.1 | 18.4, heads of 256 31.9 | 26.8; but bf16 32 x 1,000 20.7 | 21.7,
+  // 96 x 200 14.1 | 17.6)
+  const int64_t most = qt == CS_F32 || c.d > 128 ? 256 : 128;
+  p.waves = p.splits == 1 && items <= most ? 8 : 4;
   return p;
 }
 
@@ -353,7 +360,10 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
     const dim3 grid((unsigned)blocks), block(256);
     auto few = [&](auto dt) {
       constexpr int DT = decltype(dt)::value;
-      hipLaunchKernelGGL((cs::attention_few<T, DT>), grid, block, 0, s, a);
+      if (p.waves == 8)
+        hipLaunchKernelGGL((cs::attention_few<T, DT, 8>), grid, dim3(512), 0, s, a);
+      else
+        hipLaunchKernelGGL((cs::attention_few<T, DT, 4>), grid, dim3(256), 0, s, a);
     };
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;

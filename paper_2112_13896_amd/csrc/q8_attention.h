@@ -258,8 +258,8 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 
 // ---------------------------------------------------------------- few rows
 // attention_few: up to 16 rows of a cache head (a decoding token's query
-// heads, a few drafted tokens) to a workgroup of four wavefronts, the keys
-// read once.  A wavefront takes 32 keys a step, every fourth step of the
+// heads, a few drafted tokens) to a workgroup of NW wavefronts, the keys read
+// once.  A wavefront takes 32 keys a step, every NW-th step of the
 // workgroup's part of the key axis: keys and values go from memory to
 // registers (no LDS) and are turned to halves there.
 // Bound by memory: 64 sequences of up to 8,192 keys, 32 query and 8 cache
@@ -272,13 +272,13 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 // Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of 16,
 // channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels r DT/16
 // .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
-template <typename T, int DT>
-__global__ __launch_bounds__(256, DT == 256 ? 2 : DT == 128 && sizeof(T) == 4 ? 3 : 4)
+template <typename T, int DT, int NW>
+__global__ __launch_bounds__(64 * NW, DT == 256 ? 2 : DT == 128 && sizeof(T) == 4 ? 3 : 4)
 void attention_few(PagedAttention a) {
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;
   constexpr int KS = DT / 32, CT = DT / 16;
-  __shared__ float l_o[4][16][DT + 4];
-  __shared__ float l_m[4][16], l_l[4][16];
+  __shared__ float l_o[NW][16][DT + 4];
+  __shared__ float l_m[NW][16], l_l[NW][16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, h = lane / 16, d = a.c.d;
   int head, tile, split;
@@ -349,7 +349,7 @@ void attention_few(PagedAttention a) {
   for (int x = 0; x < CT; ++x) o[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kNegInf, l = 0.0f;
   if (wave < steps) pages(j0 + 32 * wave);
-  for (int step = wave; step < steps; step += 4) {
+  for (int step = wave; step < steps; step += NW) {
     const int j = j0 + 32 * step;
     u32x4 kr[2][DT / 64];
     uint32_t vr[DT / 64][8];
@@ -382,7 +382,7 @@ void attention_few(PagedAttention a) {
         for (int x = 0; x < DT / 64; ++x) vr[x][4 * u + i] = w[x];
       }
     }
-    if (step + 4 < steps) pages(j + 128);
+    if (step + NW < steps) pages(j + 32 * NW);
     f32x4 s[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -450,7 +450,7 @@ void attention_few(PagedAttention a) {
     }
   }
 
-  // the four wavefronts' sums, joined in order
+  // the wavefronts' sums, joined in order
   l = reduce_x16_x32(l, FAdd{});
   if (h == 0) {
     l_m[wave][r] = m;
@@ -465,14 +465,14 @@ void attention_few(PagedAttention a) {
   __syncthreads();
   // 16 lanes to a row
   const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16;
-  if (t.row0 + rr >= rows_end) return;
+  if (rr >= 16 || t.row0 + rr >= rows_end) return;
   float top = kNegInf;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, l_m[w][rr]);
+  for (int w = 0; w < NW; ++w) top = fmaxf(top, l_m[w][rr]);
   const float base = top == kNegInf ? 0.0f : top;
-  float f[4], sum = 0.0f;
+  float f[NW], sum = 0.0f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     // a wavefront without a key has sums of 0; one with NaN alone among its keys m = -inf
     f[w] = exp2_fast(l_m[w][rr] - base);
     sum = fmaf(l_l[w][rr], f[w], sum);
@@ -490,7 +490,7 @@ void attention_few(PagedAttention a) {
     for (int i = 0; i < 8; ++i) {
       float s = 0.0f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
+      for (int w = 0; w < NW; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
       v[i] = a.splits > 1 ? s : s * inv;
     }
     if (a.splits > 1) store8(a.part_o + po * d + x, v);
