@@ -622,7 +622,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   constexpr int KB = DT / 64;                              // keys: loads a block, 16 bytes a lane
   constexpr int PR = DT / 16;                              // lanes to a key
   const int k_key = lane / PR, k_ch = lane % PR * 16;      // + 64 / PR keys a load
-  // values: 32 lanes to a block, 16 to each half of its keys (a chunk of LDS), DT / 16 channels each
+  // values: 32 lanes to a block, 16 to each half of its keys (a chunk of LDS), DT / 16 channels
   constexpr int VD = DT / 64;                              // dwords a lane and value row
   const int v_ch = lane % 16 * 4 * VD;
   // byte of a block that this lane loads first (channels past d: any)
