@@ -858,9 +858,23 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
                        void* stream);
 
 /* cs_paged_attention_workspace_bytes - workspace of cs_paged_attention (0 for
- * invalid arguments too).  Host only. */
+ * invalid arguments too): enough for any window, and for the same call with a
+ * smaller max_len or table_width.  Host only. */
 size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt, int tokens,
                                           int q_heads, int batch, int table_width, int max_len);
+
+/*
+ * cs_paged_attention_plan - how cs_paged_attention would run these sizes.  Host
+ * only; no HIP call.  For tests and tuning.
+ *
+ *  info    host int64[6] out: [0] rows (token, query head) of a workgroup, [1]
+ *          parts of the key axis, [2] positions of a part (the last takes what
+ *          is left), [3] wavefronts of a workgroup, [4] workgroups, [5] bytes of
+ *          ws that the parts take.
+ *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE as cs_paged_attention.
+ */
+int cs_paged_attention_plan(const cs_q8_cache* cache, cs_dtype qt, int tokens, int q_heads,
+                            int batch, int table_width, int max_len, int window, int64_t* info);
 
 /*
  * cs_product_count - the number of weight x activation products the

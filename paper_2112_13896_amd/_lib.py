@@ -103,6 +103,7 @@ SIGNATURES = {
     "cs_paged_attention": (_i, [_cache, _i, _vp, _i64, _i64, _i, _i, _i, _vp, _i, _vp, _vp, _i,
                                 _c.c_float, _i, _vp, _vp, _sz, _vp]),
     "cs_paged_attention_workspace_bytes": (_sz, [_cache, _i, _i, _i, _i, _i, _i]),
+    "cs_paged_attention_plan": (_i, [_cache, _i, _i, _i, _i, _i, _i, _i, _c.POINTER(_i64)]),
     "cs_product_count": (_i, [_c.POINTER(_c.c_ulonglong), _i]),
     "cs_phase_stamps": (_i, [_c.POINTER(_c.c_ulonglong), _i, _i, _c.POINTER(_c.c_int)]),
     "cs_status_str": (_c.c_char_p, [_i]),

@@ -125,7 +125,8 @@ void with_width(int d, F f) {
 struct AttentionPlan {
   int per;             // rows of a workgroup: 128 (attention_many) or 16 (attention_few)
   int64_t tiles;       // numbers of row tiles (find_tile)
-  int splits, chunk;
+  int splits, chunk;   // parts of the key axis, positions of a part
+  int most;            // parts at most, of this axis under any window and of any shorter one
   int waves;           // wavefronts of a workgroup (attention_few)
 };
 
@@ -151,6 +152,10 @@ AttentionPlan attention_plan(const cs::CacheView& c, cs_dtype qt, int tokens, in
   const int wgs = p.per == 128 ? 1 : 2 * (c.d > 128 ? 2 : c.d > 64 && qt == CS_F32 ? 3 : 4);
   int64_t splits = std::min<int64_t>({256 * wgs / items, len / 256, cs::kMaxSplits});
   if (splits < 1 || len <= 1024) splits = 1;
+  // Parts are whole steps, so a part is rounded up and there may be fewer of them than `splits`.
+  // How many fewer depends on the length (64 at most: 16,384 positions are 64, one more makes 43);
+  // `splits` itself never grows as the axis gets shorter.
+  p.most = (int)splits;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
   // a workgroup or fewer a compute unit, keys whole: eight wavefronts halve its chain of steps
@@ -162,8 +167,13 @@ AttentionPlan attention_plan(const cs::CacheView& c, cs_dtype qt, int tokens, in
   return p;
 }
 
-size_t attention_part_bytes(const AttentionPlan& p, int64_t rows, int d) {
-  return p.splits > 1 ? (size_t)p.splits * rows * ((size_t)d * 4 + 8) : 0;
+size_t attention_part_bytes(int64_t parts, int64_t rows, int d) {
+  return parts > 1 ? (size_t)parts * rows * ((size_t)d * 4 + 8) : 0;
+}
+
+bool attention_fits(const cs::CacheView& c, int tokens, int q_heads, int table_width) {
+  return q_heads % c.heads == 0 && c.heads <= 65535 && (int64_t)tokens * q_heads <= kMaxCount &&
+         ((int64_t)table_width << c.page_log) <= CS_MAX_Q8_LEN;
 }
 
 }  // namespace
@@ -313,9 +323,30 @@ size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt,
   if (!is_float(qt) || cache_view(cache, &c) != CS_OK) return 0;
   if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0) return 0;
   if (q_heads % c.heads != 0) return 0;
-  // the split without a window is the finest: it serves any window
+  // the whole axis: a window or a shorter one has at most as many parts
   const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len, 0);
-  return attention_part_bytes(p, (int64_t)tokens * q_heads, c.d);
+  return attention_part_bytes(p.most, (int64_t)tokens * q_heads, c.d);
+}
+
+int cs_paged_attention_plan(const cs_q8_cache* cache, cs_dtype qt, int tokens, int q_heads,
+                            int batch, int table_width, int max_len, int window, int64_t* info) {
+  if (!info) return CS_ERR_ARG;
+  if (!is_float(qt)) return CS_ERR_DTYPE;
+  cs::CacheView c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0 || window < 0)
+    return CS_ERR_ARG;
+  if (!attention_fits(c, tokens, q_heads, table_width)) return CS_ERR_SHAPE;
+  const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len,
+                                         window);
+  info[0] = p.per;
+  info[1] = p.splits;
+  info[2] = p.chunk;
+  info[3] = p.per == 16 ? p.waves : 4;
+  info[4] = p.tiles * c.heads * p.splits;
+  info[5] = (int64_t)attention_part_bytes(p.splits, (int64_t)tokens * q_heads, c.d);
+  return CS_OK;
 }
 
 int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
@@ -334,16 +365,16 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
   if (!q || !table || !lens || !starts || !out || !aligned(q, float_size(qt)) ||
       !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4))
     return CS_ERR_ARG;
-  if (q_heads % c.heads != 0 || ldq < 0 || hsq < c.d) return CS_ERR_SHAPE;
-  if ((int64_t)tokens * q_heads > kMaxCount || c.heads > 65535) return CS_ERR_SHAPE;
-  if (((int64_t)table_width << c.page_log) > CS_MAX_Q8_LEN) return CS_ERR_SHAPE;
-  const size_t need = cs_paged_attention_workspace_bytes(cache, qt, tokens, q_heads, batch,
-                                                         table_width, max_len);
-  if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
+  if (ldq < 0 || hsq < c.d || !attention_fits(c, tokens, q_heads, table_width))
+    return CS_ERR_SHAPE;
   const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len,
                                           window);
   const int group = q_heads / c.heads;
   const int64_t rows = (int64_t)tokens * q_heads;
+  const size_t need = std::max(cs_paged_attention_workspace_bytes(cache, qt, tokens, q_heads, batch,
+                                                                  table_width, max_len),
+                               attention_part_bytes(p.splits, rows, c.d));
+  if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int e = (int)float_size(qt);
   const bool vec = aligned(q, 16) && (tokens == 1 || ldq * e % 16 == 0) && hsq * e % 16 == 0;

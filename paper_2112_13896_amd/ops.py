@@ -1045,6 +1045,19 @@ def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.T
     return torch.empty((int(n),), dtype=torch.uint8, device=q.device)
 
 
+def paged_attention_plan(dtype: torch.dtype, heads: int, page: int, d: int, tokens: int,
+                         q_heads: int, batch: int, table_width: int, max_len: int | None = None,
+                         window: int = 0) -> dict:
+    """How paged_attention runs these sizes (host only): cs_paged_attention_plan."""
+    # the cache's arrays are not touched; any aligned address stands for them
+    cache = _lib.Q8Cache(16, 16, 16, 16, 1, heads, page, d)
+    info = (ctypes.c_int64 * 6)()
+    check("cs_paged_attention_plan", lib().cs_paged_attention_plan(
+        ctypes.byref(cache), _float_dt(dtype), tokens, q_heads, batch, table_width,
+        0 if max_len is None else int(max_len), window, info))
+    return dict(zip(("rows", "parts", "part", "wavefronts", "workgroups", "bytes"), info))
+
+
 def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, lens: torch.Tensor,
                     starts: torch.Tensor, *, scale: float | None = None, window: int = 0,
                     max_len: int | None = None, ws: torch.Tensor | None = None,
