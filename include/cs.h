@@ -784,6 +784,9 @@ size_t cs_linear_q8_workspace_bytes(cs_dtype xt, int64_t rows, int k, int d_out)
  *  d       channels of a head: a multiple of 16 up to 256.
  *  pages * page is at most 2^31 - 1.  Scales are >= 0 or NaN, and a row of
  *  scale 0 has codes 0, as cs_cache_write leaves them.
+ *  Attention takes a value scale between 0 and 2^-122 (values below 2.4e-35)
+ *  as 2^-122, and leaves out of a row what weighs less than 2^-138 of its
+ *  largest part (weight times value scale).
  */
 typedef struct {
   int8_t* k;       /* [pages][heads][page][d] */

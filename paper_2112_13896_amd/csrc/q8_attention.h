@@ -25,6 +25,8 @@
 //    takes no precision from the others.  m follows the maximum only when that
 //    is more than 4 (2^2) above it: halves have the room, and the sums so far
 //    are rescaled rarely.
+//  - Over values below 1e-21 or so 1 / sv could take the denominator past 32-bit
+//    floats.  A row whose denominator gets large holds it times 2^-60 (SumUnit).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -202,15 +204,20 @@ __device__ __forceinline__ RowNorm row_norm(float amax, float scale) {
 
 // How a token's values enter: sv = a 2^E.  Where all of a token's values are
 // zero, so are its codes, and any scale does that leaves the others room.
+// Scales below kLeast stand for kLeast, so that there is a 1 / sv.
+constexpr float kLeast = 0x1p-122f;
 struct ValueScale {
   float e, a, r;                                           // E, a, 1 / sv
 };
+__device__ __forceinline__ float held_scale(float sv) {    // NaN stays
+  return sv == 0.0f ? 0x1p-60f : sv < kLeast ? kLeast : sv;
+}
 __device__ __forceinline__ ValueScale value_scale(float sv) {
+  sv = held_scale(sv);
   ValueScale v;
-  if (sv == 0.0f) sv = 0x1p-60f;
   const int ex = max(__builtin_amdgcn_frexp_expf(sv) - 1, -120);
   v.e = (float)ex;
-  v.a = ldexpf(sv, -ex);                                   // NaN stays
+  v.a = ldexpf(sv, -ex);
   v.r = ldexpf(__builtin_amdgcn_rcpf(v.a), -ex);
   return v;
 }
@@ -231,6 +238,35 @@ __device__ __forceinline__ float add_weights(float l, const float (&w)[8], const
     l = fmaf(t, r[i], l);
   }
   return l;
+}
+
+// The unit that a row's denominator l is held in, 1 or 2^-60, and whether a row
+// of the wavefront has the latter.
+constexpr float kUnit = 0x1p-60f, kLarge = 0x1p90f;
+struct SumUnit {
+  float g = 1.0f;
+  bool any = false;
+};
+
+// A lane's l in the unit that suits its row and what a step adds to it, p (in
+// units of 1; it may be infinite).  `most`: the maximum over the row's lanes.
+template <typename Most>
+__device__ __forceinline__ float fit_unit(SumUnit& u, float l, float p, Most most) {
+  const float row_p = most(p), row_l = most(l);            // (while all lanes are there)
+  const bool large = row_p > kLarge || (u.g != 1.0f && row_l > kLarge * kUnit);
+  const float g = large ? kUnit : 1.0f;
+  if (g != u.g) l *= large ? kUnit : 1.0f / kUnit;
+  u.g = g;
+  u.any = __builtin_amdgcn_ballot_w64(large) != 0;
+  return l;
+}
+
+// After the last step: numerator and denominator in one unit, that of m.
+template <typename V, int N>
+__device__ __forceinline__ void own_unit(const SumUnit& u, float& m, V (&o)[N]) {
+  if (u.g != 1.0f) m += 60.0f;
+#pragma unroll
+  for (int x = 0; x < N; ++x) o[x] *= u.g;
 }
 
 template <typename T>
@@ -348,6 +384,7 @@ void attention_few(PagedAttention a) {
 #pragma unroll
   for (int x = 0; x < CT; ++x) o[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kNegInf, l = 0.0f;
+  SumUnit unit;
   if (wave < steps) pages(j0 + 32 * wave);
   for (int step = wave; step < steps; step += NW) {
     const int j = j0 + 32 * step;
@@ -431,7 +468,7 @@ void attention_few(PagedAttention a) {
     for (int i = 0; i < 8; ++i) w[i] = exp2_fast(x[i] - base) * av[i];
     f16x8 p[NP];
     split_f16<NP>(w, p);
-    l = add_weights<T, NP>(l, w, p, rv);
+    float sum = add_weights<T, NP>(0.0f, w, p, rv);
     auto values = [&](auto cc, int xw) {
       constexpr int C = decltype(cc)::value;
       const f16x8 vf = codes_f16_across<C>(vr[xw]);
@@ -448,10 +485,18 @@ void attention_few(PagedAttention a) {
       values(std::integral_constant<int, 2>{}, xw);
       values(std::integral_constant<int, 3>{}, xw);
     }
+    if (__builtin_expect(unit.any || __builtin_amdgcn_ballot_w64(sum > kLarge), 0)) {
+      l = fit_unit(unit, l, sum, [](float v) { return reduce_x16_x32(v, FMax{}); });
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rv[i] *= unit.g;
+      sum = add_weights<T, NP>(0.0f, w, p, rv);
+    }
+    l += sum;
   }
 
   // the wavefronts' sums, joined in order
   l = reduce_x16_x32(l, FAdd{});
+  if (unit.any) own_unit(unit, m, o);
   if (h == 0) {
     l_m[wave][r] = m;
     l_l[wave][r] = l;
@@ -527,14 +572,18 @@ void attention_few(PagedAttention a) {
 // Where a chunk lies: key k's chunk i (channels 8 i ..) at byte (k DT 2) +
 // 16 (i ^ key_turn(k)), channel c's chunk g of values at byte 128 c +
 // 16 (g ^ chunk_turn(c)).
+// A step's share of the denominator is added up before its unit is known: 32
+// weights of up to 2^14 over values of 2^-122 would pass 2^128.
+constexpr float kUp = 0x1p24f;
 template <int DT>
 struct ManyLds {                                           // bytes
   static constexpr int k = 0;                              // [2][64][DT] halves
   static constexpr int v = 2 * 64 * DT * 2;                // [2][DT][64] halves
   static constexpr int ks = 2 * v;                         // [2][64] ks * c0
   static constexpr int ls = ks + 512;                      // [2][64] log2(vs)
-  static constexpr int rs = ls + 512;                      // [2][64] 1 / vs
-  static constexpr int bytes = rs + 512;
+  static constexpr int rs = ls + 512;                      // [2][64] 1 / (vs * up)
+  static constexpr int up = rs + 512;                      // [2] up: 1, kUp beside a small value
+  static constexpr int bytes = up + 16;
   static constexpr int buffer = 64 * DT * 2;               // one of two, keys or values
 };
 
@@ -705,12 +754,14 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     if (!brings_values) {
       float* to = reinterpret_cast<float*>(smem + At::ks + P * 256) + lane;
       if (half) {
-        // values all zero: a scale far below, their codes are 0
-        const float sv = meta == 0.0f ? 0x1p-60f : fmaxf(meta, 0x1p-120f);
+        const float sv = held_scale(meta);
         const bool num = meta == meta;
+        const bool small = __builtin_amdgcn_ballot_w64(sv < 0x1p-64f) != 0;
+        const float up = small ? kUp : 1.0f;
         to[(At::ls - At::ks) / 4] =            // no page: weight 0
             !meta_ok ? kNegInf : num ? __builtin_amdgcn_logf(sv) : meta;
-        to[(At::rs - At::ks) / 4] = num ? 1.0f / sv : 1.0f;
+        to[(At::rs - At::ks) / 4] = num ? 1.0f / (sv * up) : 1.0f;
+        if (lane == 0) *reinterpret_cast<float*>(smem + At::up + P * 4) = up;
       } else {
         to[0] = meta_ok ? meta * c0 : 0.0f;
       }
@@ -723,6 +774,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[x][i] = 0.0f;
   float m = kNegInf, l = 0.0f;
+  SumUnit unit;
   // the chunks that a lane reads: of key r, of channel r
   constexpr int KA = DT == 64 ? 4 : 8;                     // columns of chunks that turn together
   int k_at[KA], v_at[4];
@@ -807,6 +859,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       m = top;
     }
     const float base = m == kNegInf ? 0.0f : m - kHead;
+    float lp = 0.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       float w[8], rv[8];
@@ -821,7 +874,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       }
       f16x8 p[NP];
       split_f16<NP>(w, p);
-      l = add_weights<T, NP>(l, w, p, rv);
+      lp = add_weights<T, NP>(lp, w, p, rv);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         const f16x8 vf = *reinterpret_cast<const f16x8*>(smem + v_at[v] + P * At::buffer +
@@ -831,6 +884,10 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
           o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);
       }
     }
+    const float up = *reinterpret_cast<const float*>(smem + At::up + P * 4);
+    if (__builtin_expect(unit.any || __builtin_amdgcn_ballot_w64(lp * up > kLarge), 0))
+      l = fit_unit(unit, l, lp * up, [](float v) { return reduce_x32(v, FMax{}); });
+    l = fmaf(lp, up * unit.g, l);
     __syncthreads();
   };
   for (int step = 0; step < steps; step += 2) {
@@ -838,6 +895,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     if (step + 1 < steps) advance(Odd{}, Even{}, step + 1);
   }
   l = reduce_x32(l, FAdd{});
+  if (unit.any) own_unit(unit, m, o);
   if (row >= rows_end) return;
   const int64_t ro = (int64_t)(t.token0 + tok) * a.q_heads + qh;
   const bool part = a.splits > 1;
