@@ -845,17 +845,28 @@ def _float_dt(t: torch.dtype) -> int:
         raise TypeError(f"unsupported dtype {t}") from None
 
 
-def _stream_of(t: torch.Tensor) -> int:
-    """torch's current stream on the tensor's GPU, as _stream() without the Stream object (which
-    costs as much as a launch)."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+def _call(name: str, gpu: int, fn, *args) -> None:
+    """fn(*args, stream) on torch's current stream of this GPU.  (The raw handle, not _stream()'s
+    Stream object, which costs as much as a launch.)"""
+    check(name, fn(*args, torch._C._cuda_getCurrentRawStream(gpu)))
 
 
-def _rows(t: torch.Tensor, name: str):
-    """Device pointer, row stride and shape of a GPU matrix whose rows are contiguous."""
-    shape = t.shape
-    if not t.is_cuda:
+def _gpu(t: torch.Tensor, name: str) -> int:
+    gpu = t.get_device()
+    if gpu < 0:
         raise ValueError(f"{name} must be a GPU tensor")
+    return gpu
+
+
+def _on(t: torch.Tensor, name: str, gpu: int) -> None:
+    if t.get_device() != gpu:
+        raise ValueError(f"{name} must be on GPU {gpu}, as the call's other tensors")
+
+
+def _rows(t: torch.Tensor, name: str, gpu: int):
+    """Device pointer, row stride and shape of a matrix on this GPU whose rows are contiguous."""
+    shape = t.shape
+    _on(t, name, gpu)
     if len(shape) != 2:
         raise ValueError(f"{name} must be a matrix")
     ld, e = t.stride()
@@ -865,10 +876,9 @@ def _rows(t: torch.Tensor, name: str):
     return t.data_ptr(), ld if rows > 1 else max(ld, c), rows, c
 
 
-def _heads(t: torch.Tensor, name: str):
-    """Device pointer, token stride and head stride of a GPU tensor [tokens][heads][d]."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
+def _heads(t: torch.Tensor, name: str, gpu: int):
+    """Device pointer, token stride and head stride of a tensor [tokens][heads][d] on this GPU."""
+    _on(t, name, gpu)
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens][heads][d]")
     tokens, heads, d = t.shape
@@ -880,20 +890,27 @@ def _heads(t: torch.Tensor, name: str):
     return t.data_ptr(), ts if tokens > 1 else heads * hs, hs
 
 
-def _vector(t: torch.Tensor | None, name: str, dtype: torch.dtype, n: int):
+def _dense(t: torch.Tensor, name: str, gpu: int) -> int:
+    _on(t, name, gpu)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _vector(t: torch.Tensor | None, name: str, dtype: torch.dtype, n: int, gpu: int):
     if t is None:
         return None
     if t.dtype != dtype or t.shape != (n,):
         raise ValueError(f"{name} must be {dtype} [{n}]")
-    return _dev(t, name)
+    return _dense(t, name, gpu)
 
 
-def _ws(ws: torch.Tensor | None, need, device):
+def _ws(ws: torch.Tensor | None, need, device, gpu: int):
     """A workspace, its pointer and size; one of need() bytes made for the call where the caller
     keeps none (torch's allocator orders its reuse on the stream)."""
     if ws is None:
         ws = torch.empty((need(),), dtype=torch.uint8, device=device)
-    return ws, _dev(ws, "ws"), ws.numel() * ws.element_size()
+    return ws, _dense(ws, "ws", gpu), ws.numel() * ws.element_size()
 
 
 def quantise_rows(x: torch.Tensor, q: torch.Tensor | None = None,
@@ -901,17 +918,17 @@ def quantise_rows(x: torch.Tensor, q: torch.Tensor | None = None,
     """Codes int8 [rows][c] and scales float32 [rows] of the rows of x (float32, float16 or
     bfloat16 [rows][c]): cs_quantise_rows.  Codes made here have a row stride that is a multiple
     of 16, which cs_linear_q8 reads fastest."""
-    px, ldx, rows, c = _rows(x, "x")
+    gpu = _gpu(x, "x")
+    px, ldx, rows, c = _rows(x, "x", gpu)
     if q is None:
         q = torch.empty((rows, (c + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :c]
     if q.dtype != torch.int8 or q.shape != x.shape:
         raise ValueError("q must be int8 of x's shape")
     if scale is None:
         scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
-    pq, ldq, _, _ = _rows(q, "q")
-    check("cs_quantise_rows", lib().cs_quantise_rows(
-        _float_dt(x.dtype), px, ldx, rows, c, pq, ldq,
-        _vector(scale, "scale", torch.float32, rows), _stream_of(x)))
+    pq, ldq, _, _ = _rows(q, "q", gpu)
+    _call("cs_quantise_rows", gpu, lib().cs_quantise_rows, _float_dt(x.dtype), px, ldx, rows, c, pq,
+          ldq, _vector(scale, "scale", torch.float32, rows, gpu))
     return q, scale
 
 
@@ -930,8 +947,9 @@ def linear_q8(x: torch.Tensor, w: torch.Tensor, sw: torch.Tensor, sx: torch.Tens
     scales sw (quantise_rows of the weight matrix gives both).  x [rows][k] is int8 with scales
     sx, or a float tensor that the call quantises row by row.  out_dtype: x's by default, float32
     for int8 x."""
-    px, ldx, rows, k = _rows(x, "x")
-    pw, ldw, d_out, kw = _rows(w, "w")
+    gpu = _gpu(x, "x")
+    px, ldx, rows, k = _rows(x, "x", gpu)
+    pw, ldw, d_out, kw = _rows(w, "w", gpu)
     xdt = x.dtype
     if w.dtype != torch.int8 or kw != k:
         raise ValueError(f"w must be int8 [d_out][{k}]")
@@ -945,17 +963,17 @@ def linear_q8(x: torch.Tensor, w: torch.Tensor, sw: torch.Tensor, sx: torch.Tens
         out = x.new_empty((rows, d_out), dtype=out_dtype)
         py, ldy = out.data_ptr(), d_out
     else:
-        py, ldy, yr, yc = _rows(out, "out")
+        py, ldy, yr, yc = _rows(out, "out", gpu)
         if out.dtype != out_dtype or yr != rows or yc != d_out:
             raise ValueError(f"out must be {out_dtype} [{rows}][{d_out}]")
     L = lib()
-    ws, pws, nws = _ws(ws, lambda: L.cs_linear_q8_workspace_bytes(xt, rows, k, d_out), x.device)
-    st = L.cs_linear_q8(
-        xt, px, ldx, _vector(sx, "sx", torch.float32, rows), rows, k, pw, ldw,
-        _vector(sw, "sw", torch.float32, d_out), d_out,
-        _vector(bias, "bias", torch.float32, d_out), _float_dt(out_dtype), py, ldy, pws, nws,
-        _stream_of(x))
-    check("cs_linear_q8", st)
+    ws, pws, nws = _ws(ws, lambda: L.cs_linear_q8_workspace_bytes(xt, rows, k, d_out), x.device,
+                       gpu)
+    _call("cs_linear_q8", gpu, L.cs_linear_q8,
+          xt, px, ldx, _vector(sx, "sx", torch.float32, rows, gpu), rows, k, pw, ldw,
+          _vector(sw, "sw", torch.float32, d_out, gpu), d_out,
+          _vector(bias, "bias", torch.float32, d_out, gpu), _float_dt(out_dtype), py, ldy, pws,
+          nws)
     return out
 
 
@@ -979,6 +997,8 @@ class PagedCache:
                 raise ValueError(f"{name} must be {dt} {list(shape)}")
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
+            if t.device != self.k.device:
+                raise ValueError(f"{name} must be on {self.k.device}, as k is")
         c = _lib.Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
                          self.v_scale.data_ptr(), *self.k.shape)
         for name, value in (("_c", c), ("_ref", ctypes.byref(c)),
@@ -994,27 +1014,28 @@ class PagedCache:
             return torch.empty((pages, heads, page), dtype=torch.float32, device=device)
         return cls(codes(), codes(), scales(), scales())
 
-    def _ptr(self):
-        if not self.k.is_cuda:
-            raise ValueError("the cache must be on the GPU")
+    def _ptr(self, gpu: int):
+        _on(self.k, "the cache", gpu)
         return self._ref
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Quantise k and v (float [tokens][heads][d]) into the cache's slots (int64 [tokens], slot =
     page number * page + offset; one outside the cache leaves its token out): cs_cache_write."""
-    pk, ldk, hsk = _heads(k, "k")
-    pv, ldv, hsv = _heads(v, "v")
+    gpu = _gpu(k, "k")
+    pk, ldk, hsk = _heads(k, "k", gpu)
+    pv, ldv, hsv = _heads(v, "v", gpu)
     if k.dtype != v.dtype or k.shape != v.shape or tuple(k.shape[1:]) != (cache.heads, cache.d):
         raise ValueError(f"k and v must be of one type and [tokens][{cache.heads}][{cache.d}]")
-    check("cs_cache_write", lib().cs_cache_write(
-        cache._ptr(), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
-        _vector(slots, "slots", torch.int64, k.shape[0]), k.shape[0], _stream_of(k)))
+    _call("cs_cache_write", gpu, lib().cs_cache_write,
+          cache._ptr(gpu), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
+          _vector(slots, "slots", torch.int64, k.shape[0], gpu), k.shape[0])
 
 
 def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
                out: tuple | None = None):
     """(k, v), each [tokens][heads][d] of `dtype`, of the slots' tokens: cs_cache_read."""
+    gpu = _gpu(slots, "slots")
     shape = (slots.shape[0], cache.heads, cache.d)
     if out is None:
         out = (slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype))
@@ -1022,9 +1043,9 @@ def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
         for t in out:
             if t.dtype != dtype or t.shape != shape:
                 raise ValueError(f"out must be {dtype} {list(shape)}")
-    check("cs_cache_read", lib().cs_cache_read(
-        cache._ptr(), _vector(slots, "slots", torch.int64, shape[0]), shape[0], _float_dt(dtype),
-        _dev(out[0], "out"), _dev(out[1], "out"), _stream_of(slots)))
+    _call("cs_cache_read", gpu, lib().cs_cache_read,
+          cache._ptr(gpu), _vector(slots, "slots", torch.int64, shape[0], gpu), shape[0],
+          _float_dt(dtype), _dense(out[0], "out", gpu), _dense(out[1], "out", gpu))
     return out
 
 
@@ -1068,7 +1089,8 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
     each sequence in q.  scale: 1 / sqrt(d) by default.  window: positions seen, 0 for all.
     max_len: the longest of lens if the caller knows it (a hint for how the work is split)."""
     qt, ml = _attention_args(q, cache, table, max_len)
-    pq, ldq, hsq = _heads(q, "q")
+    gpu = _gpu(q, "q")
+    pq, ldq, hsq = _heads(q, "q", gpu)
     b = table.shape[0]
     if out is None:
         out = q.new_empty(q.shape)
@@ -1078,11 +1100,11 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
     tokens, q_heads, _ = q.shape
     width = table.shape[1]
     ws, pws, nws = _ws(ws, lambda: L.cs_paged_attention_workspace_bytes(
-        cache._ref, qt, tokens, q_heads, b, width, ml), q.device)
-    st = L.cs_paged_attention(
-        cache._ptr(), qt, pq, ldq, hsq, tokens, q_heads, b, _dev(table, "table"), width,
-        _vector(lens, "lens", torch.int32, b), _vector(starts, "starts", torch.int32, b + 1), ml,
-        1.0 / math.sqrt(cache.d) if scale is None else scale, window, _dev(out, "out"), pws, nws,
-        _stream_of(q))
-    check("cs_paged_attention", st)
+        cache._ref, qt, tokens, q_heads, b, width, ml), q.device, gpu)
+    _call("cs_paged_attention", gpu, L.cs_paged_attention,
+          cache._ptr(gpu), qt, pq, ldq, hsq, tokens, q_heads, b, _dense(table, "table", gpu), width,
+          _vector(lens, "lens", torch.int32, b, gpu),
+          _vector(starts, "starts", torch.int32, b + 1, gpu), ml,
+          1.0 / math.sqrt(cache.d) if scale is None else scale, window, _dense(out, "out", gpu),
+          pws, nws)
     return out
