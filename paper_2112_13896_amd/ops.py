@@ -845,10 +845,18 @@ def _float_dt(t: torch.dtype) -> int:
         raise TypeError(f"unsupported dtype {t}") from None
 
 
+_current_gpu = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _call(name: str, gpu: int, fn, *args) -> None:
-    """fn(*args, stream) on torch's current stream of this GPU.  (The raw handle, not _stream()'s
-    Stream object, which costs as much as a launch.)"""
-    check(name, fn(*args, torch._C._cuda_getCurrentRawStream(gpu)))
+    """fn(*args, stream) on torch's current stream of this GPU, whichever GPU is current.  (The raw
+    handle, not _stream()'s Stream object, which costs as much as a launch.)"""
+    if gpu == _current_gpu():
+        check(name, fn(*args, _current_stream(gpu)))
+    else:
+        with torch.cuda.device(gpu):
+            check(name, fn(*args, _current_stream(gpu)))
 
 
 def _gpu(t: torch.Tensor, name: str) -> int:

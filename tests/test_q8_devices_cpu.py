@@ -1,7 +1,9 @@
 """Where the tensors of a call lie: the 8-bit operators refuse a tensor that is not on the call's GPU
-before anything is launched.  No GPU is used: stand-ins claim to be on one, and the library is a
-recorder."""
+before anything is launched, and launch on that GPU's stream.  No GPU is used: stand-ins claim to be
+on one, and the library is a recorder."""
 from __future__ import annotations
+
+import contextlib
 
 import pytest
 import torch
@@ -44,7 +46,16 @@ class Recorder:
 @pytest.fixture
 def rec(monkeypatch):
     r = Recorder()
+    r.entered = []
+
+    @contextlib.contextmanager
+    def device(gpu):
+        r.entered.append(gpu)
+        yield
     monkeypatch.setattr(ops, "lib", lambda: r)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(ops, "_current_gpu", lambda: 0, raising=False)
+    monkeypatch.setattr(ops, "_current_stream", lambda gpu: 1000 + gpu, raising=False)
     return r
 
 
@@ -81,6 +92,17 @@ def calls(gpu):
 
 
 NAMES = list(calls(0))
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("gpu", [0, 1])
+def test_the_tensors_gpu_is_used(rec, name, gpu):
+    """On the current GPU nothing is switched; on another one it is, for the launch."""
+    f, tensors = calls(gpu)[name]
+    f(**tensors)
+    assert [c[0] for c in rec.calls] == ["cs_" + name]
+    assert rec.calls[0][1][-1] == 1000 + gpu                  # the stream is the last argument
+    assert rec.entered == ([gpu] if gpu else [])
 
 
 @pytest.mark.parametrize("name", NAMES)
