@@ -845,6 +845,7 @@ def _float_dt(t: torch.dtype) -> int:
         raise TypeError(f"unsupported dtype {t}") from None
 
 
+_INT_MAX = 2 ** 31 - 1           # ctypes would pass on the low 32 bits of a larger number
 _current_gpu = torch._C._cuda_getDevice
 _current_stream = torch._C._cuda_getCurrentRawStream
 
@@ -881,6 +882,8 @@ def _rows(t: torch.Tensor, name: str, gpu: int):
     rows, c = shape
     if e != 1 and c > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
+    if c > _INT_MAX:
+        raise ValueError(f"{name}'s rows have more than 2^31 - 1 elements")
     return t.data_ptr(), ld if rows > 1 else max(ld, c), rows, c
 
 
@@ -961,6 +964,8 @@ def linear_q8(x: torch.Tensor, w: torch.Tensor, sw: torch.Tensor, sx: torch.Tens
     xdt = x.dtype
     if w.dtype != torch.int8 or kw != k:
         raise ValueError(f"w must be int8 [d_out][{k}]")
+    if d_out > _INT_MAX:
+        raise ValueError("w has more than 2^31 - 1 rows")
     codes = xdt == torch.int8
     xt = CS_I8 if codes else _float_dt(xdt)
     if codes != (sx is not None):
@@ -1062,7 +1067,9 @@ def _attention_args(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, max
         raise ValueError(f"q must be [tokens][q_heads][{cache.d}]")
     if table.dtype != torch.int32 or table.dim() != 2:
         raise ValueError("table must be int32 [batch][pages]")
-    return _float_dt(q.dtype), 0 if max_len is None else int(max_len)
+    if max(*q.shape, *table.shape) > _INT_MAX:
+        raise ValueError("q or table has a dimension over 2^31 - 1")
+    return _float_dt(q.dtype), 0 if max_len is None else min(int(max_len), _INT_MAX)
 
 
 def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
@@ -1083,7 +1090,7 @@ def paged_attention_plan(dtype: torch.dtype, heads: int, page: int, d: int, toke
     info = (ctypes.c_int64 * 6)()
     check("cs_paged_attention_plan", lib().cs_paged_attention_plan(
         ctypes.byref(cache), _float_dt(dtype), tokens, q_heads, batch, table_width,
-        0 if max_len is None else int(max_len), window, info))
+        0 if max_len is None else min(int(max_len), _INT_MAX), min(window, _INT_MAX), info))
     return dict(zip(("rows", "parts", "part", "wavefronts", "workgroups", "bytes"), info))
 
 
@@ -1097,6 +1104,7 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
     each sequence in q.  scale: 1 / sqrt(d) by default.  window: positions seen, 0 for all.
     max_len: the longest of lens if the caller knows it (a hint for how the work is split)."""
     qt, ml = _attention_args(q, cache, table, max_len)
+    window = min(window, _INT_MAX)                            # more hides nothing either
     gpu = _gpu(q, "q")
     pq, ldq, hsq = _heads(q, "q", gpu)
     b = table.shape[0]
