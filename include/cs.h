@@ -851,8 +851,9 @@ int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens
  *          (may be NULL where that is 0); undefined afterwards.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (cache geometry, strides,
  *  q_heads not a multiple of heads, heads over 65535, tokens * q_heads over
- *  2^31 - 1, table_width * page over CS_MAX_Q8_LEN),
- *  CS_ERR_WORKSPACE, CS_ERR_DEVICE.
+ *  2^31 - 1, table_width * page over CS_MAX_Q8_LEN, more than 2^31 - 1
+ *  workgroups as cs_paged_attention_plan counts them), CS_ERR_WORKSPACE,
+ *  CS_ERR_DEVICE.
  */
 int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
                        int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,

@@ -36,7 +36,7 @@ int with_float(cs_dtype t, F f) {
 template <typename T, int WPR>
 int quantise_launch(const T* x, int64_t ldx, int64_t rows, int c, int8_t* q, int64_t ldq,
                     float* scale, hipStream_t s) {
-  const dim3 grid((unsigned)((rows * WPR + 3) / 4)), block(256);
+  const dim3 grid = cs::wide_grid((rows * WPR + 3) / 4), block(256);
   auto starts_on = [&](size_t n) {
     return aligned(x, n) && (rows == 1 || ldx * sizeof(T) % n == 0);
   };
@@ -76,7 +76,8 @@ int linear_tiles(const cs::Q8Linear& a, hipStream_t s) {
   o.tiles_n = (uint32_t)tn;
   o.per_xcd = (uint32_t)(tm * tn / 8);
   o.more = (uint32_t)(tm * tn % 8);
-  hipLaunchKernelGGL((cs::linear_q8_tile<T, BM, BN, WM, WN, NB>), dim3((unsigned)(tm * tn)),
+  o.tiles = (uint32_t)(tm * tn);
+  hipLaunchKernelGGL((cs::linear_q8_tile<T, BM, BN, WM, WN, NB>), cs::wide_grid(tm * tn),
                      dim3(BM / WM * (BN / WN) * 64), 0, s, a, o);
   return launched();
 }
@@ -238,9 +239,9 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
   return with_float(yt, [&](auto t) {
     using T = decltype(t);
     if (!al) {
-      hipLaunchKernelGGL((cs::linear_q8_any<T>),
-                         dim3((unsigned)((rows + 63) / 64), (unsigned)(((int64_t)d_out + 63) / 64)),
-                         dim3(256), 0, s, a);
+      dim3 grid = cs::wide_grid((rows + 63) / 64);
+      grid.z = (unsigned)(((int64_t)d_out + 63) / 64);
+      hipLaunchKernelGGL((cs::linear_q8_any<T>), grid, dim3(256), 0, s, a);
       return launched();
     }
     auto tiles = [&](int bm, int bn) {
@@ -275,7 +276,9 @@ int cs_cache_write(const cs_q8_cache* cache, cs_dtype xt, const void* k, int64_t
   if (ldk < 0 || ldv < 0 || hsk < c.d || hsv < c.d) return CS_ERR_SHAPE;
   if (tokens > kMaxCount / c.heads) return CS_ERR_SHAPE;
   const uint32_t rows = (uint32_t)(tokens * c.heads);
-  const dim3 grid((rows + 15) / 16, 2), block(256);
+  const dim3 block(256);
+  dim3 grid = cs::wide_grid(((int64_t)rows + 15) / 16);
+  grid.z = 2;
   return with_float(xt, [&](auto t) {
     using T = decltype(t);
     const int64_t e = sizeof(T);
@@ -307,7 +310,9 @@ int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens
     return CS_ERR_ARG;
   if (tokens > kMaxCount / c.heads) return CS_ERR_SHAPE;
   const uint32_t rows = (uint32_t)(tokens * c.heads);
-  const dim3 grid((rows + 15) / 16, 2), block(256);
+  const dim3 block(256);
+  dim3 grid = cs::wide_grid(((int64_t)rows + 15) / 16);
+  grid.z = 2;
   return with_float(yt, [&](auto t) {
     using T = decltype(t);
     hipLaunchKernelGGL((cs::cache_read<T>), grid, block, 0, static_cast<hipStream_t>(stream), c,
@@ -390,7 +395,7 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
   if (blocks > kMaxCount) return CS_ERR_SHAPE;
   return with_float(qt, [&](auto t) {
     using T = decltype(t);
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 grid = cs::wide_grid(blocks), block(256);
     auto few = [&](auto dt) {
       constexpr int DT = decltype(dt)::value;
       if (p.waves == 8)

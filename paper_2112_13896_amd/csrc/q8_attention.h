@@ -63,12 +63,13 @@ struct PagedAttention {
 // Workgroups go to the eight XCDs in turn: heads vary fastest, so that the
 // tiles and parts that read one head's keys meet in few L2s (with eight heads,
 // or a multiple, in one).
-__device__ __forceinline__ void place(const PagedAttention& a, int* head, int* tile, int* split) {
-  const uint32_t rest = fdiv(blockIdx.x, a.by_heads);
-  *head = (int)(blockIdx.x - rest * a.by_heads.d);
+__device__ __forceinline__ bool place(const PagedAttention& a, int* head, int* tile, int* split) {
+  const uint32_t id = workgroup(), rest = fdiv(id, a.by_heads);
+  *head = (int)(id - rest * a.by_heads.d);
   const uint32_t s = fdiv(rest, a.by_tiles);
   *tile = (int)(rest - s * a.by_tiles.d);
   *split = (int)s;
+  return *split < a.splits;
 }
 
 // A tile of `per` rows of one sequence.  Sequence b's tiles have the numbers
@@ -318,7 +319,7 @@ void attention_few(PagedAttention a) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, h = lane / 16, d = a.c.d;
   int head, tile, split;
-  place(a, &head, &tile, &split);
+  if (!place(a, &head, &tile, &split)) return;
   RowTile t;
   if (!find_tile(a, tile, 16, &t)) return;
   const int rows_end = min(t.rows, t.row0 + 16);
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int r = lane % 32, h = lane / 32, d = a.c.d;
   int head, tile, split;
-  place(a, &head, &tile, &split);
+  if (!place(a, &head, &tile, &split)) return;
   RowTile t;
   // the last tiles of a sequence see most keys: first
   if (!find_tile(a, (int)a.by_tiles.d - 1 - tile, 128, &t)) return;

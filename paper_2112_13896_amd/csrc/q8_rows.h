@@ -20,6 +20,19 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// The number of a workgroup.  A dimension of a launch takes less than 2^32
+// threads (more are cut to their low 32 bits): workgroups past 2^22 are spread
+// over grid rows of that many (wide_grid), and those past the last have no work.
+constexpr int kGridRow = 22;
+__device__ __forceinline__ uint32_t workgroup() {
+  return (blockIdx.y << kGridRow) + blockIdx.x;
+}
+inline dim3 wide_grid(int64_t workgroups) {
+  const int64_t row = (int64_t)1 << kGridRow;
+  return workgroups <= row ? dim3((unsigned)workgroups)
+                           : dim3((unsigned)row, (unsigned)((workgroups + row - 1) / row));
+}
+
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(_Float16 v) { return (float)v; }
 __device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
@@ -121,7 +134,7 @@ __global__ __launch_bounds__(256) void quantise_rows(const T* __restrict__ x, in
   constexpr int kLanes = 64 * WPR;
   __shared__ uint32_t part[4];
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + group;
+  const int64_t row = (int64_t)workgroup() * (4 / WPR) + group;
   const bool live = row < rows;
   const T* xr = x + (live ? row : 0) * ldx;
   const int nv = live ? (c + 7) / 8 : 0;
@@ -195,7 +208,7 @@ __device__ __forceinline__ int64_t cache_row(const CacheView& c, int64_t slot, i
 }
 
 // cache_write and cache_read: a row (token, head) to 16 lanes, 16 rows to a
-// workgroup, keys and values by blockIdx.y.  A lane has every 16th vector of
+// workgroup, keys and values by blockIdx.z.  A lane has every 16th vector of
 // eight elements, at most two of them (d <= 256): 16 lanes are the most that
 // d = 128, the usual size, has 16-byte vectors for, and their maximum takes
 // four register moves.  Bound by memory: 16,384 tokens of 8 heads of 128 f16
@@ -207,14 +220,14 @@ __global__ __launch_bounds__(256) void cache_write(CacheView c, const T* __restr
                                                    const T* __restrict__ v, int64_t ldv,
                                                    int64_t hsv, const int64_t* __restrict__ slots,
                                                    uint32_t rows, FastDiv by_heads) {
-  const uint32_t row = blockIdx.x * 16 + threadIdx.x / 16;
+  const uint32_t row = workgroup() * 16 + threadIdx.x / 16;
   if (row >= rows) return;                                 // whole groups of 16 lanes leave
   const int lane = threadIdx.x % 16;
   const uint32_t token = fdiv(row, by_heads);
   const int head = (int)(row - token * by_heads.d);
   const int64_t slot = slots[token];
   if (slot < 0 || slot >= c.slots) return;
-  const bool val = blockIdx.y != 0;
+  const bool val = blockIdx.z != 0;
   const T* x = val ? v + token * ldv + head * hsv : k + token * ldk + head * hsk;
   const int nv = c.d / 8;
   float f[2][8];
@@ -262,13 +275,13 @@ template <typename T>
 __global__ __launch_bounds__(256) void cache_read(CacheView c, const int64_t* __restrict__ slots,
                                                   uint32_t rows, FastDiv by_heads,
                                                   T* __restrict__ k, T* __restrict__ v) {
-  const uint32_t row = blockIdx.x * 16 + threadIdx.x / 16;
+  const uint32_t row = workgroup() * 16 + threadIdx.x / 16;
   if (row >= rows) return;
   const int lane = threadIdx.x % 16;
   const uint32_t token = fdiv(row, by_heads);
   const int head = (int)(row - token * by_heads.d);
   const int64_t slot = slots[token];
-  const bool val = blockIdx.y != 0, in = slot >= 0 && slot < c.slots;
+  const bool val = blockIdx.z != 0, in = slot >= 0 && slot < c.slots;
   const int64_t at = in ? cache_row(c, slot, head) : 0;
   const float s = in ? (val ? c.vs : c.ks)[at] : 0.0f;
   const int8_t* q = (val ? c.v : c.k) + at * c.d;
