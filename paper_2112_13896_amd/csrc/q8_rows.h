@@ -137,9 +137,9 @@ __global__ __launch_bounds__(256) void quantise_rows(const T* __restrict__ x, in
   const int64_t row = (int64_t)workgroup() * (4 / WPR) + group;
   const bool live = row < rows;
   const T* xr = x + (live ? row : 0) * ldx;
-  const int nv = live ? (c + 7) / 8 : 0;
+  const int nv = live ? c / 8 + (c % 8 != 0) : 0;          // (c + 7 may pass 2^31)
   auto fetch = [&](int v, float (&f)[8]) {
-    if (8 * v + 8 <= c) load8_at<ALIGN>(xr + 8 * (int64_t)v, f);
+    if (c - 8 * v >= 8) load8_at<ALIGN>(xr + 8 * (int64_t)v, f);
     else load8_some(xr + 8 * (int64_t)v, c - 8 * v, f);
   };
   float f[kRowHeld][8];
@@ -172,12 +172,12 @@ __global__ __launch_bounds__(256) void quantise_rows(const T* __restrict__ x, in
   const bool wide = (reinterpret_cast<uintptr_t>(qr) & 7) == 0;
   auto put = [&](int v, const float (&g)[8]) {
     const u32x2 w = row_codes8(g, rs);
-    if (wide && 8 * v + 8 <= c) {
+    if (wide && c - 8 * v >= 8) {
       *reinterpret_cast<u32x2*>(qr + 8 * (int64_t)v) = w;
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (8 * v + i < c) qr[8 * (int64_t)v + i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+        if (i < c - 8 * v) qr[8 * (int64_t)v + i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
     }
   };
 #pragma unroll

@@ -89,3 +89,17 @@ def test_attention():
                               torch.arange(batch + 1, dtype=torch.int32, device="cuda"), max_len=1)
     want = cache.v[:, :, 0].float() * 0.25
     assert torch.allclose(out, want[table[:, 0].long()], rtol=2.0 ** -20, atol=0)
+
+
+@pytest.mark.parametrize("c", [(1 << 31) - 1, (1 << 31) - 8])
+def test_quantise_the_longest_row(c):
+    x = torch.zeros((1, c), dtype=torch.float16, device="cuda")
+    x[0, ::1000003] = 3.0
+    x[0, -9:] = torch.tensor([1.0, -4, 2, 254, -127, 0, 0.5, 64, -254], device="cuda").half()
+    x[0, :3] = torch.tensor([100.0, -1, 253], device="cuda").half()
+    q = torch.full((1, c), -128, dtype=torch.int8, device="cuda")
+    _, s = ops.quantise_rows(x, q=q)
+    assert s.tolist() == [2.0]
+    assert q[0, :3].tolist() == [50, 0, 126] and q[0, -9:].tolist() == [0, -2, 1, 127, -64, 0, 0, 32, -127]
+    assert not any(bool((p == -128).any()) for p in q[0].split(1 << 28))
+    assert int(q[0, 3:-9].count_nonzero()) == len(range(1000003, c - 9, 1000003))
