@@ -405,8 +405,9 @@ void attention_few(PagedAttention a) {
         const int ch = h * (DT / 4) + 16 * p;              // channels past d meet zeros in q
         kr[u][p] = *reinterpret_cast<const u32x4*>(kp + (uint32_t)(r * d + (ch < d ? ch : 0)));
       }
-      ks[u] = *reinterpret_cast<const f32x4*>(a.c.ks + row0 + 4 * h);
-      vs[u] = *reinterpret_cast<const f32x4*>(a.c.vs + row0 + 4 * h);
+      // scales start on 4 bytes
+      __builtin_memcpy(&ks[u], __builtin_assume_aligned(a.c.ks + row0 + 4 * h, 4), 16);
+      __builtin_memcpy(&vs[u], __builtin_assume_aligned(a.c.vs + row0 + 4 * h, 4), 16);
       const int ch = r * (DT / 16);                        // channels past d are not stored
       const int8_t* vp = a.c.v + row0 * d;
 #pragma unroll
