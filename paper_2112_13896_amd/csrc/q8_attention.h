@@ -33,6 +33,7 @@
 
 #include <type_traits>
 
+#include "q8_places.h"
 #include "q8_rows.h"
 
 namespace cs {
@@ -571,8 +572,8 @@ void attention_few(PagedAttention a) {
 // the keys 16 s + 4 h .. +3 and 16 s + 8 + 4 h .. +3.
 // Here a = 1, E = log2(sv), taken once a step.
 //
-// Where a chunk lies: key k's chunk i (channels 8 i ..) at byte (k DT 2) +
-// 16 (i ^ key_turn(k)), channel c's chunk g of values at byte 128 c +
+// Where a chunk lies (ManyPlaces): key k's chunk i (channels 8 i ..) at byte
+// (k DT 2) + 16 (i ^ key_turn(k)), channel c's chunk g of values at byte 128 c +
 // 16 (g ^ chunk_turn(c)).
 // A step's share of the denominator is added up before its unit is known: 32
 // weights of up to 2^14 over values of 2^-122 would pass 2^128.
@@ -586,7 +587,7 @@ struct ManyLds {                                           // bytes
   static constexpr int rs = ls + 512;                      // [2][64] 1 / (vs * up)
   static constexpr int up = rs + 512;                      // [2] up: 1, kUp beside a small value
   static constexpr int bytes = up + 16;
-  static constexpr int buffer = 64 * DT * 2;               // one of two, keys or values
+  static constexpr int buffer = ManyPlaces<DT>::buffer;    // one of two, keys or values
 };
 
 template <typename T, int W>
@@ -595,6 +596,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;
   constexpr int KS = W / 16, CT = W / 32;
   using At = ManyLds<DT>;
+  using Place = ManyPlaces<DT>;
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -669,16 +671,13 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
   const bool brings_values = wave < 2;
   const int half = wave % 2;
-  auto key_turn = [](int key) { return DT == 64 ? chunk_turn(key) : key & 15; };
-  constexpr int KB = DT / 64;                              // keys: loads a block, 16 bytes a lane
-  constexpr int PR = DT / 16;                              // lanes to a key
-  const int k_key = lane / PR, k_ch = lane % PR * 16;      // + 64 / PR keys a load
-  // values: 32 lanes to a block, 16 to each half of its keys (a chunk of LDS), DT / 16 channels
-  constexpr int VD = DT / 64;                              // dwords a lane and value row
-  const int v_ch = lane % 16 * 4 * VD;
+  constexpr int KB = Place::KB, PR = Place::PR, VD = Place::VD;
+  const int k_key = Place::key(lane), k_ch = Place::key_channel(lane);
+  const int v_ch = Place::value_channel(lane);
   // byte of a block that this lane loads first (channels past d: any)
-  const uint32_t off = brings_values ? 4 * (lane / 16 % 2) * d + (v_ch < d ? v_ch : 0)
-                                     : k_key * d + (k_ch < d ? k_ch : 0);
+  const uint32_t off = brings_values
+                           ? Place::value_key(lane / 16 % 2, 0) * d + (v_ch < d ? v_ch : 0)
+                           : k_key * d + (k_ch < d ? k_ch : 0);
   uint32_t reg[8 * VD];                                    // both blocks' keys; one's values
   float meta = 0.0f;
   bool meta_ok = false;
@@ -702,7 +701,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       for (int i = 0; i < 8; ++i) {
         uint32_t w[VD];
         __builtin_memcpy(
-            w, __builtin_assume_aligned(vp + (int64_t)(i / 4 * 8 + i % 4) * d, 4 * VD), 4 * VD);
+            w, __builtin_assume_aligned(vp + (int64_t)Place::value_key(0, i) * d, 4 * VD), 4 * VD);
 #pragma unroll
         for (int y = 0; y < VD; ++y) reg[8 * y + i] = w[y];
       }
@@ -725,9 +724,9 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   };
   auto put = [&](int at, f16x8 v) { *reinterpret_cast<f16x8*>(smem + at) = v; };
   // the lane's first row in LDS and the place of its chunk there (which the rows' numbers turn)
-  const int put_row = brings_values ? At::v + v_ch * 128 : At::k + (32 * half + k_key) * DT * 2;
-  const int put_bits = 16 * (brings_values ? (4 * half + lane / 16) ^ chunk_turn(v_ch)
-                                           : k_ch / 8 ^ key_turn(32 * half + k_key));
+  const int put_row = brings_values ? At::v + Place::value_row(lane)
+                                    : At::k + Place::key_row(half, lane);
+  const int put_bits = brings_values ? Place::value_bits(half, lane) : Place::key_bits(half, lane);
   auto stage = [&](auto par) {                             // buffer par
     constexpr int P = decltype(par)::value, kBuf = P * At::buffer;
     if (brings_values) {
@@ -737,7 +736,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = reg[8 * y + i] ^ kFlip;
         auto at = [&](int c) {                             // channel v_ch + 4 y + c
-          return kBuf + put_row + (4 * y + c) * 128 + (put_bits ^ 16 * chunk_turn(4 * y + c));
+          return kBuf + Place::value_put(put_row, put_bits, 4 * y + c);
         };
         put(at(0), codes_f16_across<0>(w));
         put(at(1), codes_f16_across<1>(w));
@@ -747,10 +746,9 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
     } else {
 #pragma unroll
       for (int p = 0; p < 2 * KB; ++p) {
-        const int key = p / KB * 16 + p % KB * (64 / PR);  // + 32 half + k_key
-        const int at = kBuf + put_row + key * DT * 2, turn = 16 * key_turn(key);
-        put(at + (put_bits ^ turn), codes_f16(reg[4 * p], reg[4 * p + 1]));
-        put(at + (put_bits ^ turn ^ 16), codes_f16(reg[4 * p + 2], reg[4 * p + 3]));
+        put(kBuf + Place::key_put(put_row, put_bits, p, 0), codes_f16(reg[4 * p], reg[4 * p + 1]));
+        put(kBuf + Place::key_put(put_row, put_bits, p, 1),
+            codes_f16(reg[4 * p + 2], reg[4 * p + 3]));
       }
     }
     if (!brings_values) {
@@ -778,12 +776,12 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
   float m = kNegInf, l = 0.0f;
   SumUnit unit;
   // the chunks that a lane reads: of key r, of channel r
-  constexpr int KA = DT == 64 ? 4 : 8;                     // columns of chunks that turn together
+  constexpr int KA = Place::KA;
   int k_at[KA], v_at[4];
 #pragma unroll
-  for (int i = 0; i < KA; ++i) k_at[i] = At::k + r * DT * 2 + ((2 * i + h) ^ key_turn(r)) * 16;
+  for (int i = 0; i < KA; ++i) k_at[i] = At::k + Place::key_column(r, h, i);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v_at[i] = At::v + r * 128 + ((2 * i + h) ^ chunk_turn(r)) * 16;
+  for (int i = 0; i < 4; ++i) v_at[i] = At::v + Place::value_column(r, h, i);
   typedef std::integral_constant<int, 0> Even;
   typedef std::integral_constant<int, 1> Odd;
   if (steps > 0) {
@@ -813,8 +811,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 #pragma unroll
     for (int i = 0; i < 2 * KS; ++i) {
       const int u = NP == 1 ? i % 2 : i / KS, k = NP == 1 ? i / 2 : i % KS;
-      const f16x8 kf = *reinterpret_cast<const f16x8*>(smem + k_at[k % KA] + P * At::buffer +
-                                                       32 * u * DT * 2 + k / KA * 256);
+      const f16x8 kf = *reinterpret_cast<const f16x8*>(smem + P * At::buffer +
+                                                       Place::key_at(k_at[k % KA], u, k));
 #pragma unroll
       for (int n = 0; n < NP; ++n)
         s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[n][k], s[u], 0, 0, 0);
@@ -839,13 +837,13 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       const int last = pos - j - 4 * h;
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (8 * (i / 4) + i % 4 > last) s[i / 16][i % 16] = kNegInf;
+        if (Place::logit_key(0, i) > last) s[i / 16][i % 16] = kNegInf;
     }
     if (j < see1) {
       const int first = see - j - 4 * h;
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (8 * (i / 4) + i % 4 < first) s[i / 16][i % 16] = kNegInf;
+        if (Place::logit_key(0, i) < first) s[i / 16][i % 16] = kNegInf;
     }
     float top = m;
 #pragma unroll
@@ -879,8 +877,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
       lp = add_weights<T, NP>(lp, w, p, rv);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        const f16x8 vf = *reinterpret_cast<const f16x8*>(smem + v_at[v] + P * At::buffer +
-                                                         ct * 32 * 128);
+        const f16x8 vf = *reinterpret_cast<const f16x8*>(smem + P * At::buffer +
+                                                         Place::value_at(v_at[v], ct));
 #pragma unroll
         for (int n = 0; n < NP; ++n)
           o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[n], o[ct], 0, 0, 0);

@@ -6,6 +6,7 @@
 
 #include <type_traits>
 
+#include "q8_places.h"
 #include "q8_rows.h"
 
 namespace cs {
@@ -186,17 +187,17 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   const int8_t* xb = a.x + t0 * a.ldx;
   const int8_t* wb = a.w + (int64_t)n0 * a.ldw;
   const int xrows = (int)min<int64_t>(BM, a.rows - t0), wrows = min(BN, a.d_out - n0);
-  // the 16-byte chunk `piece` of a buffer: row piece / 8, its chunk (piece % 8) ^ chunk_turn(row)
+  // the row and chunk that the 16-byte piece of a buffer holds
   uint32_t xo[PX], wo[PW];
 #pragma unroll
   for (int p = 0; p < PX; ++p) {
-    const int piece = p * THREADS + tid, row = piece / 8;
-    xo[p] = (uint32_t)min(row, xrows - 1) * (uint32_t)a.ldx + ((piece ^ chunk_turn(row)) & 7) * 16;
+    const int piece = p * THREADS + tid, row = TilePlaces::row(piece);
+    xo[p] = (uint32_t)min(row, xrows - 1) * (uint32_t)a.ldx + TilePlaces::chunk(piece) * 16;
   }
 #pragma unroll
   for (int p = 0; p < PW; ++p) {
-    const int piece = p * THREADS + tid, row = piece / 8;
-    wo[p] = (uint32_t)min(row, wrows - 1) * (uint32_t)a.ldw + ((piece ^ chunk_turn(row)) & 7) * 16;
+    const int piece = p * THREADS + tid, row = TilePlaces::row(piece);
+    wo[p] = (uint32_t)min(row, wrows - 1) * (uint32_t)a.ldw + TilePlaces::chunk(piece) * 16;
   }
   const int mr = wave / NW * WM, nr = wave % NW * WN;
   const int fr = lane % 32, fh = lane / 32;
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   auto multiply = [&](const int8_t* lx, const int8_t* lw) {
     i32x4 fx[2][MT], fw[2][NT];
     auto read = [&](int s) {
-      const int at = fr * 128 + ((2 * s + fh) ^ chunk_turn(fr)) * 16;
+      const int at = TilePlaces::at(fr, s, fh);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
         fx[s & 1][m] = *reinterpret_cast<const i32x4*>(lx + (mr + 32 * m) * 128 + at);
@@ -289,16 +290,16 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
     const int k0 = whole * 128;
 #pragma unroll
     for (int p = 0; p < PX; ++p) {
-      const int piece = p * THREADS + tid, row = min(piece / 8, xrows - 1);
+      const int piece = p * THREADS + tid, row = min(TilePlaces::row(piece), xrows - 1);
       *reinterpret_cast<i32x4*>(lx0 + piece * 16) =
-          codes16(xb + (int64_t)row * a.ldx, k0 + ((piece ^ chunk_turn(piece / 8)) & 7) * 16, a.k,
+          codes16(xb + (int64_t)row * a.ldx, k0 + TilePlaces::chunk(piece) * 16, a.k,
                   t0 + row + 1 < a.rows);
     }
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
-      const int piece = p * THREADS + tid, row = min(piece / 8, wrows - 1);
+      const int piece = p * THREADS + tid, row = min(TilePlaces::row(piece), wrows - 1);
       *reinterpret_cast<i32x4*>(lw0 + piece * 16) =
-          codes16(wb + (int64_t)row * a.ldw, k0 + ((piece ^ chunk_turn(piece / 8)) & 7) * 16, a.k,
+          codes16(wb + (int64_t)row * a.ldw, k0 + TilePlaces::chunk(piece) * 16, a.k,
                   n0 + row + 1 < a.d_out);
     }
     __syncthreads();

@@ -67,11 +67,6 @@ __device__ __forceinline__ void load8_some(const T* p, int n, float (&f)[8]) {
   for (int i = 0; i < 8; ++i) f[i] = i < n ? to_f32(p[i]) : 0.0f;
 }
 
-// LDS rows of 128 bytes, read in columns of 16-byte chunks by 32 lanes, a row
-// each: chunk c of a row lies at c ^ chunk_turn(row).  (row and row / 8: lanes
-// 0-3, 12-15, 20-27 of 32 are served together, and the others.)
-__device__ __forceinline__ int chunk_turn(int row) { return (row ^ (row >> 3 & 3)) & 7; }
-
 // |x| as bits: ordered as numbers, infinity above all of them, NaN above that.
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
