@@ -854,10 +854,12 @@ def _call(name: str, gpu: int, fn, *args) -> None:
     """fn(*args, stream) on torch's current stream of this GPU, whichever GPU is current.  (The raw
     handle, not _stream()'s Stream object, which costs as much as a launch.)"""
     if gpu == _current_gpu():
-        check(name, fn(*args, _current_stream(gpu)))
+        st = fn(*args, _current_stream(gpu))
     else:
         with torch.cuda.device(gpu):
-            check(name, fn(*args, _current_stream(gpu)))
+            st = fn(*args, _current_stream(gpu))
+    if st:
+        check(name, st)
 
 
 def _gpu(t: torch.Tensor, name: str) -> int:
@@ -1038,11 +1040,12 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torc
     gpu = _gpu(k, "k")
     pk, ldk, hsk = _heads(k, "k", gpu)
     pv, ldv, hsv = _heads(v, "v", gpu)
-    if k.dtype != v.dtype or k.shape != v.shape or tuple(k.shape[1:]) != (cache.heads, cache.d):
+    shape = k.shape
+    if k.dtype != v.dtype or v.shape != shape or shape[1] != cache.heads or shape[2] != cache.d:
         raise ValueError(f"k and v must be of one type and [tokens][{cache.heads}][{cache.d}]")
     _call("cs_cache_write", gpu, lib().cs_cache_write,
           cache._ptr(gpu), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
-          _vector(slots, "slots", torch.int64, k.shape[0], gpu), k.shape[0])
+          _vector(slots, "slots", torch.int64, shape[0], gpu), shape[0])
 
 
 def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
@@ -1063,21 +1066,25 @@ def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
 
 
 def _attention_args(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, max_len: int | None):
-    if q.dim() != 3 or q.shape[2] != cache.d:
+    """q's dtype and the sizes of a call, as cs_paged_attention_workspace_bytes takes them."""
+    shape, pages = q.shape, table.shape
+    if len(shape) != 3 or shape[2] != cache.d:
         raise ValueError(f"q must be [tokens][q_heads][{cache.d}]")
-    if table.dtype != torch.int32 or table.dim() != 2:
+    if table.dtype != torch.int32 or len(pages) != 2:
         raise ValueError("table must be int32 [batch][pages]")
-    if max(*q.shape, *table.shape) > _INT_MAX:
+    tokens, q_heads, _ = shape
+    batch, width = pages
+    if tokens | q_heads | batch | width > _INT_MAX:           # none is negative
         raise ValueError("q or table has a dimension over 2^31 - 1")
-    return _float_dt(q.dtype), 0 if max_len is None else min(int(max_len), _INT_MAX)
+    ml = 0 if max_len is None else int(max_len)
+    return _float_dt(q.dtype), tokens, q_heads, batch, width, ml if ml < _INT_MAX else _INT_MAX
 
 
 def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
                               max_len: int | None = None) -> torch.Tensor:
     """Workspace of paged_attention for arguments of these shapes."""
-    qt, ml = _attention_args(q, cache, table, max_len)
-    n = lib().cs_paged_attention_workspace_bytes(cache._ref, qt, q.shape[0],
-                                                 q.shape[1], table.shape[0], table.shape[1], ml)
+    n = lib().cs_paged_attention_workspace_bytes(
+        cache._ref, *_attention_args(q, cache, table, max_len))
     return torch.empty((int(n),), dtype=torch.uint8, device=q.device)
 
 
@@ -1103,18 +1110,16 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
     lens int32 [batch] positions with the new ones; starts int32 [batch + 1] first new token of
     each sequence in q.  scale: 1 / sqrt(d) by default.  window: positions seen, 0 for all.
     max_len: the longest of lens if the caller knows it (a hint for how the work is split)."""
-    qt, ml = _attention_args(q, cache, table, max_len)
-    window = min(window, _INT_MAX)                            # more hides nothing either
+    qt, tokens, q_heads, b, width, ml = _attention_args(q, cache, table, max_len)
+    if window > _INT_MAX:                                     # hides nothing either
+        window = _INT_MAX
     gpu = _gpu(q, "q")
     pq, ldq, hsq = _heads(q, "q", gpu)
-    b = table.shape[0]
     if out is None:
         out = q.new_empty(q.shape)
     elif out.dtype != q.dtype or out.shape != q.shape:
         raise ValueError("out must be of q's type and shape")
     L = lib()
-    tokens, q_heads, _ = q.shape
-    width = table.shape[1]
     ws, pws, nws = _ws(ws, lambda: L.cs_paged_attention_workspace_bytes(
         cache._ref, qt, tokens, q_heads, b, width, ml), q.device, gpu)
     _call("cs_paged_attention", gpu, L.cs_paged_attention,
