@@ -1,5 +1,5 @@
-"""A decoder block served in 8 bits: attention over a paged 8-bit cache, then the
-sparse-sparse feed-forward layers of this package.
+"""A decoder block: attention in 8 bits over a paged 8-bit cache, then the
+sparse-sparse feed-forward layers of this package, in fp32.
 
     python examples/decoder_block.py [--batch 16] [--prompt 300] [--tokens 32]
 
