@@ -846,7 +846,8 @@ int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens
  *  max_len what the work is split by: the longest of lens as far as the caller
  *          knows, 0 for table_width pages.  Any value gives right results.
  *  scale   finite, > 0.  window >= 0 (0: none).
- *  out     device [tokens][q_heads][d] out (dense).  tokens may be 0.
+ *  out     device [tokens][q_heads][d] out (dense, 16-byte aligned).  tokens may
+ *          be 0, and batch and table_width then too.
  *  ws      device, 16-byte aligned, cs_paged_attention_workspace_bytes bytes
  *          (may be NULL where that is 0); undefined afterwards.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (cache geometry, strides,

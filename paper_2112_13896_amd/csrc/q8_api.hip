@@ -363,7 +363,8 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
   cs::CacheView c;
   const int st = cache_view(cache, &c);
   if (st != CS_OK) return st;
-  if (tokens < 0 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0 || window < 0)
+  const int some = tokens > 0;                             // no tokens: no sequences needed
+  if (tokens < 0 || q_heads < 1 || batch < some || table_width < some || max_len < 0 || window < 0)
     return CS_ERR_ARG;
   if (!(scale > 0.0f) || std::isinf(scale)) return CS_ERR_ARG;
   if (tokens == 0) return CS_OK;
