@@ -127,7 +127,6 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
 // 10 us, 0.3 us a step, which is the latency of twelve dependent steps.
 struct TileOrder {
   uint32_t tiles_m, tiles_n, per_xcd, more;                // tiles / 8, tiles % 8
-  uint32_t tiles;
 };
 
 // The tile of a workgroup: workgroups go to the eight XCDs in turn, and each
@@ -180,8 +179,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void linear_q8_tile(Q8
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   int tm, tn;
-  if (workgroup() >= order.tiles) return;
-  place_tile(order, workgroup(), &tm, &tn);
+  place_tile(order, blockIdx.x, &tm, &tn);
   const int64_t t0 = (int64_t)tm * BM;
   const int n0 = tn * BN;
   const int8_t* xb = a.x + t0 * a.ldx;
