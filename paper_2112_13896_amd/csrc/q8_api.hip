@@ -342,7 +342,7 @@ size_t cs_paged_attention_workspace_bytes(const cs_q8_cache* cache, cs_dtype qt,
   cs::CacheView c;
   if (!is_float(qt) || cache_view(cache, &c) != CS_OK) return 0;
   if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0) return 0;
-  if (q_heads % c.heads != 0) return 0;
+  if (!attention_fits(c, tokens, q_heads, table_width)) return 0;
   // the whole axis: a window or a shorter one has at most as many parts
   const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len, 0);
   return attention_part_bytes(p.most, (int64_t)tokens * q_heads, c.d);
