@@ -719,7 +719,8 @@ size_t cs_workspace_bytes(int op, cs_dtype xt, int64_t rows, int c_in);
  * --------------------------------------------------
  * Floats of these calls are CS_F32, CS_F16 (IEEE half) or CS_BF16; sums,
  * softmax statistics and scales are 32 bits wide whatever their type, and a
- * result is rounded to it once.  Rows may be strided: ld* is the distance of
+ * result is rounded to it once (what cs_paged_attention multiplies has fewer
+ * bits, as said there).  Rows may be strided: ld* is the distance of
  * two rows and hs* that of two heads, in elements; a row's own elements are
  * contiguous.  Vector loads are used where pointers and strides are multiples
  * of 16 bytes, single elements elsewhere, with the same results.
@@ -761,7 +762,9 @@ int cs_quantise_rows(cs_dtype xt, const void* x, int64_t ldx, int64_t rows, int 
  *  yt, y   CS_F32, CS_F16 or CS_BF16; device [rows][d_out] out, row stride
  *          ldy >= d_out.  rows may be 0.
  *  ws      device, 16-byte aligned, cs_linear_q8_workspace_bytes bytes (may be
- *          NULL where that is 0); undefined afterwards.
+ *          NULL where that is 0); undefined afterwards.  It goes by xt and the
+ *          sizes alone: a few tokens that the product quantises itself need it
+ *          too, though nothing is written there.
  *  Rows of x and w that start on 16 bytes are staged 16 bytes at a time; pad
  *  the row stride of an odd k to a multiple of 16 to have that.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (a stride below its row,
@@ -779,7 +782,8 @@ size_t cs_linear_q8_workspace_bytes(cs_dtype xt, int64_t rows, int k, int d_out)
 /*
  * A paged cache of keys and values in 8 bits: per page and head, `page` rows
  * of d codes, and a scale per row.  Slot s is offset s % page of page
- * s / page.  Every array is the caller's device memory, codes 16-byte aligned.
+ * s / page.  Every array is the caller's device memory, codes 16-byte aligned,
+ * scales 4-byte.
  *  page    tokens of a page: a power of two from 16 to 1024.
  *  d       channels of a head: a multiple of 16 up to 256.
  *  pages * page is at most 2^31 - 1.  Scales are >= 0 or NaN, and a row of
@@ -832,6 +836,11 @@ int cs_cache_read(const cs_q8_cache* cache, const int64_t* slots, int64_t tokens
  * max(0, p - window + 1) (0 without a window) to p:
  * o = sum_j softmax_j(scale * q.k_j) v_j.  Query head h reads the cache's head
  * h / (q_heads / heads).  A token that sees nothing (p < 0) has o = 0.
+ * Products are of halves: codes are exact in them; a query head's elements are
+ * held to 2^-25 of its largest (CS_F32: 22 bits of each); a key's weight times
+ * its value scale to 11 bits (CS_F32: 22), and to 2^-37 of the row's largest.
+ * The sum of the weights is 32 bits wide, of weights in 32 bits; CS_F16 sums
+ * them as rounded, which brings its outputs nearer.
  * DEVICE memory, the cs_q8_cache excepted.
  *  qt      CS_F32, CS_F16 or CS_BF16: type of q and out.
  *  q       device [tokens][q_heads][d], token stride ldq, head stride hsq >= d.

@@ -269,7 +269,7 @@ int cs_linear_q8(cs_dtype xt, const void* x, int64_t ldx, const float* sx, int64
     if (rows <= 32 && d_out <= 2048) return linear_few<T, int8_t, 2>(a, s);
     // the largest tile of which there are enough to keep most compute units busy: 2,048 x 4,096 x
     // 4,096 40 us in 128 x 128, 59 in 64 x 64; 8,192 x 4,096 x 8,192 with its tokens quantised 321
-    // in 256 x 256, 361 in 128 x 128 (before both stored whole rows; 268 now)
+    // in 256 x 256, 361 in 128 x 128 (before both stored whole rows; 302 now)
     if (tiles(256, 256) >= 200) return linear_tiles<T, 256, 256, 128, 64, 2>(a, s);
     if (tiles(128, 128) >= 200) return linear_tiles<T, 128, 128, 64, 64, 2>(a, s);
     return linear_tiles<T, 64, 64, 32, 32, 4>(a, s);

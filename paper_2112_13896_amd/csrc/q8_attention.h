@@ -302,11 +302,14 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 // registers (no LDS) and are turned to halves there.
 // Bound by memory: 64 sequences of up to 8,192 keys, 32 query and 8 cache
 // heads of 128 (623 MB), take 135 us and 6.7 to join their parts, 4.6 TB/s of
-// the 5.1 of a large copy; the vector units are busy a third of the time.
+// the 5.1 of a large copy; the vector units are busy 39 % of the time.  A
+// sequence alone, 700 keys, eight wavefronts: 10.6 us, latency, 0.4 of them the
+// check of each step's share of the denominator (SumUnit).
 // What hides the loads is other wavefronts: registers for a step in flight
 // ahead (157 us), or for a second tile of rows, would halve their number (two
 // long sequences of 20 rows a head: 70 us with two tiles that both read the
-// keys, the second out of the L2, 88 us with one of 32 rows).
+// keys, the second out of the L2, 88 us with one of 32 rows; both before the
+// check, with it 75 for the two tiles).
 // Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of 16,
 // channels h DT/4 .. ; values: keys 4h .. 4h+3 of both tiles, channels r DT/16
 // .. ; logits: keys 4h .. 4h+3 of both tiles for row r.
@@ -558,10 +561,11 @@ void attention_few(PagedAttention a) {
 // 16 (a piece of one page, so their addresses are scalar).  W <= DT: channels
 // that are computed, d rounded up to 32.
 // Four prompts of 2,048 after up to 4,096 positions, 32 query and 8 cache heads
-// of 128, bf16 (409 GFLOP): 545-590 us, 700-750 TFLOP/s.  Bound by each
+// of 128, bf16 (409 GFLOP): 566-603 us, 680-720 TFLOP/s (1.7 % of it the check
+// of a step's share of the denominator).  Bound by each
 // wavefront's own stream of some 700 instructions a step: the registers allow
-// two wavefronts a SIMD, and with matrix units busy for 30 % and vector units
-// for 50 % of the time neither is full.  Measured by leaving work out: loads 18 %
+// two wavefronts a SIMD, and with matrix units busy for 29 % and vector units
+// for 48 % of the time neither is full.  Measured by leaving work out: loads 18 %
 // of the time, the first product 20, the second 15, exponentials 7, turning
 // codes 4.  Slower: 32 keys a step (720 us: twice the barriers; with three
 // wavefronts a SIMD registers spill, 808), the next half step's logits among

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) void linear_q8_any(Q8Linear a) {
 // stores and each row's scale loaded beside them, a tile's end took as long as
 // a third of its products: 315 us for the case below).
 // 256 x 256 with eight wavefronts, two buffers (128 KB): 8,192 x 4,096 x 8,192
-// in 250-290 us, 1.9-2.2 POP/s (a library int8 product of that size: 2.5).  Matrix
+// in 286 us, 252 at best, 1.9-2.2 POP/s (a library int8 product of that size: 2.4-2.5).  Matrix
 // instructions issue half of the time; of a step of 128 codes a fifth is the
 // wait for its loads, and a tile's start and end, which nothing overlaps, are a
 // fifth of the whole.  64 x 64, four wavefronts, four buffers: 777 x 1,500 x 1,001 in
