@@ -891,6 +891,164 @@ int cs_paged_attention_plan(const cs_q8_cache* cache, cs_dtype qt, int tokens, i
                             int batch, int table_width, int max_len, int window, int64_t* info);
 
 /*
+ * 4-bit cache and what a step of serving needs beside it
+ * -------------------------------------------------------
+ * Types, strides and roundings as for the 8-bit operators.
+ *
+ * Codes in 4 bits: a row of d channels is cut into groups of 32 (the last one
+ * may hold 16), each with a scale 2^E: the least power of two with max|x| <=
+ * 7 * 2^E, E kept within [-60, 60].  A code is the nearest of 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 to |x| / 2^E (ties to the even code of these eight, 0 to 7) with
+ * the value's sign as its fourth bit; what is beyond 6 is 6.  So magnitudes
+ * above 6 * 2^60 are held as that, and those up to 2^-62 as 0.  The scale is
+ * the byte E + 127.  A row with an infinity or a NaN has scale bytes 255 and
+ * codes 0: all of it is NaN, and so is what is computed from it.
+ */
+
+/*
+ * A paged cache of keys and values in 4 bits.  With dp = d rounded up to 32 and
+ * G = dp / 32 groups a row:
+ *  k        [pages][heads][page][dp / 2]: byte i of a row holds channel 2 i
+ *           (low half) and 2 i + 1; codes of channels from d on are 0.
+ *  k_scale  [pages][heads][page][G].
+ *  v        [pages][heads][page / 4][dp / 8][4][4]: blocks of four tokens, per
+ *           eight channels the four tokens' four bytes in turn.
+ *  v_scale  [pages][heads][page / 4][G][4].
+ * Every array is the caller's device memory; codes 16-byte aligned, scales
+ * 4-byte.  page and d as in cs_q8_cache, pages * page at most 2^31 - 1.
+ * Scale bytes are 67 to 187, or 255 in all of a row's groups beside codes 0,
+ * as cs_mx4_cache_write leaves them.
+ */
+typedef struct {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int pages, heads, page, d;
+} cs_mx4_cache;
+
+/*
+ * cs_mx4_cache_write, cs_mx4_cache_read - as cs_cache_write and cs_cache_read,
+ * for the 4-bit cache.  Errors: the same.
+ */
+int cs_mx4_cache_write(const cs_mx4_cache* cache, cs_dtype xt, const void* k, int64_t ldk,
+                       int64_t hsk, const void* v, int64_t ldv, int64_t hsv,
+                       const int64_t* slots, int64_t tokens, void* stream);
+int cs_mx4_cache_read(const cs_mx4_cache* cache, const int64_t* slots, int64_t tokens, cs_dtype yt,
+                      void* k, void* v, void* stream);
+
+/*
+ * cs_mx4_paged_attention - cs_paged_attention over the 4-bit cache: the same
+ * arguments, checks and errors.  Keys meet the queries as they are held, on the
+ * matrix cores' own 4-bit form; a query head's elements are held to 2^-20 of its
+ * largest and CS_BF16 otherwise in full (CS_F16: 2^-24, CS_F32: 2^-32 and 24
+ * bits of each).  A key's weight has 16 bits (CS_F32: 24), but 8 where the call
+ * runs CS_BF16 rows 128 at a time (cs_mx4_paged_attention_plan's rows); the sum
+ * of the weights is 32 bits wide.
+ */
+int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
+                           int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,
+                           int table_width, const int32_t* lens, const int32_t* starts,
+                           int max_len, float scale, int window, void* out, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* Workspace and plan of cs_mx4_paged_attention, as cs_paged_attention's. */
+size_t cs_mx4_paged_attention_workspace_bytes(const cs_mx4_cache* cache, cs_dtype qt, int tokens,
+                                              int q_heads, int batch, int table_width,
+                                              int max_len);
+int cs_mx4_paged_attention_plan(const cs_mx4_cache* cache, cs_dtype qt, int tokens, int q_heads,
+                                int batch, int table_width, int max_len, int window,
+                                int64_t* info);
+
+/*
+ * cs_rotary - rotary positions: the first `rot` channels of every head are
+ * rot / 2 pairs, and pair i of a token at position p is turned by the angle
+ * p * f_i: (x1, x2) -> amplitude * (x1 cos - x2 sin, x2 cos + x1 sin).  One call
+ * turns two tensors of the same tokens (queries and keys).  DEVICE memory.
+ *  xt           CS_F32, CS_F16 or CS_BF16; computed in 32 bits, rounded once.
+ *  turns        device uint64 [rot / 2]: f_i / (2 pi) as a fraction of a turn,
+ *               times 2^64.  Angles are formed in integers, exact to 2^-64 of a
+ *               turn a position, so that far positions lose nothing.
+ *  positions    device int32 [tokens]; the rows of a token below 0 are copied.
+ *  interleaved  0: pair i is channels i and i + rot / 2; else 2 i and 2 i + 1.
+ *  inverse      non-zero: by minus the angle (the gradient of a call with 0).
+ *  x[n], y[n]   device [tokens][heads[n]][d], n = 0, 1, token strides ldx[n],
+ *               ldy[n], head strides hsx[n], hsy[n] >= d.  y may be x with the
+ *               same strides, and must not overlap it otherwise; channels from
+ *               rot on are copied.  heads[n] may be 0 (x[n], y[n] then NULL).
+ * The arrays x, y, ldx, hsx, ldy, hsy and heads are host memory of two entries.
+ * tokens may be 0.
+ *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (rot odd, below 2 or over d,
+ *  d over 1024, strides, tokens of y less than d apart, more than 65535 heads
+ *  in all, tokens * heads over 2^31 - 1), CS_ERR_DEVICE.
+ */
+int cs_rotary(cs_dtype xt, const uint64_t* turns, int rot, int interleaved, float amplitude,
+              int inverse, const int32_t* positions, int64_t tokens, int d, const int* heads,
+              const void* const* x, const int64_t* ldx, const int64_t* hsx, void* const* y,
+              const int64_t* ldy, const int64_t* hsy, void* stream);
+
+/*
+ * The pages of a cache and the sequences that hold them, in DEVICE memory, so
+ * that a step is planned without the host.  Sequence s has length lengths[s] and
+ * holds the pages table[s][0 .. ceil(lengths[s] / page) - 1]; the free pages are
+ * a stack, free_pages[0 .. count - 1].  marks belongs to the calls: all
+ * 0x7FFFFFFF before the first one and after each.
+ *  page   as the cache's.  sequences * width and pages are at most 2^31 - 1,
+ *         width * page at most CS_MAX_Q8_LEN.
+ * The struct itself is host memory.  Calls on one pool are made in stream order.
+ */
+typedef struct {
+  int32_t* table;       /* [sequences][width] */
+  int32_t* lengths;     /* [sequences] */
+  int32_t* free_pages;  /* [pages] */
+  int32_t* count;       /* [1] */
+  int32_t* marks;       /* [sequences] */
+  int sequences, width, pages, page;
+} cs_page_pool;
+
+/*
+ * cs_plan_step - gives sequences room for new tokens and writes what
+ * cs_mx4_cache_write and cs_mx4_paged_attention (and cs_cache_write and
+ * cs_paged_attention) take of the step.  DEVICE memory.
+ *  seqs, fresh  device int32 [batch]: entry i brings fresh[i] new tokens to
+ *               sequence seqs[i]; -1 names none (a batch padded to a fixed size).
+ *  Pages are taken off the stack's top, entry after entry.
+ *  table        device int32 [batch][table_width] out: the entries' pages, -1
+ *               behind them.
+ *  lens, starts device int32 [batch], [batch + 1] out: lengths with the new
+ *               tokens, and each entry's first new token.
+ *  slots, positions  device int64, int32 [tokens] out: slot and position of each
+ *               new token, entry after entry; -1 behind the last.
+ *  status       device int32 [2] out: 0, 0 where the step was planned; 1 and the
+ *               first entry that is wrong (no such sequence, the same one twice,
+ *               fewer than 0 new tokens, more positions than table_width or the
+ *               pool's width hold); 2 and how many tokens `tokens` falls short
+ *               by; 3 and how many pages the pool does.  Unless it is 0 the pool
+ *               is left as it was, and the step has no tokens: lengths and starts
+ *               0, everything else -1.
+ *  ws           device, 16-byte aligned, cs_plan_step_workspace_bytes bytes.
+ *  Errors: CS_ERR_ARG, CS_ERR_SHAPE (pool geometry; batch over 2^20, batch *
+ *  table_width or tokens over 2^31 - 1, table_width * page over CS_MAX_Q8_LEN),
+ *  CS_ERR_WORKSPACE, CS_ERR_DEVICE.
+ */
+int cs_plan_step(const cs_page_pool* pool, const int32_t* seqs, const int32_t* fresh, int batch,
+                 int32_t* table, int table_width, int32_t* lens, int32_t* starts, int64_t* slots,
+                 int32_t* positions, int64_t tokens, int32_t* status, void* ws, size_t ws_bytes,
+                 void* stream);
+size_t cs_plan_step_workspace_bytes(int batch);
+
+/*
+ * cs_pool_truncate - cuts sequences to lens[i] positions (NULL: 0, the sequence
+ * has ended); pages past that go onto the stack, the last one first, so that a
+ * step taken back leaves the stack as it was before it.  DEVICE memory.  Entries
+ * that name no sequence, repeat one, or would make it longer are left out.
+ *  Errors: CS_ERR_ARG, CS_ERR_SHAPE (pool geometry, batch over 2^20),
+ *  CS_ERR_DEVICE.
+ */
+int cs_pool_truncate(const cs_page_pool* pool, const int32_t* seqs, const int32_t* lens, int batch,
+                     void* stream);
+
+/*
  * cs_product_count - the number of weight x activation products the
  * multiply-route-sum kernels have formed on the current device since the
  * last reset (Section 3.2 and Figure 1: only pairs of a non-zero activation

@@ -41,7 +41,19 @@ class Q8Cache(ctypes.Structure):
                 ("heads", _i), ("page", _i), ("d", _i)]
 
 
-_cache = _c.POINTER(Q8Cache)
+class Mx4Cache(ctypes.Structure):
+    """cs_mx4_cache"""
+    _fields_ = Q8Cache._fields_
+
+
+class PagePool(ctypes.Structure):
+    """cs_page_pool"""
+    _fields_ = [("table", _vp), ("lengths", _vp), ("free_pages", _vp), ("count", _vp),
+                ("marks", _vp), ("sequences", _i), ("width", _i), ("pages", _i), ("page", _i)]
+
+
+_cache, _cache4, _pool = _c.POINTER(Q8Cache), _c.POINTER(Mx4Cache), _c.POINTER(PagePool)
+_vps, _i64s = _c.POINTER(_vp), _c.POINTER(_i64)
 SIGNATURES = {
     "cs_pack": (_i, [_i, _vp, _i, _i, _i, _vp, _c.POINTER(_i64), _c.POINTER(_i), _c.POINTER(_i)]),
     "cs_compact": (_i, [_i, _vp, _i64, _i, _vp, _vp, _vp, _vp]),
@@ -104,6 +116,18 @@ SIGNATURES = {
                                 _c.c_float, _i, _vp, _vp, _sz, _vp]),
     "cs_paged_attention_workspace_bytes": (_sz, [_cache, _i, _i, _i, _i, _i, _i]),
     "cs_paged_attention_plan": (_i, [_cache, _i, _i, _i, _i, _i, _i, _i, _c.POINTER(_i64)]),
+    "cs_mx4_cache_write": (_i, [_cache4, _i, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp]),
+    "cs_mx4_cache_read": (_i, [_cache4, _vp, _i64, _i, _vp, _vp, _vp]),
+    "cs_mx4_paged_attention": (_i, [_cache4, _i, _vp, _i64, _i64, _i, _i, _i, _vp, _i, _vp, _vp,
+                                    _i, _c.c_float, _i, _vp, _vp, _sz, _vp]),
+    "cs_mx4_paged_attention_workspace_bytes": (_sz, [_cache4, _i, _i, _i, _i, _i, _i]),
+    "cs_mx4_paged_attention_plan": (_i, [_cache4, _i, _i, _i, _i, _i, _i, _i, _c.POINTER(_i64)]),
+    "cs_rotary": (_i, [_i, _vp, _i, _i, _c.c_float, _i, _vp, _i64, _i, _c.POINTER(_i), _vps, _i64s,
+                       _i64s, _vps, _i64s, _i64s, _vp]),
+    "cs_plan_step": (_i, [_pool, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _sz,
+                          _vp]),
+    "cs_plan_step_workspace_bytes": (_sz, [_i]),
+    "cs_pool_truncate": (_i, [_pool, _vp, _vp, _i, _vp]),
     "cs_product_count": (_i, [_c.POINTER(_c.c_ulonglong), _i]),
     "cs_phase_stamps": (_i, [_c.POINTER(_c.c_ulonglong), _i, _i, _c.POINTER(_c.c_int)]),
     "cs_status_str": (_c.c_char_p, [_i]),

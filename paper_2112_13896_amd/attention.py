@@ -1,16 +1,20 @@
-"""An attention layer served in 8 bits, and the plan of a step over many sequences.
+"""An attention layer served in 8 bits, its cache in 8 or 4, and the plan of a step over many
+sequences.
 
-The layer runs the four 8-bit operators as they are meant to be used together:
+The layer runs the operators as they are meant to be used together:
 
   tokens -> linear_q8 (queries, keys and values in one product)
-         -> cache_write (the new tokens' keys and values, a scale per token and head)
+         -> rotary (queries and keys to their positions, where the layer has them)
+         -> cache_write (the new tokens' keys and values, quantised per token and head)
          -> paged_attention (each sequence's new tokens over all its positions)
          -> linear_q8 (output projection)
 
 Weights are quantised once (quantise_rows, a scale per output channel).  A Step
 says which tokens of the batch belong to which sequence and where their keys
 live; a prompt, a part of one, drafted tokens and a decoding step differ in
-nothing but the number of new tokens.  forward() only enqueues kernels on
+nothing but the number of new tokens.  It is made on the host (Step.of, with a
+PagePool's pages) or on the GPU (Step.plan, with an ops.DevicePool's), where a
+recorded graph can make the next one.  forward() only enqueues kernels on
 torch's current stream; buffers that its caller wants to keep (for a recorded
 graph, say) come from make_buffers().
 """
@@ -60,12 +64,14 @@ class PagePool:
 
 @dataclass
 class Step:
-    """What paged_attention and cache_write need to know of a batch of new tokens."""
+    """What paged_attention, cache_write and rotary need to know of a batch of new tokens."""
     table: torch.Tensor      # int32 [batch][pages]
     lens: torch.Tensor       # int32 [batch]
     starts: torch.Tensor     # int32 [batch + 1]
     slots: torch.Tensor      # int64 [tokens]
     max_len: int
+    positions: torch.Tensor | None = None    # int32 [tokens]
+    status: torch.Tensor | None = None       # int32 [2], of a step planned on the GPU
 
     @classmethod
     def of(cls, seqs, new, page: int, device="cuda", width: int = 0) -> "Step":
@@ -79,31 +85,54 @@ class Step:
         width = max(width, 1, max(len(s.pages) for s in seqs))
         table = torch.full((len(seqs), width), -1, dtype=torch.int32)
         starts = torch.zeros(len(seqs) + 1, dtype=torch.int32)
-        slots = []
+        slots, positions = [], []
         for i, (s, n) in enumerate(zip(seqs, new)):
             table[i, :len(s.pages)] = torch.tensor(s.pages, dtype=torch.int32)
             starts[i + 1] = starts[i] + n
             slots += [s.pages[j // page] * page + j % page for j in range(s.length - n, s.length)]
+            positions += range(s.length - n, s.length)
         lens = torch.tensor([s.length for s in seqs], dtype=torch.int32)
         return cls(table.to(device), lens.to(device), starts.to(device),
                    torch.tensor(slots, dtype=torch.int64).to(device),
-                   max(s.length for s in seqs))
+                   max(s.length for s in seqs),
+                   torch.tensor(positions, dtype=torch.int32).to(device))
+
+    @classmethod
+    def plan(cls, pool: ops.DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: int,
+             max_len: int, width: int | None = None, ws: torch.Tensor | None = None,
+             into: "Step | None" = None) -> "Step":
+        """The step in which new[i] tokens come to sequence seqs[i] of the pool, planned by a kernel
+        (ops.plan_step): of up to `tokens` tokens, padded to that many, and sequences of up to
+        max_len positions as far as the caller knows.  `into`: an earlier step of these sizes,
+        overwritten and returned.  The step's status is 0, 0 unless the pool could not give it."""
+        out = None
+        if into is not None:
+            out = (into.table, into.lens, into.starts, into.slots, into.positions, into.status)
+        table, lens, starts, slots, positions, status = ops.plan_step(pool, seqs, new, tokens,
+                                                                      width, ws, out)
+        if into is not None:
+            into.max_len = max_len
+            return into
+        return cls(table, lens, starts, slots, max_len, positions, status)
 
 
 class AttentionLayer:
     """wq [q_heads * d][width], wk and wv [heads * d][width], wo [width][q_heads * d]: float
     weights, quantised here; biases (float32) or None.  `dtype`: the type of the tokens and of
-    what is between the products."""
+    what is between the products.  `rotary`: what turns queries and keys to their positions."""
 
     def __init__(self, wq, wk, wv, wo, heads: int, d: int, *, bias=None, out_bias=None,
-                 dtype: torch.dtype = torch.bfloat16, window: int = 0, device="cuda"):
+                 dtype: torch.dtype = torch.bfloat16, window: int = 0, device="cuda",
+                 rotary: ops.Rotary | None = None):
         if wq.shape[0] % d or wk.shape[0] != heads * d or wv.shape != wk.shape or \
                 wo.shape != (wq.shape[1], wq.shape[0]):
             raise ValueError("weights do not fit the heads")
         self.heads, self.d, self.q_heads = heads, d, wq.shape[0] // d
         if self.q_heads % heads:
             raise ValueError("query heads must be a multiple of the cache's heads")
-        self.width, self.dtype, self.window = wq.shape[1], dtype, window
+        if rotary is not None and rotary.rot > d:
+            raise ValueError("rotary positions turn more channels than a head has")
+        self.width, self.dtype, self.window, self.rotary = wq.shape[1], dtype, window, rotary
         self.device = torch.device(device)
 
         def weights(w):
@@ -113,8 +142,11 @@ class AttentionLayer:
         self.bias = None if bias is None else bias.to(self.device, torch.float32)
         self.out_bias = None if out_bias is None else out_bias.to(self.device, torch.float32)
 
-    def make_cache(self, pages: int, page: int = 64) -> ops.PagedCache:
-        return ops.PagedCache.empty(pages, self.heads, page, self.d, self.device)
+    def make_cache(self, pages: int, page: int = 64, bits: int = 8) -> ops.PagedCache:
+        if bits not in (8, 4):
+            raise ValueError("a cache has 8 or 4 bits")
+        kind = ops.PagedCache if bits == 8 else ops.PagedCache4
+        return kind.empty(pages, self.heads, page, self.d, self.device)
 
     def make_buffers(self, tokens: int, cache: ops.PagedCache, step: Step) -> dict:
         """Intermediates and workspaces of forward() for this many tokens and such a step."""
@@ -134,11 +166,15 @@ class AttentionLayer:
         keys and values."""
         if x.dtype != self.dtype:
             raise TypeError(f"tokens must be {self.dtype}")
+        if self.rotary is not None and step.positions is None:
+            raise ValueError("the layer's rotary positions need the step's positions")
         b = buffers or {}
         qkv = ops.linear_q8(x, self.wqkv, self.sqkv, bias=self.bias, out=b.get("qkv"),
                             ws=b.get("ws_qkv"))
         heads = qkv.unflatten(1, (-1, self.d))
         q, k, v = heads.split([self.q_heads, self.heads, self.heads], dim=1)
+        if self.rotary is not None:
+            ops.rotary(self.rotary, step.positions, q, k, out=(q, k))
         ops.cache_write(cache, k, v, step.slots)
         o = ops.paged_attention(q, cache, step.table, step.lens, step.starts, window=self.window,
                                 max_len=step.max_len, out=b.get("o"), ws=b.get("ws_att"))

@@ -3,8 +3,9 @@
     python -m paper_2112_13896_amd.build
 
 Compiles the HIP kernels and C ABI (csrc/cs_api.hip, the sparse layers;
-csrc/q8_api.hip, the 8-bit attention-layer operators) and the host pack
-routine (csrc/cs_pack.cpp) with hipcc and links them, once as the product
+csrc/q8_api.hip, the 8-bit attention-layer operators; csrc/mx4_api.hip, the
+4-bit cache and attention; csrc/step_api.hip, rotary positions and step plans)
+and the host pack routine (csrc/cs_pack.cpp) with hipcc and links them, once as the product
 library and once with the product counter compiled in (libcs_count.so, used by
 tests).  Packed-fp32 instruction generation is switched off for all device
 code.
@@ -38,16 +39,18 @@ def hipcc() -> str:
 
 def sources() -> list:
     """Translation units; only the first knows the instrumented builds' defines."""
-    return [os.path.join(CSRC, f) for f in ("cs_api.hip", "q8_api.hip", "cs_pack.cpp")]
+    return [os.path.join(CSRC, f) for f in ("cs_api.hip", "q8_api.hip", "mx4_api.hip",
+                                          "step_api.hip", "cs_pack.cpp")]
 
 
 def source_digest() -> str:
     """SHA-256 over every source and header the layer kernels (csrc/cs_api.hip, csrc/cs_pack.cpp)
-    are built from: the native sources but those of the 8-bit attention-layer operators."""
+    are built from: the native sources but those of the attention-layer operators."""
     import hashlib
     h = hashlib.sha256()
     files = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)
-                   if f.endswith((".hip", ".cpp", ".h")) and not f.startswith("q8_"))
+                   if f.endswith((".hip", ".cpp", ".h"))
+                   and not f.startswith(("q8_", "mx4_", "step_")))
     files.append(os.path.join(INCLUDE, "cs.h"))
     for f in files:
         h.update(os.path.basename(f).encode())
@@ -93,7 +96,7 @@ def build(verbose: bool = False, extra: list | None = None, counting: bool = Tru
     """Compile libcs.so (always recompiles) and, with `counting`, the two
     instrumented builds: libcs_count.so (every multiply-route-sum kernel counts
     the products it forms; tests only) and libcs_stamps.so (phase stamps; the
-    benchmark's phase report), the compilations side by side.  The other two
+    benchmark's phase report), the compilations side by side.  The other
     sources know neither define: the three libraries share their objects.
     Returns the path of libcs.so."""
     extra = list(extra or [])

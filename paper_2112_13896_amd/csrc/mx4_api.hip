@@ -1,0 +1,207 @@
+// C ABI entry points of the 4-bit cache and attention over it (declared in
+// include/cs.h).  Every argument is checked on the host before the first HIP
+// call; kernels are enqueued on the caller's stream and nothing is allocated,
+// freed or synchronised here.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "cs.h"
+#include "mx4_attention.h"
+#include "mx4_rows.h"
+#include "q8_api_util.h"
+
+namespace {
+
+int cache_view(const cs_mx4_cache* c, cs::Mx4View* out) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return CS_ERR_ARG;
+  if (c->pages < 1 || c->heads < 1 || c->page < 1 || c->d < 1) return CS_ERR_ARG;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) ||
+      !aligned(c->v_scale, 4))
+    return CS_ERR_ARG;
+  if (c->d % 16 != 0 || c->d > 256) return CS_ERR_SHAPE;
+  if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)) != 0) return CS_ERR_SHAPE;
+  if ((int64_t)c->pages * c->page > kMaxCount) return CS_ERR_SHAPE;
+  int lg = 4;
+  while ((1 << lg) < c->page) ++lg;
+  *out = {c->k, c->v, c->k_scale, c->v_scale, (int64_t)c->pages * c->page, c->heads, lg, c->d,
+          (c->d + 31) / 32};
+  return CS_OK;
+}
+
+// Workgroups of mx4_write and mx4_read: four wavefronts, four tokens of a head each.
+dim3 cache_grid(int64_t tokens, int heads) {
+  dim3 grid = cs::wide_grid(((tokens + 3) / 4 * heads + 3) / 4);
+  grid.z = 2;
+  return grid;
+}
+
+struct AttentionPlan {
+  int per;             // rows of a workgroup
+  int64_t tiles;       // numbers of row tiles (find_tile)
+  int splits, chunk;   // parts of the key axis, positions of a part
+  int most;            // parts at most, of this axis under any window and of any shorter one
+  int waves;           // wavefronts of a workgroup
+};
+
+AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int q_heads,
+                             int batch, int table_width, int max_len, int window) {
+  AttentionPlan p;
+  const int64_t group = q_heads / c.heads, rows = tokens * group;
+  p.per = 1;
+  p.tiles = rows / p.per + batch + 1;
+  p.splits = p.most = 1;
+  p.chunk = CS_MAX_Q8_LEN;
+  p.waves = 1;
+  return p;
+}
+
+size_t attention_part_bytes(int64_t parts, int64_t rows, int d) {
+  return parts > 1 ? (size_t)parts * rows * ((size_t)d * 4 + 8) : 0;
+}
+
+bool attention_fits(const cs::Mx4View& c, int tokens, int q_heads, int table_width) {
+  return q_heads % c.heads == 0 && c.heads <= 65535 && (int64_t)tokens * q_heads <= kMaxCount &&
+         ((int64_t)table_width << c.page_log) <= CS_MAX_Q8_LEN;
+}
+
+}  // namespace
+
+extern "C" {
+
+int cs_mx4_cache_write(const cs_mx4_cache* cache, cs_dtype xt, const void* k, int64_t ldk,
+                       int64_t hsk, const void* v, int64_t ldv, int64_t hsv,
+                       const int64_t* slots, int64_t tokens, void* stream) {
+  if (!is_float(xt)) return CS_ERR_DTYPE;
+  cs::Mx4View c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 0) return CS_ERR_ARG;
+  if (tokens == 0) return CS_OK;
+  if (!k || !v || !slots || !aligned(k, float_size(xt)) || !aligned(v, float_size(xt)) ||
+      !aligned(slots, 8))
+    return CS_ERR_ARG;
+  if (ldk < 0 || ldv < 0 || hsk < c.d || hsv < c.d) return CS_ERR_SHAPE;
+  if (tokens > kMaxCount / c.heads) return CS_ERR_SHAPE;
+  return with_float(xt, [&](auto t) {
+    using T = decltype(t);
+    const int64_t e = sizeof(T);
+    const bool vec = aligned(k, 16) && aligned(v, 16) && ldk * e % 16 == 0 && ldv * e % 16 == 0 &&
+                     hsk * e % 16 == 0 && hsv * e % 16 == 0;
+    auto go = [&](auto wide) {
+      hipLaunchKernelGGL((cs::mx4_write<T, decltype(wide)::value>), cache_grid(tokens, c.heads),
+                         dim3(256), 0, static_cast<hipStream_t>(stream), c,
+                         static_cast<const T*>(k), ldk, hsk, static_cast<const T*>(v), ldv, hsv,
+                         slots, tokens, cs::make_fastdiv((uint32_t)c.heads));
+      return launched();
+    };
+    return vec ? go(std::true_type{}) : go(std::false_type{});
+  });
+}
+
+int cs_mx4_cache_read(const cs_mx4_cache* cache, const int64_t* slots, int64_t tokens, cs_dtype yt,
+                      void* k, void* v, void* stream) {
+  if (!is_float(yt)) return CS_ERR_DTYPE;
+  cs::Mx4View c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 0) return CS_ERR_ARG;
+  if (tokens == 0) return CS_OK;
+  if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8))
+    return CS_ERR_ARG;
+  if (tokens > kMaxCount / c.heads) return CS_ERR_SHAPE;
+  return with_float(yt, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL((cs::mx4_read<T>), cache_grid(tokens, c.heads), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), c, slots, tokens,
+                       cs::make_fastdiv((uint32_t)c.heads), static_cast<T*>(k),
+                       static_cast<T*>(v));
+    return launched();
+  });
+}
+
+size_t cs_mx4_paged_attention_workspace_bytes(const cs_mx4_cache* cache, cs_dtype qt, int tokens,
+                                              int q_heads, int batch, int table_width,
+                                              int max_len) {
+  cs::Mx4View c;
+  if (!is_float(qt) || cache_view(cache, &c) != CS_OK) return 0;
+  if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0) return 0;
+  if (!attention_fits(c, tokens, q_heads, table_width)) return 0;
+  // the whole axis: a window or a shorter one has at most as many parts
+  const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len, 0);
+  return attention_part_bytes(p.most, (int64_t)tokens * q_heads, c.d);
+}
+
+int cs_mx4_paged_attention_plan(const cs_mx4_cache* cache, cs_dtype qt, int tokens, int q_heads,
+                                int batch, int table_width, int max_len, int window,
+                                int64_t* info) {
+  if (!info) return CS_ERR_ARG;
+  if (!is_float(qt)) return CS_ERR_DTYPE;
+  cs::Mx4View c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  if (tokens < 1 || q_heads < 1 || batch < 1 || table_width < 1 || max_len < 0 || window < 0)
+    return CS_ERR_ARG;
+  if (!attention_fits(c, tokens, q_heads, table_width)) return CS_ERR_SHAPE;
+  const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len,
+                                         window);
+  info[0] = p.per;
+  info[1] = p.splits;
+  info[2] = p.chunk;
+  info[3] = p.waves;
+  info[4] = p.tiles * c.heads * p.splits;
+  info[5] = (int64_t)attention_part_bytes(p.splits, (int64_t)tokens * q_heads, c.d);
+  return CS_OK;
+}
+
+int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
+                           int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,
+                           int table_width, const int32_t* lens, const int32_t* starts,
+                           int max_len, float scale, int window, void* out, void* ws,
+                           size_t ws_bytes, void* stream) {
+  if (!is_float(qt)) return CS_ERR_DTYPE;
+  cs::Mx4View c;
+  const int st = cache_view(cache, &c);
+  if (st != CS_OK) return st;
+  const int some = tokens > 0;                             // no tokens: no sequences needed
+  if (tokens < 0 || q_heads < 1 || batch < some || table_width < some || max_len < 0 || window < 0)
+    return CS_ERR_ARG;
+  if (!(scale > 0.0f) || std::isinf(scale)) return CS_ERR_ARG;
+  if (tokens == 0) return CS_OK;
+  if (!q || !table || !lens || !starts || !out || !aligned(q, float_size(qt)) ||
+      !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4))
+    return CS_ERR_ARG;
+  if (ldq < 0 || hsq < c.d || !attention_fits(c, tokens, q_heads, table_width))
+    return CS_ERR_SHAPE;
+  const AttentionPlan p = attention_plan(c, qt, tokens, q_heads, batch, table_width, max_len,
+                                          window);
+  const int group = q_heads / c.heads;
+  const int64_t rows = (int64_t)tokens * q_heads;
+  const size_t need = std::max(
+      cs_mx4_paged_attention_workspace_bytes(cache, qt, tokens, q_heads, batch, table_width,
+                                             max_len),
+      attention_part_bytes(p.splits, rows, c.d));
+  if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return CS_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int e = (int)float_size(qt);
+  const bool vec = aligned(q, 16) && (tokens == 1 || ldq * e % 16 == 0) && hsq * e % 16 == 0;
+  cs::Mx4Attention a{c, q, ldq, hsq, vec, tokens, q_heads, group, batch,
+                     cs::make_fastdiv((uint32_t)group), cs::make_fastdiv((uint32_t)c.heads),
+                     cs::make_fastdiv((uint32_t)p.tiles), table, table_width, lens, starts, scale,
+                     std::min(window, CS_MAX_Q8_LEN), out, p.splits, p.chunk, nullptr, nullptr};
+  if (p.splits > 1) {
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)p.splits * rows * c.d);
+  }
+  const int64_t blocks = p.tiles * c.heads * p.splits;
+  if (blocks > kMaxCount) return CS_ERR_SHAPE;
+  return with_float(qt, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL((cs::mx4_attention_row<T>), cs::wide_grid(blocks), dim3(64), 0, s, a);
+    return launched();
+  });
+}
+
+}  // extern "C"

@@ -9,28 +9,12 @@
 #include <cmath>
 
 #include "cs.h"
+#include "q8_api_util.h"
 #include "q8_attention.h"
 #include "q8_linear.h"
 #include "q8_rows.h"
 
 namespace {
-
-constexpr int64_t kMaxCount = 0x7FFFFFFF;
-
-size_t float_size(cs_dtype t) { return t == CS_F32 ? 4 : 2; }
-bool is_float(cs_dtype t) { return t == CS_F32 || t == CS_F16 || t == CS_BF16; }
-bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-size_t round_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
-
-int launched() { return hipGetLastError() == hipSuccess ? CS_OK : CS_ERR_DEVICE; }
-
-// f(T{}) with the C++ type of a float dtype.
-template <typename F>
-int with_float(cs_dtype t, F f) {
-  if (t == CS_F32) return f(float{});
-  if (t == CS_F16) return f(_Float16{});
-  return f(__bf16{});
-}
 
 // ---------------------------------------------------------------- rows
 template <typename T, int WPR>
@@ -130,14 +114,6 @@ int cache_view(const cs_q8_cache* c, cs::CacheView* out) {
 }
 
 // ---------------------------------------------------------------- attention
-// f(integral_constant) with the width of the kernels' registers for d channels.
-template <typename F>
-void with_width(int d, F f) {
-  if (d <= 64) f(std::integral_constant<int, 64>{});
-  else if (d <= 128) f(std::integral_constant<int, 128>{});
-  else f(std::integral_constant<int, 256>{});
-}
-
 struct AttentionPlan {
   int per;             // rows of a workgroup: 128 (attention_many) or 16 (attention_few)
   int64_t tiles;       // numbers of row tiles (find_tile)
@@ -430,7 +406,7 @@ int cs_paged_attention(const cs_q8_cache* cache, cs_dtype qt, const void* q, int
     else with_width(c.d, many);
     int r = launched();
     if (r == CS_OK && p.splits > 1) {
-      hipLaunchKernelGGL((cs::attention_join<T>), dim3((unsigned)rows), block, 0, s, a);
+      hipLaunchKernelGGL((cs::attention_join<T, cs::CacheView>), dim3((unsigned)rows), block, 0, s, a);
       r = launched();
     }
     return r;

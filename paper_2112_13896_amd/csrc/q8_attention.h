@@ -42,8 +42,9 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-struct PagedAttention {
-  CacheView c;
+template <typename View>
+struct PagedAttentionOf {
+  View c;
   const void* q;
   int64_t ldq, hsq;
   int q_vec;           // query heads start on 16 bytes
@@ -60,11 +61,14 @@ struct PagedAttention {
   float* part_o;       // [splits][tokens * q_heads][d], splits > 1
   float2* part_ml;     // [splits][tokens * q_heads]: m, l
 };
+typedef PagedAttentionOf<CacheView> PagedAttention;
 
 // Workgroups go to the eight XCDs in turn: heads vary fastest, so that the
 // tiles and parts that read one head's keys meet in few L2s (with eight heads,
 // or a multiple, in one).
-__device__ __forceinline__ bool place(const PagedAttention& a, int* head, int* tile, int* split) {
+template <typename View>
+__device__ __forceinline__ bool place(const PagedAttentionOf<View>& a, int* head, int* tile,
+                                      int* split) {
   const uint32_t id = workgroup(), rest = fdiv(id, a.by_heads);
   *head = (int)(id - rest * a.by_heads.d);
   const uint32_t s = fdiv(rest, a.by_tiles);
@@ -85,7 +89,9 @@ struct RowTile {
   int len;             // positions
 };
 
-__device__ __forceinline__ bool find_tile(const PagedAttention& a, int tile, int per, RowTile* t) {
+template <typename View>
+__device__ __forceinline__ bool find_tile(const PagedAttentionOf<View>& a, int tile, int per,
+                                          RowTile* t) {
   auto base = [&](int b, int start) { return (int)((int64_t)start * a.group / per) + b; };
   const int lane = threadIdx.x % 64;
   int b = 0;
@@ -114,8 +120,9 @@ __device__ __forceinline__ int position(const RowTile& t, int token) {
 }
 
 // Positions [lo, hi) that some row of tokens t0 .. t1 of the tile sees.
-__device__ __forceinline__ void tile_keys(const PagedAttention& a, const RowTile& t, int t0,
-                                          int t1, int* lo, int* hi) {
+template <typename View>
+__device__ __forceinline__ void tile_keys(const PagedAttentionOf<View>& a, const RowTile& t,
+                                          int t0, int t1, int* lo, int* hi) {
   const int p0 = position(t, t0), p1 = position(t, t1);
   *hi = p1 + 1;
   *lo = a.window > 0 ? max(p0 - a.window + 1, 0) : 0;
@@ -930,9 +937,10 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 // fourth part, so their loads wait for nothing but each other's turn, and the
 // four sums meet in LDS.
 constexpr int kMaxSplits = 64;
+constexpr float out_unit(const CacheView&) { return kCodeScale; }
 
-template <typename T>
-__global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
+template <typename T, typename View>
+__global__ __launch_bounds__(256) void attention_join(PagedAttentionOf<View> a) {
   __shared__ f32x4 l_y[4][64];
   const int lane = threadIdx.x % 64, d = a.c.d;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -960,7 +968,7 @@ __global__ __launch_bounds__(256) void attention_join(PagedAttention a) {
   __syncthreads();
   if (wave > 0 || 4 * lane >= d) return;
   y = l_y[0][lane] + l_y[1][lane] + l_y[2][lane] + l_y[3][lane];
-  y *= sum == 0.0f ? 0.0f : kCodeScale / sum;
+  y *= sum == 0.0f ? 0.0f : out_unit(a.c) / sum;
   typedef T t4 __attribute__((ext_vector_type(4)));
   *reinterpret_cast<t4*>(static_cast<T*>(a.out) + row * d + ch) =
       t4{(T)y[0], (T)y[1], (T)y[2], (T)y[3]};

@@ -1001,23 +1001,29 @@ class PagedCache:
     k_scale: torch.Tensor
     v_scale: torch.Tensor
 
+    _entry = "cs_"                    # its calls' names start so
+
     def __post_init__(self):
         if self.k.dim() != 4:
             raise ValueError("codes must be [pages][heads][page][d]")
-        for t, dt, shape, name in ((self.k, torch.int8, self.k.shape, "k"),
-                                   (self.v, torch.int8, self.k.shape, "v"),
-                                   (self.k_scale, torch.float32, self.k.shape[:3], "k_scale"),
-                                   (self.v_scale, torch.float32, self.k.shape[:3], "v_scale")):
+        shape = self.k.shape
+        self._hold(_lib.Q8Cache, shape, ((torch.int8, shape), (torch.int8, shape),
+                                         (torch.float32, shape[:3]), (torch.float32, shape[:3])))
+
+    def _hold(self, struct, sizes, parts):
+        """Check the four arrays and keep the C view of them."""
+        for (dt, shape), name in zip(parts, ("k", "v", "k_scale", "v_scale")):
+            t = getattr(self, name)
             if t.dtype != dt or t.shape != shape:
                 raise ValueError(f"{name} must be {dt} {list(shape)}")
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
             if t.device != self.k.device:
                 raise ValueError(f"{name} must be on {self.k.device}, as k is")
-        c = _lib.Q8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
-                         self.v_scale.data_ptr(), *self.k.shape)
+        c = struct(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                   self.v_scale.data_ptr(), *sizes)
         for name, value in (("_c", c), ("_ref", ctypes.byref(c)),
-                            *zip(("pages", "heads", "page", "d"), self.k.shape)):
+                            *zip(("pages", "heads", "page", "d"), sizes)):
             object.__setattr__(self, name, value)
 
     @classmethod
@@ -1034,23 +1040,57 @@ class PagedCache:
         return self._ref
 
 
+@dataclass(frozen=True)
+class PagedCache4(PagedCache):
+    """Keys and values of many sequences in 4 bits (cs_mx4_cache), with a power of two for every 32
+    channels.  With groups = ceil(d / 32): codes uint8 [pages][heads][page][16 groups] of keys and
+    [pages][heads][page / 4][4 groups][4][4] of values, scales uint8 [pages][heads][page][groups]
+    and [pages][heads][page / 4][groups][4]."""
+    d: int
+
+    _entry = "cs_mx4_"
+
+    def __post_init__(self):
+        if self.k.dim() != 4:
+            raise ValueError("keys' codes must be [pages][heads][page][16 groups]")
+        pages, heads, page, _ = self.k.shape
+        if page % 4 or self.d < 1:
+            raise ValueError("a page holds a multiple of four tokens, of at least one channel")
+        self._hold(_lib.Mx4Cache, (pages, heads, page, self.d),
+                   [(torch.uint8, torch.Size(t)) for t in self._shapes(pages, heads, page, self.d)])
+
+    @staticmethod
+    def _shapes(pages, heads, page, d):
+        g = -(-d // 32)
+        return ((pages, heads, page, 16 * g), (pages, heads, page // 4, 4 * g, 4, 4),
+                (pages, heads, page, g), (pages, heads, page // 4, g, 4))
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page: int, d: int, device="cuda") -> "PagedCache4":
+        return cls(*(torch.empty(t, dtype=torch.uint8, device=device)
+                     for t in cls._shapes(pages, heads, page, d)), d=d)
+
+
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Quantise k and v (float [tokens][heads][d]) into the cache's slots (int64 [tokens], slot =
-    page number * page + offset; one outside the cache leaves its token out): cs_cache_write."""
+    page number * page + offset; one outside the cache leaves its token out): cs_cache_write, or
+    cs_mx4_cache_write for a PagedCache4."""
     gpu = _gpu(k, "k")
     pk, ldk, hsk = _heads(k, "k", gpu)
     pv, ldv, hsv = _heads(v, "v", gpu)
     shape = k.shape
     if k.dtype != v.dtype or v.shape != shape or shape[1] != cache.heads or shape[2] != cache.d:
         raise ValueError(f"k and v must be of one type and [tokens][{cache.heads}][{cache.d}]")
-    _call("cs_cache_write", gpu, lib().cs_cache_write,
+    name = cache._entry + "cache_write"
+    _call(name, gpu, getattr(lib(), name),
           cache._ptr(gpu), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
           _vector(slots, "slots", torch.int64, shape[0], gpu), shape[0])
 
 
 def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
                out: tuple | None = None):
-    """(k, v), each [tokens][heads][d] of `dtype`, of the slots' tokens: cs_cache_read."""
+    """(k, v), each [tokens][heads][d] of `dtype`, of the slots' tokens: cs_cache_read, or
+    cs_mx4_cache_read for a PagedCache4."""
     gpu = _gpu(slots, "slots")
     shape = (slots.shape[0], cache.heads, cache.d)
     if out is None:
@@ -1059,7 +1099,8 @@ def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
         for t in out:
             if t.dtype != dtype or t.shape != shape:
                 raise ValueError(f"out must be {dtype} {list(shape)}")
-    _call("cs_cache_read", gpu, lib().cs_cache_read,
+    name = cache._entry + "cache_read"
+    _call(name, gpu, getattr(lib(), name),
           cache._ptr(gpu), _vector(slots, "slots", torch.int64, shape[0], gpu), shape[0],
           _float_dt(dtype), _dense(out[0], "out", gpu), _dense(out[1], "out", gpu))
     return out
@@ -1083,19 +1124,24 @@ def _attention_args(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, max
 def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
                               max_len: int | None = None) -> torch.Tensor:
     """Workspace of paged_attention for arguments of these shapes."""
-    n = lib().cs_paged_attention_workspace_bytes(
-        cache._ref, *_attention_args(q, cache, table, max_len))
+    need = getattr(lib(), cache._entry + "paged_attention_workspace_bytes")
+    n = need(cache._ref, *_attention_args(q, cache, table, max_len))
     return torch.empty((int(n),), dtype=torch.uint8, device=q.device)
 
 
 def paged_attention_plan(dtype: torch.dtype, heads: int, page: int, d: int, tokens: int,
                          q_heads: int, batch: int, table_width: int, max_len: int | None = None,
-                         window: int = 0) -> dict:
-    """How paged_attention runs these sizes (host only): cs_paged_attention_plan."""
+                         window: int = 0, bits: int = 8) -> dict:
+    """How paged_attention runs these sizes over a cache of 8 or 4 bits (host only):
+    cs_paged_attention_plan, cs_mx4_paged_attention_plan."""
+    if bits not in (8, 4):
+        raise ValueError("a cache has 8 or 4 bits")
+    struct, kind = (_lib.Q8Cache, PagedCache) if bits == 8 else (_lib.Mx4Cache, PagedCache4)
     # the cache's arrays are not touched; any aligned address stands for them
-    cache = _lib.Q8Cache(16, 16, 16, 16, 1, heads, page, d)
+    cache = struct(16, 16, 16, 16, 1, heads, page, d)
     info = (ctypes.c_int64 * 6)()
-    check("cs_paged_attention_plan", lib().cs_paged_attention_plan(
+    name = kind._entry + "paged_attention_plan"
+    check(name, getattr(lib(), name)(
         ctypes.byref(cache), _float_dt(dtype), tokens, q_heads, batch, table_width,
         0 if max_len is None else min(int(max_len), _INT_MAX), min(window, _INT_MAX), info))
     return dict(zip(("rows", "parts", "part", "wavefronts", "workgroups", "bytes"), info))
@@ -1106,7 +1152,7 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
                     max_len: int | None = None, ws: torch.Tensor | None = None,
                     out: torch.Tensor | None = None) -> torch.Tensor:
     """Causal attention of each sequence's new tokens over the cache that already holds them
-    (cs_paged_attention).  q float [tokens][q_heads][d]; table int32 [batch][pages] page numbers;
+    (cs_paged_attention, or cs_mx4_paged_attention for a PagedCache4).  q float [tokens][q_heads][d]; table int32 [batch][pages] page numbers;
     lens int32 [batch] positions with the new ones; starts int32 [batch + 1] first new token of
     each sequence in q.  scale: 1 / sqrt(d) by default.  window: positions seen, 0 for all.
     max_len: the longest of lens if the caller knows it (a hint for how the work is split)."""
@@ -1119,13 +1165,238 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
         out = q.new_empty(q.shape)
     elif out.dtype != q.dtype or out.shape != q.shape:
         raise ValueError("out must be of q's type and shape")
-    L = lib()
-    ws, pws, nws = _ws(ws, lambda: L.cs_paged_attention_workspace_bytes(
+    L, name = lib(), cache._entry + "paged_attention"
+    ws, pws, nws = _ws(ws, lambda: getattr(L, name + "_workspace_bytes")(
         cache._ref, qt, tokens, q_heads, b, width, ml), q.device, gpu)
-    _call("cs_paged_attention", gpu, L.cs_paged_attention,
+    _call(name, gpu, getattr(L, name),
           cache._ptr(gpu), qt, pq, ldq, hsq, tokens, q_heads, b, _dense(table, "table", gpu), width,
           _vector(lens, "lens", torch.int32, b, gpu),
           _vector(starts, "starts", torch.int32, b + 1, gpu), ml,
           1.0 / math.sqrt(cache.d) if scale is None else scale, window, _dense(out, "out", gpu),
           pws, nws)
     return out
+
+
+# ------------------------------------------------- rotary positions
+@dataclass(frozen=True)
+class Rotary:
+    """Rotary positions of the first `rot` channels of a head: their frequencies, as fractions of a
+    turn a position times 2^64 (turns int64 [rot / 2], on the GPU), and what the results are
+    multiplied by.  make() forms the usual ones."""
+    turns: torch.Tensor
+    rot: int
+    interleaved: bool = False
+    amplitude: float = 1.0
+
+    def __post_init__(self):
+        if self.rot < 2 or self.rot % 2:
+            raise ValueError("rot must be even and at least 2")
+        if self.turns.dtype != torch.int64 or self.turns.shape != (self.rot // 2,) or \
+                not self.turns.is_contiguous():
+            raise ValueError(f"turns must be torch.int64 [{self.rot // 2}]")
+        if not math.isfinite(self.amplitude):
+            raise ValueError("amplitude must be finite")
+
+    @classmethod
+    def of(cls, frequencies, interleaved: bool = False, amplitude: float = 1.0,
+           device="cuda") -> "Rotary":
+        """Of these frequencies (radians a position, 64 bits)."""
+        turns = []
+        for f in frequencies:
+            t = float(f) / (2 * math.pi)
+            if not math.isfinite(t):
+                raise ValueError("a frequency is not finite")
+            n = int(math.ldexp(t - math.floor(t), 64)) % 2 ** 64
+            turns.append(n - 2 ** 64 if n >= 2 ** 63 else n)
+        return cls(torch.tensor(turns, dtype=torch.int64, device=device), 2 * len(turns),
+                   bool(interleaved), float(amplitude))
+
+    @classmethod
+    def make(cls, rot: int, base: float = 10000.0, *, interleaved: bool = False,
+             scaling: str = "none", device="cuda", **how) -> "Rotary":
+        """With the frequencies of rotary_frequencies(rot, base, scaling, **how)."""
+        f, amplitude = rotary_frequencies(rot, base, scaling, **how)
+        return cls.of(f, interleaved, amplitude, device)
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", *,
+                       factor: float = 1.0, original: int = 0, low: float = 1.0,
+                       high: float = 0.0):
+    """(frequencies float64 [rot / 2] in radians a position, amplitude): base^(-2 i / rot), scaled
+    for contexts `factor` times longer:
+
+      none    as they are
+      linear  all divided by factor
+      base    the base times factor^(rot / (rot - 2)): the lowest frequency is divided by factor,
+              the highest kept
+      bands   by their turns over `original` positions: kept from `high` (4) turns on, divided up
+              to `low` (1), mixed in proportion to the turns between
+      ramp    the same with `high` 32, mixed in proportion to the place among the frequencies,
+              between whole places; amplitude 0.1 ln(factor) + 1
+    """
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be even and at least 2")
+    if not base > 1 or not factor > 0:
+        raise ValueError("base must be more than 1 and factor more than 0")
+    if scaling == "base" and rot > 2:
+        base = base * factor ** (rot / (rot - 2))
+    i = np.arange(rot // 2)
+    f = base ** (-2.0 * i / rot)
+    if scaling in ("none", "base"):
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling not in ("bands", "ramp"):
+        raise ValueError(f"no such scaling: {scaling}")
+    high = high or (4.0 if scaling == "bands" else 32.0)
+    if original < 1 or not 0 < low < high:
+        raise ValueError("bands and ramp take the original length and 0 < low < high")
+    if scaling == "bands":
+        keep = (original * f / (2 * math.pi) - low) / (high - low)
+    else:
+        def place(turns):
+            return rot * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base))
+        first = max(math.floor(place(high)), 0)
+        last = min(math.ceil(place(low)), rot - 1)
+        keep = 1.0 - (i - first) / max(last - first, 0.001)
+    keep = np.clip(keep, 0.0, 1.0)
+    amplitude = 0.1 * math.log(factor) + 1.0 if scaling == "ramp" and factor > 1 else 1.0
+    return keep * f + (1.0 - keep) * (f / factor), amplitude
+
+
+def rotary(rot: Rotary, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, *,
+           inverse: bool = False, out=None):
+    """q and k (float [tokens][heads][d], strided) turned to their tokens' positions (int32
+    [tokens]; the rows of a token below 0 are copied): cs_rotary.  Returns q, or (q, k); `out`: the
+    tensors to write, which may be the inputs.  inverse: turned back, the gradient of a call
+    without it."""
+    gpu = _gpu(q, "q")
+    xs = (q,) if k is None else (q, k)
+    tokens, _, d = q.shape if q.dim() == 3 else (0, 0, 0)
+    ptrs = [_heads(t, name, gpu) for t, name in zip(xs, ("q", "k"))]
+    if k is not None and (k.dtype != q.dtype or k.shape[0] != tokens or k.shape[2] != d):
+        raise ValueError(f"k must be {q.dtype} [{tokens}][heads][{d}]")
+    if out is None:
+        ys = tuple(t.new_empty(t.shape) for t in xs)
+    else:
+        ys = (out,) if k is None else tuple(out)
+        if len(ys) != len(xs):
+            raise ValueError("out must be as many tensors as are turned")
+        for x, y in zip(xs, ys):
+            if y.dtype != x.dtype or y.shape != x.shape:
+                raise ValueError("out must be of the inputs' types and shapes")
+    outs = [_heads(t, "out", gpu) for t in ys]
+    heads = [t.shape[1] for t in xs]
+    if max(heads) > _INT_MAX or d > _INT_MAX:
+        raise ValueError("q or k has a dimension over 2^31 - 1")
+    if k is None:
+        ptrs.append((None, 0, d))
+        outs.append((None, 0, d))
+        heads.append(0)
+    two, two64 = ctypes.c_void_p * 2, ctypes.c_int64 * 2
+    px, ldx, hsx = zip(*ptrs)
+    py, ldy, hsy = zip(*outs)
+    _call("cs_rotary", gpu, lib().cs_rotary,
+          _float_dt(q.dtype), _vector(rot.turns, "turns", torch.int64, rot.rot // 2, gpu), rot.rot,
+          int(rot.interleaved), rot.amplitude, int(bool(inverse)),
+          _vector(positions, "positions", torch.int32, tokens, gpu), tokens, d,
+          (ctypes.c_int * 2)(*heads), two(*px), two64(*ldx), two64(*hsx), two(*py), two64(*ldy),
+          two64(*hsy))
+    return ys[0] if k is None else ys
+
+
+# ------------------------------------------------- steps planned on the GPU
+@dataclass(frozen=True)
+class DevicePool:
+    """A cache's pages and the sequences that hold them, on the GPU (cs_page_pool): table int32
+    [sequences][width], lengths int32 [sequences], free int32 [pages], a stack of which count int32
+    [1] are on it, and the page's tokens."""
+    table: torch.Tensor
+    lengths: torch.Tensor
+    free: torch.Tensor
+    count: torch.Tensor
+    page: int
+
+    def __post_init__(self):
+        if self.table.dim() != 2:
+            raise ValueError("table must be [sequences][width]")
+        sequences, width = self.table.shape
+        for name, shape in (("table", self.table.shape), ("lengths", (sequences,)),
+                            ("free", (self.free.numel(),)), ("count", (1,))):
+            t = getattr(self, name)
+            if t.dtype != torch.int32 or t.shape != shape:
+                raise ValueError(f"{name} must be torch.int32 {list(shape)}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            if t.device != self.table.device:
+                raise ValueError(f"{name} must be on {self.table.device}, as table is")
+        if max(sequences, width, self.free.numel(), self.page) > _INT_MAX:
+            raise ValueError("the pool has a dimension over 2^31 - 1")
+        marks = torch.full_like(self.lengths, _INT_MAX)
+        c = _lib.PagePool(self.table.data_ptr(), self.lengths.data_ptr(), self.free.data_ptr(),
+                          self.count.data_ptr(), marks.data_ptr(), sequences, width,
+                          self.free.numel(), self.page)
+        for name, value in (("marks", marks), ("_c", c), ("_ref", ctypes.byref(c))):
+            object.__setattr__(self, name, value)
+
+    @classmethod
+    def empty(cls, sequences: int, width: int, pages: int, page: int, device="cuda") -> "DevicePool":
+        """No sequence holds anything; the stack gives page 0 first."""
+        def zeros(*shape):
+            return torch.zeros(shape, dtype=torch.int32, device=device)
+        free = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device)
+        return cls(zeros(sequences, width) - 1, zeros(sequences), free, zeros(1) + pages, page)
+
+    def _ptr(self, gpu: int):
+        _on(self.table, "the pool", gpu)
+        return self._ref
+
+
+def plan_step_workspace(batch: int, device="cuda") -> torch.Tensor:
+    """Workspace of plan_step for this many entries."""
+    return torch.empty((int(lib().cs_plan_step_workspace_bytes(batch)),), dtype=torch.uint8,
+                       device=device)
+
+
+def plan_step(pool: DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: int,
+              width: int | None = None, ws: torch.Tensor | None = None, out: tuple | None = None):
+    """Pages for the new[i] tokens that entry i brings to sequence seqs[i] (int32 [batch]; -1 names
+    none), and the step (cs_plan_step): (table int32 [batch][width], lens int32 [batch], starts
+    int32 [batch + 1], slots int64 [tokens], positions int32 [tokens], status int32 [2]).  `tokens`:
+    the most that the step may have; width: the pool's by default.  status is 0, 0 where the step
+    was planned; otherwise nothing was taken, and the step is empty."""
+    gpu = _gpu(seqs, "seqs")
+    batch = seqs.numel()
+    width = pool.table.shape[1] if width is None else width
+    if max(batch, width, tokens) > _INT_MAX:
+        raise ValueError("seqs, width or tokens is over 2^31 - 1")
+    if batch < 1 or width < 1 or tokens < 0:
+        raise ValueError("a step has at least one entry, a column and no fewer than 0 tokens")
+    i32 = torch.int32
+    shapes = ((i32, (batch, width)), (i32, (batch,)), (i32, (batch + 1,)), (torch.int64, (tokens,)),
+              (i32, (tokens,)), (i32, (2,)))
+    if out is None:
+        out = tuple(seqs.new_empty(shape, dtype=dt) for dt, shape in shapes)
+    else:
+        for t, (dt, shape) in zip(out, shapes, strict=True):
+            if t.dtype != dt or t.shape != shape:
+                raise ValueError(f"out must be {[(str(dt), list(shape)) for dt, shape in shapes]}")
+    L = lib()
+    ws, pws, nws = _ws(ws, lambda: L.cs_plan_step_workspace_bytes(batch), seqs.device, gpu)
+    table, lens, starts, slots, positions, status = (_dense(t, "out", gpu) for t in out)
+    _call("cs_plan_step", gpu, L.cs_plan_step, pool._ptr(gpu),
+          _vector(seqs, "seqs", i32, batch, gpu), _vector(new, "new", i32, batch, gpu), batch, table,
+          width, lens, starts, slots, positions, tokens, status, pws, nws)
+    return out
+
+
+def pool_truncate(pool: DevicePool, seqs: torch.Tensor, lens: torch.Tensor | None = None) -> None:
+    """Cut sequences seqs (int32 [batch]) to lens positions (int32 [batch]; None: they have ended);
+    their other pages go back onto the stack (cs_pool_truncate)."""
+    gpu = _gpu(seqs, "seqs")
+    batch = seqs.numel()
+    if batch > _INT_MAX:
+        raise ValueError("seqs is over 2^31 - 1")
+    _call("cs_pool_truncate", gpu, lib().cs_pool_truncate, pool._ptr(gpu),
+          _vector(seqs, "seqs", torch.int32, batch, gpu),
+          _vector(lens, "lens", torch.int32, batch, gpu), batch)

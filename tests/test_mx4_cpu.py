@@ -1,0 +1,371 @@
+"""The 4-bit cache, attention over it, rotary positions and step plans without a GPU: refusals of
+the C ABI and of the Python wrappers (every check runs before the first HIP call), workspace sizes,
+frequencies, and the oracle's own definitions on hand-made rows."""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as o4
+from paper_2112_13896_amd import _lib, ops
+from paper_2112_13896_amd._lib import (CS_BF16, CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE,
+                                       CS_ERR_WORKSPACE, CS_F32, CS_I8, CS_I32, CS_OK)
+from paper_2112_13896_amd.attention import AttentionLayer, Sequence, Step
+from tests.test_q8_devices_cpu import at, rec  # noqa: F401  (rec: fixture)
+
+P = 0x100000            # an aligned address that must never be dereferenced
+
+
+@pytest.fixture(scope="module")
+def L():
+    return _lib.lib()
+
+
+def _cache(k=P, v=P, ks=P, vs=P, pages=4, heads=2, page=16, d=64):
+    return ctypes.byref(_lib.Mx4Cache(k, v, ks, vs, pages, heads, page, d))
+
+
+def test_cache_refusals(L):
+    def write(c=None, xt=CS_F32, k=P, ldk=128, hsk=64, v=P, ldv=128, hsv=64, slots=P, tokens=3):
+        return L.cs_mx4_cache_write(c or _cache(), xt, k, ldk, hsk, v, ldv, hsv, slots, tokens,
+                                    None)
+
+    def read(c=None, slots=P, tokens=3, yt=CS_F32, k=P, v=P):
+        return L.cs_mx4_cache_read(c or _cache(), slots, tokens, yt, k, v, None)
+    for f in (write, read):
+        for kw in (dict(k=0), dict(v=0), dict(ks=0), dict(vs=0), dict(pages=0), dict(heads=0),
+                   dict(page=0), dict(d=0), dict(k=P + 8), dict(v=P + 4), dict(ks=P + 2),
+                   dict(vs=P + 1)):
+            assert f(_cache(**kw)) == CS_ERR_ARG, kw
+        for kw in (dict(d=24), dict(d=8), dict(d=272), dict(page=8), dict(page=48),
+                   dict(page=2048), dict(pages=1 << 27, page=16)):
+            assert f(_cache(**kw)) == CS_ERR_SHAPE, kw
+        assert f(tokens=1 << 31) == CS_ERR_SHAPE
+        for kw in (dict(k=0), dict(v=0), dict(slots=0), dict(tokens=-1), dict(slots=P + 4)):
+            assert f(**kw) == CS_ERR_ARG, kw
+        assert f(tokens=0, k=0, v=0, slots=0) == CS_OK
+    assert write(xt=CS_I8) == CS_ERR_DTYPE and read(yt=CS_I32) == CS_ERR_DTYPE
+    for kw in (dict(ldk=-1), dict(ldv=-1), dict(hsk=63), dict(hsv=63)):
+        assert write(**kw) == CS_ERR_SHAPE, kw
+    assert write(xt=CS_BF16, k=P + 1) == CS_ERR_ARG and read(k=P + 8) == CS_ERR_ARG
+
+
+def test_attention_refusals(L):
+    def call(c=None, qt=CS_BF16, q=P, ldq=256, hsq=64, tokens=5, q_heads=4, batch=2, table=P,
+             width=3, lens=P, starts=P, max_len=0, scale=0.1, window=0, out=P, ws=P, n=1 << 40):
+        return L.cs_mx4_paged_attention(c or _cache(), qt, q, ldq, hsq, tokens, q_heads, batch,
+                                        table, width, lens, starts, max_len, scale, window, out,
+                                        ws, n, None)
+    for qt in (CS_I8, CS_I32, 11):
+        assert call(qt=qt) == CS_ERR_DTYPE
+    for kw in (dict(q=0), dict(table=0), dict(lens=0), dict(starts=0), dict(out=0), dict(tokens=-1),
+               dict(q_heads=0), dict(batch=0), dict(width=0), dict(max_len=-1), dict(window=-1),
+               dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")),
+               dict(scale=float("nan")), dict(q=P + 1), dict(out=P + 2), dict(table=P + 1),
+               dict(lens=P + 2), dict(starts=P + 3)):
+        assert call(**kw) == CS_ERR_ARG, kw
+    for kw in (dict(q_heads=3), dict(ldq=-1), dict(hsq=63), dict(tokens=1 << 30),
+               dict(width=1 << 27)):
+        assert call(**kw) == CS_ERR_SHAPE, kw
+    assert call(_cache(page=20)) == CS_ERR_SHAPE and call(_cache(k=0)) == CS_ERR_ARG
+    assert call(tokens=0, q=0, batch=0, width=0, table=0) == CS_OK
+    big = dict(tokens=1, batch=1, width=4096)
+    need = L.cs_mx4_paged_attention_workspace_bytes(_cache(), CS_BF16, 1, 4, 1, 4096, 0)
+    if need:
+        assert call(**big, n=need - 1) == CS_ERR_WORKSPACE
+        assert call(**big, ws=0) == CS_ERR_WORKSPACE
+        assert call(**big, ws=P + 8) == CS_ERR_WORKSPACE
+    for args in ((CS_I8, 1, 4, 1, 4, 0), (CS_BF16, 0, 4, 1, 4, 0), (CS_BF16, 1, 3, 1, 4, 0),
+                 (CS_BF16, 1, 4, 0, 4, 0), (CS_BF16, 1, 4, 1, 0, 0), (CS_BF16, 1, 4, 1, 1 << 30, 0)):
+        assert L.cs_mx4_paged_attention_workspace_bytes(_cache(), *args) == 0
+
+
+def test_workspace_is_enough_for_any_window_and_shorter_axis(L):
+    """The parts of every window and of every smaller table or max_len fit what the whole takes."""
+    info = (ctypes.c_int64 * 6)()
+    for d, heads, q_heads in ((64, 2, 8), (128, 8, 32), (256, 1, 1)):
+        c = _cache(d=d, heads=heads, page=64)
+        for dt in (CS_F32, CS_BF16):
+            for tokens, batch in ((1, 1), (5, 3), (64, 64), (300, 2)):
+                for width in (1, 16, 100, 1024, 1500):
+                    need = L.cs_mx4_paged_attention_workspace_bytes(c, dt, tokens, q_heads, batch,
+                                                                    width, 0)
+                    for less in (width, max(1, width - 1), max(1, width // 3)):
+                        for max_len in (0, 1, less * 64 - 5, less * 64, less * 64 + 1000):
+                            for window in (0, 1, 100, 1000, 4097, 50000):
+                                assert L.cs_mx4_paged_attention_plan(
+                                    c, dt, tokens, q_heads, batch, less, max_len, window,
+                                    info) == CS_OK
+                                parts, part, size = info[1], info[2], info[5]
+                                assert size <= need
+                                assert parts >= 1 and (parts == 1 or part % 64 == 0)
+
+
+def _pool(table=P, lengths=P, free=P, count=P, marks=P, sequences=4, width=5, pages=9, page=16):
+    return ctypes.byref(_lib.PagePool(table, lengths, free, count, marks, sequences, width, pages,
+                                      page))
+
+
+def test_plan_refusals(L):
+    def plan(pool=None, seqs=P, new=P, batch=3, table=P, width=4, lens=P, starts=P, slots=P,
+             positions=P, tokens=7, status=P, ws=P, n=1 << 30):
+        return L.cs_plan_step(pool or _pool(), seqs, new, batch, table, width, lens, starts, slots,
+                              positions, tokens, status, ws, n, None)
+
+    def cut(pool=None, seqs=P, lens=0, batch=3):
+        return L.cs_pool_truncate(pool or _pool(), seqs, lens, batch, None)
+    for f in (plan, cut):
+        for kw in (dict(table=0), dict(lengths=0), dict(free=0), dict(count=0), dict(marks=0),
+                   dict(sequences=0), dict(width=0), dict(pages=0), dict(page=0),
+                   dict(table=P + 2), dict(marks=P + 1)):
+            assert f(_pool(**kw)) == CS_ERR_ARG, kw
+        for kw in (dict(page=8), dict(page=24), dict(page=2048), dict(pages=1 << 27),
+                   dict(sequences=1 << 20, width=1 << 12), dict(width=(1 << 26) + 1)):
+            assert f(_pool(**kw)) == CS_ERR_SHAPE, kw
+        for kw in (dict(seqs=0), dict(seqs=P + 1), dict(batch=-1), dict(lens=P + 2)):
+            assert f(**kw) == CS_ERR_ARG, kw
+        assert f(batch=(1 << 20) + 1) == CS_ERR_SHAPE
+    for kw in (dict(batch=0), dict(new=0), dict(table=0), dict(width=0), dict(lens=0),
+               dict(starts=0), dict(slots=0), dict(positions=0), dict(tokens=-1), dict(status=0),
+               dict(slots=P + 4), dict(new=P + 2), dict(starts=P + 1), dict(status=P + 2)):
+        assert plan(**kw) == CS_ERR_ARG, kw
+    for kw in (dict(width=(1 << 26) + 1), dict(tokens=1 << 31), dict(batch=1 << 20, width=1 << 12)):
+        assert plan(**kw) == CS_ERR_SHAPE, kw
+    need = L.cs_plan_step_workspace_bytes(3)
+    for kw in (dict(ws=0), dict(ws=P + 8), dict(n=need - 1)):
+        assert plan(**kw) == CS_ERR_WORKSPACE, kw
+    assert need and not L.cs_plan_step_workspace_bytes(0)
+    assert not L.cs_plan_step_workspace_bytes((1 << 20) + 1)
+    assert cut(batch=0, seqs=0) == CS_OK
+
+
+def test_rotary_refusals(L):
+    def call(xt=CS_F32, turns=P, rot=32, amplitude=1.0, positions=P, tokens=3, d=32, heads=(2, 1),
+             x=(P, P), ldx=(96, 96), hsx=(32, 32), y=(2 * P, 2 * P), ldy=(96, 96), hsy=(32, 32)):
+        vp, i64 = ctypes.c_void_p * 2, ctypes.c_int64 * 2
+        return L.cs_rotary(xt, turns, rot, 0, amplitude, 0, positions, tokens, d,
+                           (ctypes.c_int * 2)(*heads), vp(*x), i64(*ldx), i64(*hsx), vp(*y),
+                           i64(*ldy), i64(*hsy), None)
+    for xt in (CS_I8, CS_I32, 9):
+        assert call(xt=xt) == CS_ERR_DTYPE
+    for kw in (dict(turns=0), dict(turns=P + 4), dict(positions=0), dict(positions=P + 2),
+               dict(tokens=-1), dict(d=0), dict(heads=(-1, 2)), dict(x=(0, P)), dict(y=(P, 0)),
+               dict(x=(P, P + 2)), dict(amplitude=float("nan")), dict(amplitude=float("inf")),
+               dict(y=(P, P), ldy=(64, 96)), dict(y=(P, P), ldy=(200, 96), hsy=(64, 32))):
+        assert call(**kw) == CS_ERR_ARG, kw
+    for kw in (dict(rot=0), dict(rot=1), dict(rot=31), dict(rot=34), dict(d=1026, rot=2),
+               dict(hsx=(31, 32)), dict(hsy=(32, 31)), dict(ldx=(-1, 96)), dict(ldy=(96, 16)),
+               dict(heads=(65535, 1)), dict(tokens=1 << 30)):
+        assert call(**kw) == CS_ERR_SHAPE, kw
+    assert call(tokens=0, turns=0, positions=0, x=(0, 0), y=(0, 0)) == CS_OK
+    assert call(heads=(0, 0), x=(0, 0), y=(0, 0)) == CS_OK
+    assert L.cs_rotary(CS_F32, P, 32, 0, 1.0, 0, P, 3, 32, None, None, None, None, None, None, None,
+                       None) == CS_ERR_ARG
+
+
+def cache4(*gpus):
+    gpus = gpus if len(gpus) > 1 else gpus * 4
+    return ops.PagedCache4(*(at(g, *s, dtype=torch.uint8) for g, s in zip(
+        gpus, ops.PagedCache4._shapes(4, 2, 16, 32))), d=32)
+
+
+def pool(*gpus):
+    gpus = gpus if len(gpus) > 1 else gpus * 4
+    i32 = torch.int32
+    return ops.DevicePool(at(gpus[0], 4, 3, dtype=i32), at(gpus[1], 4, dtype=i32),
+                          at(gpus[2], 9, dtype=i32), at(gpus[3], 1, dtype=i32), 16)
+
+
+def calls(gpu):
+    """name -> (function of its tensors, the tensors) of a good call on a GPU."""
+    i32, i64, u8 = torch.int32, torch.int64, torch.uint8
+
+    def plan(pool, seqs, new, ws, **out):
+        return ops.plan_step(pool, seqs, new, 5, ws=ws, out=tuple(out.values()))
+
+    def rot(turns, positions, q, k, a, b):
+        return ops.rotary(ops.Rotary(turns, 16), positions, q, k, out=(a, b))
+    return {
+        "mx4_cache_write": (lambda cache, k, v, slots: ops.cache_write(cache, k, v, slots),
+                            dict(cache=cache4(gpu), k=at(gpu, 3, 2, 32), v=at(gpu, 3, 2, 32),
+                                 slots=at(gpu, 3, dtype=i64))),
+        "mx4_cache_read": (lambda cache, slots, a, b: ops.cache_read(cache, slots, torch.float32,
+                                                                     out=(a, b)),
+                           dict(cache=cache4(gpu), slots=at(gpu, 3, dtype=i64),
+                                a=at(gpu, 3, 2, 32), b=at(gpu, 3, 2, 32))),
+        "mx4_paged_attention": (lambda q, cache, table, lens, starts, ws, out: ops.paged_attention(
+            q, cache, table, lens, starts, ws=ws, out=out),
+            dict(q=at(gpu, 3, 4, 32), cache=cache4(gpu), table=at(gpu, 2, 3, dtype=i32),
+                 lens=at(gpu, 2, dtype=i32), starts=at(gpu, 3, dtype=i32),
+                 ws=at(gpu, 64, dtype=u8), out=at(gpu, 3, 4, 32))),
+        "rotary": (rot, dict(turns=at(gpu, 8, dtype=i64), positions=at(gpu, 3, dtype=i32),
+                             q=at(gpu, 3, 4, 32), k=at(gpu, 3, 2, 32), a=at(gpu, 3, 4, 32),
+                             b=at(gpu, 3, 2, 32))),
+        "plan_step": (plan, dict(pool=pool(gpu), seqs=at(gpu, 2, dtype=i32),
+                                 new=at(gpu, 2, dtype=i32), ws=at(gpu, 256, dtype=u8),
+                                 table=at(gpu, 2, 3, dtype=i32), lens=at(gpu, 2, dtype=i32),
+                                 starts=at(gpu, 3, dtype=i32), slots=at(gpu, 5, dtype=i64),
+                                 positions=at(gpu, 5, dtype=i32), status=at(gpu, 2, dtype=i32))),
+        "pool_truncate": (lambda pool, seqs, lens: ops.pool_truncate(pool, seqs, lens),
+                          dict(pool=pool(gpu), seqs=at(gpu, 2, dtype=i32),
+                               lens=at(gpu, 2, dtype=i32))),
+    }
+
+
+NAMES = list(calls(0))
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("gpu", [0, 1])
+def test_the_tensors_gpu_is_used(rec, name, gpu):  # noqa: F811
+    f, tensors = calls(gpu)[name]
+    f(**tensors)
+    assert [c[0] for c in rec.calls] == ["cs_" + name]
+    assert rec.calls[0][1][-1] == 1000 + gpu                  # the stream is the last argument
+    assert rec.entered == ([gpu] if gpu else [])
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("other", [-1, 1])
+def test_a_tensor_elsewhere_is_refused(rec, name, other):  # noqa: F811
+    f, tensors = calls(0)[name]
+    for arg, t in tensors.items():
+        made = {"cache": cache4, "pool": pool}.get(arg)
+        moved = made(other) if made else at(other, *t.shape, dtype=t.dtype)
+        with pytest.raises(ValueError):
+            f(**{**tensors, arg: moved})
+    assert not rec.calls
+
+
+@pytest.mark.parametrize("which", [1, 2, 3])
+def test_a_cache_and_a_pool_lie_on_one_device(which):
+    gpus = [0, 0, 0, 0]
+    gpus[which] = 1
+    for made in (cache4, pool):
+        with pytest.raises(ValueError):
+            made(*gpus)
+
+
+def test_wrapper_refusals(rec):  # noqa: F811
+    i32, i64, u8 = torch.int32, torch.int64, torch.uint8
+    shapes = ops.PagedCache4._shapes(4, 2, 16, 32)
+    for i in range(4):
+        bad = [torch.zeros(s, dtype=u8) for s in shapes]
+        bad[i] = torch.zeros(shapes[i], dtype=torch.int8)
+        with pytest.raises(ValueError):
+            ops.PagedCache4(*bad, d=32)
+        bad[i] = torch.zeros((3, *shapes[i][1:]), dtype=u8)
+        with pytest.raises(ValueError):
+            ops.PagedCache4(*bad, d=32)
+    good = [torch.zeros(s, dtype=u8) for s in shapes]
+    for d in (0, -16, 33, 64):
+        with pytest.raises(ValueError):
+            ops.PagedCache4(*good, d=d)
+    with pytest.raises(ValueError):
+        ops.PagedCache4(good[0][0], *good[1:], d=32)
+    f, t = calls(0)["mx4_cache_write"]
+    for name, x in (("k", at(0, 3, 2, 48)), ("k", at(0, 3, 3, 32)), ("v", at(0, 2, 2, 32)),
+                    ("v", at(0, 3, 2, 32, dtype=torch.float16)), ("slots", at(0, 3, dtype=i32))):
+        with pytest.raises(ValueError):
+            f(**{**t, name: x})
+    f, t = calls(0)["rotary"]
+    for name, x in (("turns", at(0, 8)), ("turns", at(0, 9, dtype=i64)), ("q", at(0, 4, 32)),
+                    ("k", at(0, 4, 2, 32)), ("k", at(0, 3, 2, 16)),
+                    ("k", at(0, 3, 2, 32, dtype=torch.float16)), ("a", at(0, 3, 2, 32)),
+                    ("positions", at(0, 3, dtype=i64)), ("positions", at(0, 4, dtype=i32)),
+                    ("q", at(0, 3, 32, 4).transpose(1, 2))):
+        with pytest.raises(ValueError):
+            f(**{**t, name: x})
+    with pytest.raises(TypeError):
+        ops.rotary(ops.Rotary(at(0, 8, dtype=i64), 16), at(0, 3, dtype=i32),
+                   at(0, 3, 2, 32, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        ops.rotary(ops.Rotary(at(0, 8, dtype=i64), 16), at(0, 3, dtype=i32), at(0, 3, 2, 32),
+                   at(0, 3, 2, 32), out=(at(0, 3, 2, 32),))
+    f, t = calls(0)["plan_step"]
+    for name, x in (("new", at(0, 3, dtype=i32)), ("seqs", at(0, 2, dtype=i64)),
+                    ("table", at(0, 2, 4, dtype=i32)), ("starts", at(0, 2, dtype=i32)),
+                    ("slots", at(0, 5, dtype=i32)), ("positions", at(0, 4, dtype=i32))):
+        with pytest.raises(ValueError):
+            f(**{**t, name: x})
+    for more in (dict(tokens=-1), dict(tokens=2 ** 31), dict(tokens=5, width=0),
+                 dict(tokens=5, width=2 ** 32)):
+        with pytest.raises(ValueError):
+            ops.plan_step(t["pool"], t["seqs"], t["new"], **more)
+    with pytest.raises(ValueError):
+        ops.plan_step(t["pool"], t["seqs"][:0], t["new"][:0], 5)
+    for bad in (dict(table=at(0, 4, 3)), dict(lengths=at(0, 3, dtype=i32)),
+                dict(count=at(0, 2, dtype=i32)), dict(table=at(0, 12, dtype=i32))):
+        parts = dict(table=at(0, 4, 3, dtype=i32), lengths=at(0, 4, dtype=i32),
+                     free=at(0, 9, dtype=i32), count=at(0, 1, dtype=i32))
+        with pytest.raises(ValueError):
+            ops.DevicePool(**{**parts, **bad}, page=16)
+    with pytest.raises(ValueError):
+        ops.paged_attention_plan(torch.float32, 2, 16, 32, 1, 2, 1, 1, bits=5)
+    assert not rec.calls
+
+
+def test_frequencies():
+    f, a = ops.rotary_frequencies(8, 10000.0)
+    assert np.allclose(f, [1, 0.1, 0.01, 0.001], rtol=1e-15) and a == 1
+    g, a = ops.rotary_frequencies(8, 10000.0, "linear", factor=4.0)
+    assert np.allclose(g, f / 4, rtol=1e-15) and a == 1
+    g, a = ops.rotary_frequencies(8, 10000.0, "base", factor=4.0)
+    assert g[0] == 1 and math.isclose(g[-1], f[-1] / 4, rel_tol=1e-12) and a == 1
+    # 1000 positions: 159, 16, 1.6 and 0.16 turns; kept, kept, (1.6 - 1) / 3 kept, divided
+    g, a = ops.rotary_frequencies(8, 10000.0, "bands", factor=4.0, original=1000)
+    keep = (10 / (2 * math.pi) - 1) / 3
+    assert np.allclose(g, [1, 0.1, 0.01 * (keep + (1 - keep) / 4), 0.001 / 4], rtol=1e-12) and a == 1
+    # 32 turns at place 0.70, one at 2.20: kept up to 0, divided from 3 on, thirds between
+    g, a = ops.rotary_frequencies(8, 10000.0, "ramp", factor=4.0, original=1000)
+    want = f * (1 - np.arange(4) / 3) + f / 4 * (np.arange(4) / 3)
+    assert np.allclose(g, want, rtol=1e-12) and math.isclose(a, 0.1 * math.log(4) + 1)
+    for bad in (dict(rot=7), dict(rot=0), dict(rot=8, base=1.0), dict(rot=8, factor=0.0),
+                dict(rot=8, scaling="other"), dict(rot=8, scaling="bands"),
+                dict(rot=8, scaling="ramp", original=100, low=5.0, high=2.0)):
+        with pytest.raises(ValueError):
+            ops.rotary_frequencies(**bad)
+    with pytest.raises(ValueError):
+        ops.Rotary.of([float("nan")], device="cpu")
+    with pytest.raises(ValueError):
+        ops.Rotary.of([1.0], amplitude=float("inf"), device="cpu")
+    r = ops.Rotary.of([math.pi / 2, -math.pi / 2, 4 * math.pi], device="cpu")
+    assert r.rot == 6 and r.turns.tolist() == [2 ** 62, -2 ** 62, 0]
+
+
+def test_oracle_codes():
+    """By hand: 7 is the largest of its scale, the next number doubles it; ties go to the even
+    code; both ends."""
+    def row(*head):
+        x = np.zeros(32)
+        x[:len(head)] = head
+        code, scale = o4.quantise(x)
+        return o4.values(code, scale)[:len(head)].tolist(), int(scale[0])
+    assert row(7, 5, 3.5, 2.5, 1.75, 1.25, .75, .25) == ([6, 4, 4, 2, 2, 1, 1, 0], 127)
+    assert row(7.001, 1.0, -3.0) == ([8, 1, -3], 128)
+    assert row(3.5, -0.1) == ([3, 0], 126)
+    assert row(0.0) == ([0], 67) and row(2.0 ** -62) == ([0], 67)
+    assert row(2.0 ** -61) == ([2.0 ** -61], 67)
+    assert row(1e30) == ([6 * 2.0 ** 60], 187)
+    code, scale = o4.quantise(np.array([1.0] * 40 + [np.inf]))
+    assert not code.any() and scale.tolist() == [255, 255]
+
+
+def test_layer_refusals():
+    w = [torch.zeros(s) for s in ((32, 8), (16, 8), (16, 8), (8, 32))]
+    with pytest.raises(ValueError):
+        AttentionLayer(*w, 1, 16, device="cpu",
+                       rotary=ops.Rotary(torch.zeros(9, dtype=torch.int64), 18))
+    with pytest.raises(ValueError):
+        AttentionLayer.make_cache(None, 1, bits=3)
+
+
+def test_step_positions():
+    a, b = Sequence([3, 1], 20), Sequence([0], 4)
+    step = Step.of([a, b], [3, 4], 16, device="cpu")
+    assert step.positions.tolist() == [17, 18, 19, 0, 1, 2, 3]
+    assert step.positions.dtype == torch.int32
