@@ -50,11 +50,23 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
                              int batch, int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
-  p.per = 1;
+  p.per = 16;
   p.tiles = rows / p.per + batch + 1;
-  p.splits = p.most = 1;
-  p.chunk = CS_MAX_Q8_LEN;
-  p.waves = 1;
+  int64_t len = (int64_t)table_width << c.page_log;
+  if (max_len > 0) len = std::min<int64_t>(len, max_len);
+  if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
+  const int64_t per_seq = (rows + batch - 1) / batch;
+  const int64_t items = batch * ((per_seq + p.per - 1) / p.per) * c.heads;
+  const int wgs = 2 * (c.d > 128 || qt == CS_F32 ? 2 : 4);
+  int64_t splits = std::min<int64_t>({256 * wgs / items, len / 256, cs::kMaxSplits});
+  if (splits < 1 || len <= 1024) splits = 1;
+  // Parts are whole steps, so a part is rounded up and there may be fewer of them than `splits`;
+  // `splits` itself never grows as the axis gets shorter.
+  p.most = (int)splits;
+  p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
+  p.splits = (int)((len + p.chunk - 1) / p.chunk);
+  const int64_t most = qt == CS_F32 || c.d > 128 ? 256 : 128;
+  p.waves = p.splits == 1 && items <= most ? 8 : 4;
   return p;
 }
 
@@ -199,8 +211,22 @@ int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q
   if (blocks > kMaxCount) return CS_ERR_SHAPE;
   return with_float(qt, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL((cs::mx4_attention_row<T>), cs::wide_grid(blocks), dim3(64), 0, s, a);
-    return launched();
+    const dim3 grid = cs::wide_grid(blocks);
+    auto few = [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      if (p.waves == 8)
+        hipLaunchKernelGGL((cs::mx4_few<T, DT, 8>), grid, dim3(512), 0, s, a);
+      else
+        hipLaunchKernelGGL((cs::mx4_few<T, DT, 4>), grid, dim3(256), 0, s, a);
+    };
+    with_width(c.d, few);
+    int r = launched();
+    if (r == CS_OK && p.splits > 1) {
+      hipLaunchKernelGGL((cs::attention_join<T, cs::Mx4View>), dim3((unsigned)rows), dim3(256), 0,
+                         s, a);
+      r = launched();
+    }
+    return r;
   });
 }
 

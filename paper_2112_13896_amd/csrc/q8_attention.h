@@ -301,6 +301,51 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
   }
 }
 
+// What a sum of weighted codes is multiplied by.
+constexpr float out_unit(const CacheView&) { return kCodeScale; }
+
+// The wavefronts' sums of up to 16 rows, in LDS, joined in order: 16 lanes to a
+// row.
+template <typename T, int NW, int DP, typename View>
+__device__ __forceinline__ void few_out(const PagedAttentionOf<View>& a,
+                                        const float (&l_o)[NW][16][DP],
+                                        const float (&l_m)[NW][16], const float (&l_l)[NW][16],
+                                        const RowTile& t, int rows_end, int head, int split) {
+  const int d = a.c.d;
+  const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16;
+  if (rr >= 16 || t.row0 + rr >= rows_end) return;
+  float top = kNegInf;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) top = fmaxf(top, l_m[w][rr]);
+  const float base = top == kNegInf ? 0.0f : top;
+  float f[NW], sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    // a wavefront without a key has sums of 0; one with NaN alone among its keys m = -inf
+    f[w] = exp2_fast(l_m[w][rr] - base);
+    sum = fmaf(l_l[w][rr], f[w], sum);
+  }
+  const int orow = t.row0 + rr;
+  const int otok = (int)fdiv((uint32_t)orow, a.by_group);
+  const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
+                     otok * a.group;
+  const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
+  if (a.splits > 1 && x0 == 0) a.part_ml[po] = float2{top, sum};
+  const float inv = sum == 0.0f ? 0.0f : out_unit(a.c) / sum;
+  for (int x = 8 * x0; x < d; x += 128) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
+      v[i] = a.splits > 1 ? s : s * inv;
+    }
+    if (a.splits > 1) store8(a.part_o + po * d + x, v);
+    else store8(static_cast<T*>(a.out) + ro * d + x, v);
+  }
+}
+
 // ---------------------------------------------------------------- few rows
 // attention_few: up to 16 rows of a cache head (a decoding token's query
 // heads, a few drafted tokens) to a workgroup of NW wavefronts, the keys read
@@ -521,39 +566,7 @@ void attention_few(PagedAttention a) {
       *reinterpret_cast<f32x4*>(&l_o[wave][r][(4 * h + i) * CT + x]) =
           f32x4{o[x][i], o[x + 1][i], o[x + 2][i], o[x + 3][i]};
   __syncthreads();
-  // 16 lanes to a row
-  const int rr = threadIdx.x / 16, x0 = threadIdx.x % 16;
-  if (rr >= 16 || t.row0 + rr >= rows_end) return;
-  float top = kNegInf;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) top = fmaxf(top, l_m[w][rr]);
-  const float base = top == kNegInf ? 0.0f : top;
-  float f[NW], sum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    // a wavefront without a key has sums of 0; one with NaN alone among its keys m = -inf
-    f[w] = exp2_fast(l_m[w][rr] - base);
-    sum = fmaf(l_l[w][rr], f[w], sum);
-  }
-  const int orow = t.row0 + rr;
-  const int otok = (int)fdiv((uint32_t)orow, a.by_group);
-  const int64_t ro = (int64_t)(t.token0 + otok) * a.q_heads + head * a.group + orow -
-                     otok * a.group;
-  const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
-  if (a.splits > 1 && x0 == 0) a.part_ml[po] = float2{top, sum};
-  const float inv = sum == 0.0f ? 0.0f : kCodeScale / sum;
-  for (int x = 8 * x0; x < d; x += 128) {
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) s = fmaf(l_o[w][rr][x + i], f[w], s);
-      v[i] = a.splits > 1 ? s : s * inv;
-    }
-    if (a.splits > 1) store8(a.part_o + po * d + x, v);
-    else store8(static_cast<T*>(a.out) + ro * d + x, v);
-  }
+  few_out<T>(a, l_o, l_m, l_l, t, rows_end, head, split);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -937,7 +950,6 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void attention_many(PagedAtte
 // fourth part, so their loads wait for nothing but each other's turn, and the
 // four sums meet in LDS.
 constexpr int kMaxSplits = 64;
-constexpr float out_unit(const CacheView&) { return kCodeScale; }
 
 template <typename T, typename View>
 __global__ __launch_bounds__(256) void attention_join(PagedAttentionOf<View> a) {
