@@ -50,14 +50,14 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
                              int batch, int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
-  p.per = 16;
+  p.per = rows > 64 * (int64_t)batch ? 128 : 16;
   p.tiles = rows / p.per + batch + 1;
   int64_t len = (int64_t)table_width << c.page_log;
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
   const int64_t per_seq = (rows + batch - 1) / batch;
   const int64_t items = batch * ((per_seq + p.per - 1) / p.per) * c.heads;
-  const int wgs = 2 * (c.d > 128 || qt == CS_F32 ? 2 : 4);
+  const int wgs = p.per == 128 ? 1 : 2 * (c.d > 128 || qt == CS_F32 ? 2 : 4);
   int64_t splits = std::min<int64_t>({256 * wgs / items, len / 256, cs::kMaxSplits});
   if (splits < 1 || len <= 1024) splits = 1;
   // Parts are whole steps, so a part is rounded up and there may be fewer of them than `splits`;
@@ -66,7 +66,7 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
   const int64_t most = qt == CS_F32 || c.d > 128 ? 256 : 128;
-  p.waves = p.splits == 1 && items <= most ? 8 : 4;
+  p.waves = p.per == 16 && p.splits == 1 && items <= most ? 8 : 4;
   return p;
 }
 
@@ -219,7 +219,14 @@ int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q
       else
         hipLaunchKernelGGL((cs::mx4_few<T, DT, 4>), grid, dim3(256), 0, s, a);
     };
-    with_width(c.d, few);
+    auto many = [&](auto dt) {
+      constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
+      hipLaunchKernelGGL((cs::mx4_many<T, W>), grid, dim3(256), cs::Mx4Lds<DT>::bytes, s, a);
+    };
+    if (p.per == 16) with_width(c.d, few);
+    else if (c.d > 64 && c.d <= 96) many(std::integral_constant<int, 96>{});
+    else if (c.d > 128 && c.d <= 192) many(std::integral_constant<int, 192>{});
+    else with_width(c.d, many);
     int r = launched();
     if (r == CS_OK && p.splits > 1) {
       hipLaunchKernelGGL((cs::attention_join<T, cs::Mx4View>), dim3((unsigned)rows), dim3(256), 0,

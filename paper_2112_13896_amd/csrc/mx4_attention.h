@@ -22,6 +22,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mx4_places.h"
 #include "mx4_rows.h"
 #include "q8_attention.h"
 
@@ -336,6 +337,383 @@ void mx4_few(Mx4Attention a) {
           f32x4{o[x][i], o[x + 1][i], o[x + 2][i], o[x + 3][i]};
   __syncthreads();
   few_out<T>(a, l_o, l_m, l_l, t, rows_end, head, split);
+}
+
+// ---------------------------------------------------------------- many rows
+// mx4_many: 128 rows of a cache head to a workgroup of four wavefronts, 32 rows
+// each, 64 keys a step, two buffers (Mx4Places).  Keys' codes go to LDS as they
+// are; values are turned to bf16 and transposed once for all four wavefronts.
+// The next step's operands are written at the start of a step, beside its first
+// products, and the loads for the one after that are then on their way under all
+// of its arithmetic; one barrier a step.  W <= DT: channels of values that are
+// computed, d rounded up to 32.
+// Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y = 0..3) of
+// row r.  So a lane's eight weights of 16 keys are those at 4 h .. and 8 + 4 h ..,
+// and the values' chunk g = 2 s + h of a channel holds just the keys 16 s + 4 h ..
+// +3 and 16 s + 8 + 4 h .. +3: two blocks of four tokens of the cache.
+// Queries: row r, channels 16 h .. and 32 + 16 h .. of each 64.
+template <int DT>
+struct Mx4Lds {                                            // bytes
+  using Place = Mx4Places<DT>;
+  static constexpr int k = 0;                              // [2][64][DT / 2] codes
+  static constexpr int v = 2 * Place::key_bytes;           // [2][DT][64] bf16
+  static constexpr int ks = v + 2 * Place::value_bytes;    // [2][words][64] scale bytes
+  static constexpr int mask = ks + 2 * Place::words * 256; // [2] keys without a page, NaN values
+  static constexpr int bytes = mask + 32;
+};
+
+template <typename T, int W>
+__global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a) {
+  constexpr int DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
+  constexpr int NP = Mx4Pieces<T>::q, WP = sizeof(T) == 4 ? 3 : Mx4Pieces<T>::q - 1;
+  constexpr int KS = (W + 63) / 64, CT = W / 32;
+  using At = Mx4Lds<DT>;
+  using Place = Mx4Places<DT>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int r = lane % 32, h = lane / 32, d = a.c.d, groups = a.c.groups;
+  int head, tile, split;
+  if (!place(a, &head, &tile, &split)) return;
+  RowTile t;
+  // the last tiles of a sequence see most keys: first
+  if (!find_tile(a, (int)a.by_tiles.d - 1 - tile, 128, &t)) return;
+  const int rows_end = min(t.rows, t.row0 + 128);
+  const int row = t.row0 + wave * 32 + r;
+  const int row_c = min(row, t.rows - 1);
+  const int tok = (int)fdiv((uint32_t)row_c, a.by_group);
+  const int qh = head * a.group + row_c - tok * a.group;
+  int lo, hi;
+  tile_keys(a, t, (int)fdiv((uint32_t)t.row0, a.by_group),
+            (int)fdiv((uint32_t)(rows_end - 1), a.by_group), &lo, &hi);
+  const int pos = position(t, tok), see = a.window > 0 ? pos - a.window + 1 : 0;
+  // the wavefront's rows all see up to pos0 and from see1 on
+  const int w0 = min(t.row0 + wave * 32, t.rows - 1), w1 = min(w0 + 31, t.rows - 1);
+  const int pos0 = position(t, (int)fdiv((uint32_t)w0, a.by_group));
+  const int pos1 = position(t, (int)fdiv((uint32_t)w1, a.by_group));
+  const int see1 = a.window > 0 ? pos1 - a.window + 1 : 0;
+  const int j0 = lo / 64 * 64 + split * a.chunk;
+  if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
+  const int steps = hi > j0 ? (hi - j0 + 63) / 64 : 0;
+
+  i32x8 q[NP][KS];
+  float c;                                                 // turns products into log2 units
+  {
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
+    float f[KS][32];
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = 64 * k + 32 * (i / 2) + 16 * h + 8 * (i % 2);
+        float g[8];
+        load_q8(qp + (ch < d ? ch : 0), a.q_vec, g);       // all loads before the first use
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[k][8 * i + e] = g[e];
+      }
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (64 * k + 32 * (i / 16) + 16 * h + 8 * (i / 8 % 2) >= d) f[k][i] = 0.0f;
+        top = max(top, abs_bits(f[k][i]));
+      }
+    const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    const float big = __uint_as_float(max(s32[0], s32[1]));
+    const bool bad = !(big < __builtin_inff());
+    const int ex = bad || big == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(big);
+    // (never 0: hidden logits are -inf times it)
+    c = fmaxf(ldexpf(a.scale * 1.4426950408889634f, ex - 8), 0x1p-126f);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+        f[k][e] = bad ? __uint_as_float(0x7FC00000u) : ldexpf(f[k][e], 8 - ex);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) q[n][k] = e4m3_piece(f[k]);
+    }
+  }
+
+  // staging: pieces of keys tid, tid + 256, ..; a unit of values to each of the first DT threads;
+  // wavefront 3 has a key's scales and marks to a lane
+  const int32_t* table = a.table + (int64_t)t.b * a.table_width;
+  const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
+  constexpr int PIECES = (64 * Place::KC + 255) / 256;
+  const bool has_keys = tid < 64 * Place::KC;              // (DT 64: half of them)
+  const bool has_values = tid < DT;
+  const int piece_key = Place::piece_key(tid);
+  const uint32_t k_off = (uint32_t)(piece_key % 16 * 16 * groups +
+                                    (tid % Place::KC < groups ? 16 * (tid % Place::KC) : 0));
+  const int v_chunk = Place::unit_chunk(tid), v_eight = Place::unit_channels(tid);
+  const int v_i = v_eight < 4 * groups ? v_eight : 0;
+  const uint32_t v_off = (uint32_t)((v_chunk % 2 * 4 * groups + v_i) * 16);
+  const uint32_t u_off = (uint32_t)((v_chunk % 2 * groups + v_i / 4) * 4);
+  i32x4 kr[PIECES];
+  u32x4 vr[2];
+  uint32_t vs[2], ks[Place::words];
+  bool key_ok = false, key_bad = false;
+  int page[4];
+  auto pages = [&](int j) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      page[b] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * b, hi - 1) >> lg]);
+  };
+  auto page_of = [&](int b) {                              // of the step's block of 16 keys b
+    return b == 0 ? page[0] : b == 1 ? page[1] : b == 2 ? page[2] : page[3];
+  };
+  // first row of block b times the row's groups; a page outside the cache: any rows, hidden
+  auto block_groups = [&](int pg, int j, int b) {
+    return ((((int64_t)((uint32_t)pg < (uint32_t)n_pages ? pg : 0) * a.c.heads + head) << lg) +
+            ((j + 16 * b) & in_page)) * groups;
+  };
+  auto fetch = [&](int j) {
+    if (has_keys) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        // a wavefront's pieces are of one block of 16 keys, of two where DT is 64
+        const int b = (piece_key + p * (256 / Place::KC)) / 16;
+        const int bu = DT == 64 ? b : __builtin_amdgcn_readfirstlane(b);
+        kr[p] = *reinterpret_cast<const i32x4*>(a.c.k + 16 * block_groups(page_of(bu), j, bu) +
+                                                k_off);
+      }
+    }
+    if (has_values) {
+      const int b = v_chunk / 2;
+      const int64_t g0 = block_groups(page_of(b), j, b);
+      const uint8_t* vp = a.c.v + 16 * g0 + v_off;
+      const uint8_t* up = a.c.vs + g0 + u_off;
+      vr[0] = *reinterpret_cast<const u32x4*>(vp);
+      vr[1] = *reinterpret_cast<const u32x4*>(vp + 128 * groups);
+      vs[0] = *reinterpret_cast<const uint32_t*>(up);
+      vs[1] = *reinterpret_cast<const uint32_t*>(up + 8 * groups);
+    }
+    if (wave == 3) {                                       // key `lane` of the step
+      const int b = lane / 16, pg = page_of(b);
+      const int64_t g0 = block_groups(pg, j, b);
+      const uint8_t* sp = a.c.ks + g0 + lane % 16 * groups;
+#pragma unroll
+      for (int n = 0; n < Place::words; ++n) {
+        ks[n] = 0x7F7F7F7Fu;                               // groups that there are not
+        if (groups >= 4 * n + 4) {
+          __builtin_memcpy(&ks[n], sp + 4 * n, 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (4 * n + i < groups)
+              ks[n] = (ks[n] & ~(0xFFu << 8 * i)) | (uint32_t)sp[4 * n + i] << 8 * i;
+        }
+      }
+      key_ok = (uint32_t)pg < (uint32_t)n_pages;
+      key_bad = a.c.vs[g0 + lane % 16 / 4 * 4 * groups + lane % 4] == kMx4Bad;
+    }
+  };
+  int k_put[PIECES];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) k_put[p] = At::k + Place::piece_put(tid + 256 * p);
+  const int v_row = At::v + Place::unit_row(tid), v_bits = Place::unit_bits(tid);
+  auto stage = [&](auto par) {                             // buffer par
+    constexpr int P = decltype(par)::value;
+    if (has_keys) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+        *reinterpret_cast<i32x4*>(smem + P * Place::key_bytes + k_put[p]) = kr[p];
+    }
+    if (has_values) {
+      const int bits = opaque_int(v_bits);                 // (eight addresses, not eight registers)
+      uint32_t v[8];
+      float scale[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = vr[i / 4][i % 4];
+        // what no row sees may hold anything: a weight of 0 needs a finite value beside it (and
+        // NaN rows have codes of 0)
+        scale[i] = power_of_two((int)min(byte_of(vs[i / 4], i % 4), (uint32_t)(kMx4Most + 127)));
+      }
+      auto put = [&](auto b) {
+        constexpr int B = decltype(b)::value;
+        bf16x8 o[2];
+        values_across<B>(v, scale, o);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          *reinterpret_cast<bf16x8*>(smem + P * Place::value_bytes +
+                                     Place::value_put(v_row, bits, 2 * B + e)) = o[e];
+      };
+      put(std::integral_constant<int, 0>{});
+      put(std::integral_constant<int, 1>{});
+      put(std::integral_constant<int, 2>{});
+      put(std::integral_constant<int, 3>{});
+    }
+    if (wave == 3) {
+#pragma unroll
+      for (int n = 0; n < Place::words; ++n)
+        *reinterpret_cast<uint32_t*>(smem + At::ks + (P * Place::words + n) * 256 + 4 * lane) =
+            ks[n];
+      const uint64_t hidden = __builtin_amdgcn_ballot_w64(!key_ok);
+      const uint64_t bad = __builtin_amdgcn_ballot_w64(key_bad);
+      if (lane == 0)
+        *reinterpret_cast<i32x4*>(smem + At::mask + 16 * P) =
+            i32x4{(int)hidden, (int)(hidden >> 32), (int)bad, (int)(bad >> 32)};
+    }
+  };
+
+  f32x16 o[CT];
+#pragma unroll
+  for (int x = 0; x < CT; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[x][i] = 0.0f;
+  float m = kNegInf, l = 0.0f;                             // m: in log2 units
+  int k_at[KS], v_at[4];                                   // the chunks that a lane reads
+#pragma unroll
+  for (int i = 0; i < KS; ++i) k_at[i] = At::k + Place::key_column(r, h, i);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v_at[i] = At::v + Place::value_column(r, h, i);
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  if (steps > 0) {
+    pages(j0);
+    fetch(j0);
+    stage(Even{});
+    pages(j0 + 64);
+    if (steps > 1) fetch(j0 + 64);
+    pages(j0 + 128);
+  }
+  __syncthreads();
+  auto advance = [&](auto par, auto other, int step) {
+    constexpr int P = decltype(par)::value;
+    const int j = j0 + 64 * step;
+    if (step + 1 < steps) stage(other);
+    if (step + 2 < steps) {
+      fetch(j + 128);
+      pages(j + 192);
+    }
+    f32x16 s[2];
+    int sa[2][Place::words];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+#pragma unroll
+      for (int n = 0; n < Place::words; ++n)
+        sa[u][n] = (int)(*reinterpret_cast<const uint32_t*>(
+                             smem + At::ks + (P * Place::words + n) * 256 + 4 * (32 * u + r)) >>
+                         8 * h);
+    }
+    auto logits = [&](auto kk) {
+      constexpr int K = decltype(kk)::value;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const i32x4 kc = *reinterpret_cast<const i32x4*>(smem + P * Place::key_bytes +
+                                                         Place::key_at(k_at[K], u));
+        const i32x8 kf = {kc[0], kc[1], kc[2], kc[3], 0, 0, 0, 0};
+#pragma unroll
+        for (int n = NP - 1; n >= 0; --n)
+          s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+              kf, q[n][K], s[u], kFp4, kFp8, K % 2 * 2, sa[u][K / 2], 0, 127 - 4 * n);
+      }
+    };
+    logits(std::integral_constant<int, 0>{});
+    if constexpr (KS > 1) logits(std::integral_constant<int, 1>{});
+    if constexpr (KS > 2) logits(std::integral_constant<int, 2>{});
+    if constexpr (KS > 3) logits(std::integral_constant<int, 3>{});
+    const i32x4 marks = *reinterpret_cast<const i32x4*>(smem + At::mask + 16 * P);
+    if (__builtin_expect(
+            __builtin_amdgcn_readfirstlane(marks[0] | marks[1] | marks[2] | marks[3]) != 0, 0)) {
+      // (bits of constants in the lane's own words: a bit of its own for each key would be 32 pairs
+      // of registers, kept through the loop)
+      uint32_t word[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) word[i] = (uint32_t)marks[i] >> opaque_int(4 * h);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const int key = Place::logit_key(0, i);
+        if (word[2 + key / 32] >> key % 32 & 1) s[i / 16][i % 16] = __uint_as_float(0x7FC00000u);
+        if (word[key / 32] >> key % 32 & 1) s[i / 16][i % 16] = kNegInf;
+      }
+    }
+    if (j + 63 > pos0) {
+      const int last = pos - j - 4 * h;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (Place::logit_key(0, i) > last) s[i / 16][i % 16] = kNegInf;
+    }
+    if (j < see1) {
+      const int first = see - j - 4 * h;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (Place::logit_key(0, i) < first) s[i / 16][i % 16] = kNegInf;
+    }
+    float top = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+    for (int i = 3; i < 31; i += 2) top = max3(top, s[i / 16][i % 16], s[(i + 1) / 16][(i + 1) % 16]);
+    top = fmaxf(top, s[1][15]);
+    top = fmaxf(m, reduce_x32(top, FMax{}) * c);
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
+      l *= f;
+#pragma unroll
+      for (int y = 0; y < CT; ++y)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[y][i] *= f;
+      m = top;
+    }
+    const float base = m == kNegInf ? 0.0f : m;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      float w[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        w[y] = exp2_fast(fmaf(s[v / 2][v % 2 * 8 + y], c, -base));
+      bf16x8 p[WP];
+      weight_pieces<WP>(w, p);
+      if constexpr (WP == 1) {
+        // one piece: the sum is of the weights as rounded, so that they still sum to 1
+        const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[0][2 * y], p[0][2 * y + 1]}, one, l, false);
+      } else {
+        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+      }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(
+            smem + P * Place::value_bytes + Place::value_at(v_at[Place::column_of(v, ct)], ct));
+#pragma unroll
+        for (int n = WP - 1; n >= 0; --n)
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[n], o[ct], 0, 0, 0);
+      }
+    }
+    __syncthreads();
+  };
+  for (int step = 0; step < steps; step += 2) {
+    advance(Even{}, Odd{}, step);
+    if (step + 1 < steps) advance(Odd{}, Even{}, step + 1);
+  }
+  l = reduce_x32(l, FAdd{});
+  if (row >= rows_end) return;
+  const int64_t ro = (int64_t)(t.token0 + tok) * a.q_heads + qh;
+  const bool part = a.splits > 1;
+  const int64_t po = (int64_t)split * a.tokens * a.q_heads + ro;
+  if (part && h == 0) a.part_ml[po] = float2{m, l};
+  const float inv = part ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const int ch = 32 * ct + 8 * y + 4 * h;
+      if (ch >= d) continue;
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = o[ct][4 * y + i] * inv;
+      if (part) {
+        *reinterpret_cast<f32x4*>(a.part_o + po * d + ch) = f32x4{v[0], v[1], v[2], v[3]};
+      } else {
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<t4*>(static_cast<T*>(a.out) + ro * d + ch) =
+            t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+      }
+    }
 }
 
 }  // namespace cs
