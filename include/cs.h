@@ -972,20 +972,21 @@ int cs_mx4_paged_attention_plan(const cs_mx4_cache* cache, cs_dtype qt, int toke
  *  positions    device int32 [tokens]; the rows of a token below 0 are copied.
  *  interleaved  0: pair i is channels i and i + rot / 2; else 2 i and 2 i + 1.
  *  inverse      non-zero: by minus the angle (the gradient of a call with 0).
- *  x[n], y[n]   device [tokens][heads[n]][d], n = 0, 1, token strides ldx[n],
- *               ldy[n], head strides hsx[n], hsy[n] >= d.  y may be x with the
- *               same strides, and must not overlap it otherwise; channels from
- *               rot on are copied.  heads[n] may be 0 (x[n], y[n] then NULL).
- * The arrays x, y, ldx, hsx, ldy, hsy and heads are host memory of two entries.
+ *  q, yq        device [tokens][q_heads][d], token strides ldq, ldyq, head strides
+ *               hsq, hsyq >= d: turned from q to yq, which may be q with the same
+ *               strides and must not overlap it otherwise.  Channels from rot on
+ *               are copied.  q_heads may be 0 (q, yq then NULL).
+ *  k, yk ...    a second tensor, the same way.
  * tokens may be 0.
  *  Errors: CS_ERR_ARG, CS_ERR_DTYPE, CS_ERR_SHAPE (rot odd, below 2 or over d,
- *  d over 1024, strides, tokens of y less than d apart, more than 65535 heads
+ *  d over 1024, strides, tokens of yq or yk less than d apart, more than 65535 heads
  *  in all, tokens * heads over 2^31 - 1), CS_ERR_DEVICE.
  */
 int cs_rotary(cs_dtype xt, const uint64_t* turns, int rot, int interleaved, float amplitude,
-              int inverse, const int32_t* positions, int64_t tokens, int d, const int* heads,
-              const void* const* x, const int64_t* ldx, const int64_t* hsx, void* const* y,
-              const int64_t* ldy, const int64_t* hsy, void* stream);
+              int inverse, const int32_t* positions, int64_t tokens, int d, int q_heads,
+              const void* q, int64_t ldq, int64_t hsq, void* yq, int64_t ldyq, int64_t hsyq,
+              int k_heads, const void* k, int64_t ldk, int64_t hsk, void* yk, int64_t ldyk,
+              int64_t hsyk, void* stream);
 
 /*
  * The pages of a cache and the sequences that hold them, in DEVICE memory, so

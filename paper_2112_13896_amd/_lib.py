@@ -53,7 +53,6 @@ class PagePool(ctypes.Structure):
 
 
 _cache, _cache4, _pool = _c.POINTER(Q8Cache), _c.POINTER(Mx4Cache), _c.POINTER(PagePool)
-_vps, _i64s = _c.POINTER(_vp), _c.POINTER(_i64)
 SIGNATURES = {
     "cs_pack": (_i, [_i, _vp, _i, _i, _i, _vp, _c.POINTER(_i64), _c.POINTER(_i), _c.POINTER(_i)]),
     "cs_compact": (_i, [_i, _vp, _i64, _i, _vp, _vp, _vp, _vp]),
@@ -122,8 +121,8 @@ SIGNATURES = {
                                     _i, _c.c_float, _i, _vp, _vp, _sz, _vp]),
     "cs_mx4_paged_attention_workspace_bytes": (_sz, [_cache4, _i, _i, _i, _i, _i, _i]),
     "cs_mx4_paged_attention_plan": (_i, [_cache4, _i, _i, _i, _i, _i, _i, _i, _c.POINTER(_i64)]),
-    "cs_rotary": (_i, [_i, _vp, _i, _i, _c.c_float, _i, _vp, _i64, _i, _c.POINTER(_i), _vps, _i64s,
-                       _i64s, _vps, _i64s, _i64s, _vp]),
+    "cs_rotary": (_i, [_i, _vp, _i, _i, _c.c_float, _i, _vp, _i64, _i, _i, _vp, _i64, _i64, _vp,
+                       _i64, _i64, _i, _vp, _i64, _i64, _vp, _i64, _i64, _vp]),
     "cs_plan_step": (_i, [_pool, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _sz,
                           _vp]),
     "cs_plan_step_workspace_bytes": (_sz, [_i]),

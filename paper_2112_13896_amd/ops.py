@@ -1271,38 +1271,33 @@ def rotary(rot: Rotary, positions: torch.Tensor, q: torch.Tensor, k: torch.Tenso
     tensors to write, which may be the inputs.  inverse: turned back, the gradient of a call
     without it."""
     gpu = _gpu(q, "q")
-    xs = (q,) if k is None else (q, k)
-    tokens, _, d = q.shape if q.dim() == 3 else (0, 0, 0)
-    ptrs = [_heads(t, name, gpu) for t, name in zip(xs, ("q", "k"))]
-    if k is not None and (k.dtype != q.dtype or k.shape[0] != tokens or k.shape[2] != d):
-        raise ValueError(f"k must be {q.dtype} [{tokens}][heads][{d}]")
+    pq, ldq, hsq = _heads(q, "q", gpu)
+    tokens, q_heads, d = q.shape
     if out is None:
-        ys = tuple(t.new_empty(t.shape) for t in xs)
+        yq, yk = q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)
     else:
-        ys = (out,) if k is None else tuple(out)
-        if len(ys) != len(xs):
-            raise ValueError("out must be as many tensors as are turned")
-        for x, y in zip(xs, ys):
-            if y.dtype != x.dtype or y.shape != x.shape:
-                raise ValueError("out must be of the inputs' types and shapes")
-    outs = [_heads(t, "out", gpu) for t in ys]
-    heads = [t.shape[1] for t in xs]
-    if max(heads) > _INT_MAX or d > _INT_MAX:
+        yq, yk = (out, None) if k is None else out
+    turned = _turned(yq, q, gpu)
+    more = (0, None, 0, d, None, 0, d)
+    if k is not None:
+        pk, ldk, hsk = _heads(k, "k", gpu)
+        _, k_heads, dk = shape = k.shape
+        if k.dtype != q.dtype or shape[0] != tokens or dk != d:
+            raise ValueError(f"k must be {q.dtype} [{tokens}][heads][{d}]")
+        more = (k_heads, pk, ldk, hsk, *_turned(yk, k, gpu))
+    if tokens | q_heads | d | more[0] > _INT_MAX:
         raise ValueError("q or k has a dimension over 2^31 - 1")
-    if k is None:
-        ptrs.append((None, 0, d))
-        outs.append((None, 0, d))
-        heads.append(0)
-    two, two64 = ctypes.c_void_p * 2, ctypes.c_int64 * 2
-    px, ldx, hsx = zip(*ptrs)
-    py, ldy, hsy = zip(*outs)
     _call("cs_rotary", gpu, lib().cs_rotary,
-          _float_dt(q.dtype), _vector(rot.turns, "turns", torch.int64, rot.rot // 2, gpu), rot.rot,
-          int(rot.interleaved), rot.amplitude, int(bool(inverse)),
-          _vector(positions, "positions", torch.int32, tokens, gpu), tokens, d,
-          (ctypes.c_int * 2)(*heads), two(*px), two64(*ldx), two64(*hsx), two(*py), two64(*ldy),
-          two64(*hsy))
-    return ys[0] if k is None else ys
+          _float_dt(q.dtype), _dense(rot.turns, "turns", gpu), rot.rot, rot.interleaved,
+          rot.amplitude, bool(inverse), _vector(positions, "positions", torch.int32, tokens, gpu),
+          tokens, d, q_heads, pq, ldq, hsq, *turned, *more)
+    return yq if k is None else (yq, yk)
+
+
+def _turned(y: torch.Tensor, x: torch.Tensor, gpu: int):
+    if y.dtype != x.dtype or y.shape != x.shape:
+        raise ValueError("out must be of the inputs' types and shapes")
+    return _heads(y, "out", gpu)
 
 
 # ------------------------------------------------- steps planned on the GPU
@@ -1363,7 +1358,8 @@ def plan_step(pool: DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: i
     """Pages for the new[i] tokens that entry i brings to sequence seqs[i] (int32 [batch]; -1 names
     none), and the step (cs_plan_step): (table int32 [batch][width], lens int32 [batch], starts
     int32 [batch + 1], slots int64 [tokens], positions int32 [tokens], status int32 [2]).  `tokens`:
-    the most that the step may have; width: the pool's by default.  status is 0, 0 where the step
+    the most that the step may have; width: the pool's by default; the results are parts of one allocation unless `out`
+    gives them.  status is 0, 0 where the step
     was planned; otherwise nothing was taken, and the step is empty."""
     gpu = _gpu(seqs, "seqs")
     batch = seqs.numel()
@@ -1373,20 +1369,40 @@ def plan_step(pool: DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: i
     if batch < 1 or width < 1 or tokens < 0:
         raise ValueError("a step has at least one entry, a column and no fewer than 0 tokens")
     i32 = torch.int32
-    shapes = ((i32, (batch, width)), (i32, (batch,)), (i32, (batch + 1,)), (torch.int64, (tokens,)),
-              (i32, (tokens,)), (i32, (2,)))
+    L = lib()
     if out is None:
-        out = tuple(seqs.new_empty(shape, dtype=dt) for dt, shape in shapes)
+        # parts of one allocation: slots, then 32-bit parts (the table first, its rows as aligned as
+        # its width), then the workspace where the caller keeps none
+        cells, own = batch * width, 0 if ws is not None else L.cs_plan_step_workspace_bytes(batch)
+        rest = cells + 2 * batch + 3 + tokens
+        words = 2 * tokens + rest
+        pad = -words % 4
+        buf = seqs.new_empty((words + pad + own // 4,), dtype=i32)
+        slots, table, lens, starts, positions, status, _ = buf.split_with_sizes(
+            (2 * tokens, cells, batch, batch + 1, tokens, 2, pad + own // 4))
+        out = (table.view(batch, width), lens, starts, slots.view(torch.int64), positions, status)
+        at = buf.data_ptr()
+        p_slots, p_table = at, at + 8 * tokens
+        p_lens = p_table + 4 * cells
+        p_starts = p_lens + 4 * batch
+        p_positions = p_starts + 4 * batch + 4
+        p_status = p_positions + 4 * tokens
+        if own:
+            pws, nws = at + 4 * (words + pad), own
+        else:
+            _, pws, nws = _ws(ws, None, seqs.device, gpu)
     else:
+        shapes = ((i32, (batch, width)), (i32, (batch,)), (i32, (batch + 1,)),
+                  (torch.int64, (tokens,)), (i32, (tokens,)), (i32, (2,)))
         for t, (dt, shape) in zip(out, shapes, strict=True):
             if t.dtype != dt or t.shape != shape:
                 raise ValueError(f"out must be {[(str(dt), list(shape)) for dt, shape in shapes]}")
-    L = lib()
-    ws, pws, nws = _ws(ws, lambda: L.cs_plan_step_workspace_bytes(batch), seqs.device, gpu)
-    table, lens, starts, slots, positions, status = (_dense(t, "out", gpu) for t in out)
+        p_table, p_lens, p_starts, p_slots, p_positions, p_status = (_dense(t, "out", gpu)
+                                                                     for t in out)
+        ws, pws, nws = _ws(ws, lambda: L.cs_plan_step_workspace_bytes(batch), seqs.device, gpu)
     _call("cs_plan_step", gpu, L.cs_plan_step, pool._ptr(gpu),
-          _vector(seqs, "seqs", i32, batch, gpu), _vector(new, "new", i32, batch, gpu), batch, table,
-          width, lens, starts, slots, positions, tokens, status, pws, nws)
+          _vector(seqs, "seqs", i32, batch, gpu), _vector(new, "new", i32, batch, gpu), batch,
+          p_table, width, p_lens, p_starts, p_slots, p_positions, tokens, p_status, pws, nws)
     return out
 
 
