@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <numeric>
 
 #include "cs.h"
 #include "mx4_attention.h"
@@ -39,8 +40,8 @@ dim3 cache_grid(int64_t tokens, int heads) {
 }
 
 struct AttentionPlan {
-  int per;             // rows of a workgroup
-  int64_t tiles;       // numbers of row tiles (find_tile)
+  int per;             // rows of a workgroup: 128 (mx4_many), 32 or 16 (mx4_few)
+  int64_t tiles;       // numbers of row tiles (mx4_place)
   int splits, chunk;   // parts of the key axis, positions of a part
   int most;            // parts at most, of this axis under any window and of any shorter one
   int waves;           // wavefronts of a workgroup
@@ -50,21 +51,39 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
                              int batch, int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
-  p.per = rows > 64 * (int64_t)batch ? 128 : 16;
-  p.tiles = rows / p.per + batch + 1;
+  // Rows of a sequence (bf16, d 128, eight heads; 16 | 32 | 128 rows a workgroup, us).  One sequence
+  // of 32,768 keys: 32 rows 29.8 | 29.3 | 41, 64 37.6 | 36.5 | 44, 96 45.5 | 43.7 | 46, 128 - | 53 |
+  // 49; three of 85,000: 20 rows 103 | 87 | 185; eight of 8,192: 32 rows 38.8 | 38.6 | 62, 64 58 |
+  // 56 | 66, 96 78 | 84 | 73; 32 of 2,048: 64 rows 47 | 45 | 64, 96 69 | 72 | 73, 160 - | 110 | 91; 32
+  // of 200: 64 rows 13.6 | 13.9 | 16.4, 96 18.7 | 21.4 | 17.8.  fp32, 32 | 128: 128 rows 62 | 64, 106 |
+  // 107, 100 | 107, 31.8 | 25.6; 96 of eight sequences 100 | 101.
+  const int few = qt == CS_F32 ? 112 : 80;
+  p.per = rows > few * (int64_t)batch ? 128 : rows > 16 * (int64_t)batch && c.d <= 128 ? 32 : 16;
+  // numbers that mx4_place gives: sequences of at least a token, each with less than a tile of rows
+  // that are not there, in steps of what divides both
+  const int64_t seqs = std::min(batch, tokens);
+  p.tiles = (rows + seqs * (p.per - std::gcd(group, (int64_t)p.per))) / p.per;
   int64_t len = (int64_t)table_width << c.page_log;
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
+  // As many parts as fill the card once: four workgroups a compute unit (two or three where
+  // registers are more).  More make sequences of unequal length even out better, but parts have to
+  // be joined: 96 sequences of up to 12,000 keys 144 us so, 140 at twice as many, 135 at three times;
+  // 96 of 6,000 108 | 117 | 123; 128 of 4,500 107 | 118 | 124.  128 rows take 1.5 times as long to
+  // join as a second part saves (32 sequences of 2,048 keys: whole 74 us, two parts 102; eight of
+  // 8,192 in four parts 93, in eight 79).  Short axes stay whole: the join is a launch of its own
+  // (1,500 keys of one sequence 12.2 us, 14.3 in parts).
   const int64_t per_seq = (rows + batch - 1) / batch;
   const int64_t items = batch * ((per_seq + p.per - 1) / p.per) * c.heads;
-  const int wgs = p.per == 128 ? 1 : 2 * (c.d > 128 || qt == CS_F32 ? 2 : 4);
+  const int wgs = p.per > 16 || c.d > 128 ? 2 : qt == CS_F32 ? 3 : 4;
   int64_t splits = std::min<int64_t>({256 * wgs / items, len / 256, cs::kMaxSplits});
-  if (splits < 1 || len <= 1024) splits = 1;
-  // Parts are whole steps, so a part is rounded up and there may be fewer of them than `splits`;
+  if (splits < (p.per == 128 ? 3 : 1) || len <= 2048) splits = 1;
+  // Parts are whole steps, so a part is rounded up and there may be fewer of them than `splits`.
   // `splits` itself never grows as the axis gets shorter.
   p.most = (int)splits;
   p.chunk = (int)round_up((size_t)((len + splits - 1) / splits), 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
+  // a workgroup or fewer a compute unit, keys whole: eight wavefronts halve its chain of steps
   const int64_t most = qt == CS_F32 || c.d > 128 ? 256 : 128;
   p.waves = p.per == 16 && p.splits == 1 && items <= most ? 8 : 4;
   return p;
@@ -214,16 +233,18 @@ int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q
     const dim3 grid = cs::wide_grid(blocks);
     auto few = [&](auto dt) {
       constexpr int DT = decltype(dt)::value;
-      if (p.waves == 8)
-        hipLaunchKernelGGL((cs::mx4_few<T, DT, 8>), grid, dim3(512), 0, s, a);
+      if (DT <= 128 && p.per == 32)
+        hipLaunchKernelGGL((cs::mx4_few<T, DT <= 128 ? DT : 128, 4, 2>), grid, dim3(256), 0, s, a);
+      else if (p.waves == 8)
+        hipLaunchKernelGGL((cs::mx4_few<T, DT, 8, 1>), grid, dim3(512), 0, s, a);
       else
-        hipLaunchKernelGGL((cs::mx4_few<T, DT, 4>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((cs::mx4_few<T, DT, 4, 1>), grid, dim3(256), 0, s, a);
     };
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
       hipLaunchKernelGGL((cs::mx4_many<T, W>), grid, dim3(256), cs::Mx4Lds<DT>::bytes, s, a);
     };
-    if (p.per == 16) with_width(c.d, few);
+    if (p.per < 128) with_width(c.d, few);
     else if (c.d > 64 && c.d <= 96) many(std::integral_constant<int, 96>{});
     else if (c.d > 128 && c.d <= 192) many(std::integral_constant<int, 192>{});
     else with_width(c.d, many);

@@ -35,31 +35,72 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float out_unit(const Mx4View&) { return 1.0f; }
+constexpr bool rest_apart(const Mx4View&) { return true; }
 
-constexpr int kFp8 = 0, kFp4 = 4;                          // operand formats
+constexpr int kFp8 = 0, kFp6 = 2, kFp4 = 4;                // operand formats
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
 
+// The pieces of queries (their format, their number, log2 of their units) and of
+// weights.
 template <typename T>
-struct Mx4Pieces {                                         // of a query, of a weight
-  static constexpr int q = sizeof(T) == 4 ? 6 : sizeof(T) == 2 ? 3 : 0, w = sizeof(T) == 4 ? 3 : 2;
+struct Mx4Pieces {
+  static constexpr int format = kFp6, q = sizeof(T) == 4 ? 5 : 4, w = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int unit(int n) { return n < 3 ? -4 * n : -5 * n + 2; }
+  // elements of an operand are the channels in order: `half` of them, and the second half `apart`
+  static constexpr int first(int h) { return 32 * h; }
+  static constexpr int apart(int) { return 16; }
 };
 template <>
 struct Mx4Pieces<__bf16> {
-  static constexpr int q = 2, w = 2;
+  static constexpr int format = kFp8, q = 2, w = 2;
+  static constexpr int unit(int n) { return -4 * n; }
+  // 16 channels of the operand's first half, and 16 of its second
+  static constexpr int first(int h) { return 16 * h; }
+  static constexpr int apart(int channels) { return channels / 2; }
 };
 
-// 32 elements as an operand, bytes in order; f becomes 16 times what they leave.
-__device__ __forceinline__ i32x8 e4m3_piece(float (&f)[32]) {
-  i32x8 out;
+// What a row is multiplied by before it is cut, log2: 8-bit pieces take a largest
+// element in [2^7, 2^8), 6-bit ones in [3.5, 7).
+template <typename T>
+__device__ __forceinline__ int mx4_shift(float big) {
+  if (!(big < __builtin_inff()) || big == 0.0f) return 0;
+  const int ex = __builtin_amdgcn_frexp_expf(big);
+  if (Mx4Pieces<T>::format == kFp8) return 8 - ex;
+  return (__builtin_amdgcn_frexp_mantf(big) < 0.875f ? 3 : 2) - ex;
+}
+
+// Piece n of 32 elements as an operand; f becomes what it leaves, in the next
+// piece's units.
+template <typename T>
+__device__ __forceinline__ i32x8 query_piece(float (&f)[32], int n) {
+  const float up = ldexpf(1.0f, Mx4Pieces<T>::unit(n) - Mx4Pieces<T>::unit(n + 1));
+  i32x8 out = {0, 0, 0, 0, 0, 0, 0, 0};
+  if constexpr (Mx4Pieces<T>::format == kFp8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], w, true);
-    out[i] = w;
-    f[4 * i] = 16.0f * (f[4 * i] - __builtin_amdgcn_cvt_f32_fp8(w, 0));
-    f[4 * i + 1] = 16.0f * (f[4 * i + 1] - __builtin_amdgcn_cvt_f32_fp8(w, 1));
-    f[4 * i + 2] = 16.0f * (f[4 * i + 2] - __builtin_amdgcn_cvt_f32_fp8(w, 2));
-    f[4 * i + 3] = 16.0f * (f[4 * i + 3] - __builtin_amdgcn_cvt_f32_fp8(w, 3));
+    for (int i = 0; i < 8; ++i) {
+      int w = 0;
+      w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], w, false);
+      w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], w, true);
+      out[i] = w;
+      f[4 * i] = up * (f[4 * i] - __builtin_amdgcn_cvt_f32_fp8(w, 0));
+      f[4 * i + 1] = up * (f[4 * i + 1] - __builtin_amdgcn_cvt_f32_fp8(w, 1));
+      f[4 * i + 2] = up * (f[4 * i + 2] - __builtin_amdgcn_cvt_f32_fp8(w, 2));
+      f[4 * i + 3] = up * (f[4 * i + 3] - __builtin_amdgcn_cvt_f32_fp8(w, 3));
+    }
+  } else {
+    f32x16 even, odd;                                      // (the instruction takes them in turn)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      even[i] = f[2 * i];
+      odd[i] = f[2 * i + 1];
+    }
+    const u32x6 w = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 1.0f);
+    const f32x32 held = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(w, 1.0f);
+#pragma unroll
+    for (int i = 0; i < 6; ++i) out[i] = (int)w[i];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) f[i] = up * (f[i] - held[i]);
   }
   return out;
 }
@@ -68,12 +109,18 @@ __device__ __forceinline__ i32x8 e4m3_piece(float (&f)[32]) {
 template <int NW>
 __device__ __forceinline__ void weight_pieces(const float (&w)[8], bf16x8 (&p)[NW]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float v = w[j];
+  for (int j = 0; j < 8; j += 2) {
+    float a = w[j], b = w[j + 1];
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
-      p[n][j] = (__bf16)v;
-      v -= (float)p[n][j];
+      const bf16x2 t = {(__bf16)a, (__bf16)b};             // one instruction
+      p[n][j] = t[0];
+      p[n][j + 1] = t[1];
+      if (n + 1 == NW) break;
+      uint32_t bits;
+      __builtin_memcpy(&bits, &t, 4);
+      a -= __uint_as_float(bits << 16);
+      b -= __uint_as_float(bits & 0xFFFF0000u);
     }
   }
 }
@@ -103,8 +150,72 @@ __device__ __forceinline__ bool has_bad(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return w >> (8 * i) & 0xFFu; }
 
+// A workgroup's head, tile of `per` rows and part.  Heads vary fastest (see
+// place()), then tiles, then parts, the last parts first: those are long
+// sequences', and whole.  Tiles are numbered sequence after sequence, with no
+// number left out, so that workgroups without rows are the last of all (at every
+// fourth place, say, they leave every fourth compute unit idle: three sequences'
+// 20 rows over 85,000 keys 139 us, 85 so).  Sequences' tiles are added up 64 at a
+// time.  Tokens past the last sequence have none: mx4_rest writes their zeros.
+__device__ __forceinline__ bool mx4_place(const Mx4Attention& a, int per, int* head, RowTile* t,
+                                          int* split) {
+  const int lane = threadIdx.x % 64;
+  const uint32_t id = workgroup();
+  int tile = (int)fdiv(id, a.by_heads);
+  *head = (int)(id - tile * a.by_heads.d);
+  int start, n, tiles;                                     // of sequence b0 + lane
+  auto count = [&](int b0) {                               // tiles up to the lane's sequence
+    const int b = min(b0 + lane, a.batch - 1);
+    start = min(max(a.starts[b], 0), a.tokens);
+    const int next = min(max(a.starts[b + 1], 0), a.tokens);
+    n = b0 + lane < a.batch ? max(next - start, 0) : 0;
+    tiles = (int)(((int64_t)n * a.group + per - 1) / per);
+    return (int)wave_incl_scan((uint32_t)tiles, 0u, OpAdd{});
+  };
+  *split = 0;
+  if (a.splits > 1) {
+    int all = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) all += __builtin_amdgcn_readlane(count(b0), 63);
+    if (all == 0) return false;
+    const int turn = (int)((uint32_t)tile / (uint32_t)all);
+    tile -= turn * all;
+    *split = a.splits - 1 - turn;
+    if (*split < 0) return false;
+  }
+  int base = 0;                                            // tiles of the sequences before b0
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int end = base + count(b0);
+    const uint64_t there = __builtin_amdgcn_ballot_w64(end > tile);
+    if (there) {
+      const int i = __builtin_ctzll(there);
+      t->b = b0 + i;
+      t->token0 = __builtin_amdgcn_readlane(start, i);
+      t->n = __builtin_amdgcn_readlane(n, i);
+      t->rows = t->n * a.group;
+      // a sequence's last tiles see most keys: first
+      t->row0 = (__builtin_amdgcn_readlane(end, i) - 1 - tile) * per;
+      t->len = min(max(a.lens[t->b], 0), a.table_width << a.c.page_log);
+      return true;
+    }
+    base = __builtin_amdgcn_readlane(end, 63);
+  }
+  return false;
+}
+
+// Zeros for the tokens past the last sequence (a padded batch), a row to a
+// wavefront; the workgroups share them.
+template <typename T>
+__device__ __forceinline__ void mx4_rest(const Mx4Attention& a) {
+  const int from = min(max(a.starts[a.batch], 0), a.tokens);
+  const int lane = threadIdx.x % 64, waves = blockDim.x / 64;
+  const int64_t end = (int64_t)a.tokens * a.q_heads, step = (int64_t)gridDim.x * gridDim.y * waves;
+  for (int64_t row = (int64_t)from * a.q_heads + (int64_t)workgroup() * waves + threadIdx.x / 64;
+       row < end; row += step)
+    for (int x = lane; x < a.c.d; x += 64) static_cast<T*>(a.out)[row * a.c.d + x] = (T)0.0f;
+}
+
 // ---------------------------------------------------------------- few rows
-// mx4_few: up to 16 rows of a cache head to a workgroup of NW wavefronts, the
+// mx4_few: up to 16 RT rows of a cache head to a workgroup of NW wavefronts, the
 // keys read once.  A wavefront takes 32 keys a step, every NW-th step of the
 // workgroup's part of the key axis, straight from memory to registers.
 // Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of 16, channels
@@ -113,22 +224,23 @@ __device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return w >> (8 
 // products.  Values: keys 4 h .. 4 h + 3 of both tiles, eight channels (four
 // where DT is 64, twice eight where it is 256).  Logits: keys 4 h .. 4 h + 3 of
 // both tiles for row r.
-template <typename T, int DT, int NW>
-__global__ __launch_bounds__(64 * NW, DT == 256 || sizeof(T) == 4 ? 2 : 4)
+template <typename T, int DT, int NW, int RT>
+__global__ __launch_bounds__(64 * NW, RT == 2 || DT == 256 || sizeof(T) == 4 ? 2 : 4)
 void mx4_few(Mx4Attention a) {
-  constexpr int NP = Mx4Pieces<T>::q, WP = Mx4Pieces<T>::w;
+  using Pieces = Mx4Pieces<T>;
+  constexpr int NP = Pieces::q, WP = Pieces::w;
   constexpr int KC = DT == 256 ? 2 : 1;                    // products of 128 channels
   constexpr int VC = DT == 256 ? 2 : 1;                    // loads of eight channels
-  constexpr int CT = DT / 16;
+  constexpr int CT = DT / 16, PER = 16 * RT;
   __shared__ float l_o[NW][16][DT + 4];
   __shared__ float l_m[NW][16], l_l[NW][16];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 16, h = lane / 16, d = a.c.d, groups = a.c.groups;
-  int head, tile, split;
-  if (!place(a, &head, &tile, &split)) return;
+  mx4_rest<T>(a);
+  int head, split;
   RowTile t;
-  if (!find_tile(a, tile, 16, &t)) return;
-  const int rows_end = min(t.rows, t.row0 + 16);
+  if (!mx4_place(a, PER, &head, &t, &split)) return;
+  const int rows_end = min(t.rows, t.row0 + PER);
   const int tok0 = (int)fdiv((uint32_t)t.row0, a.by_group);
   const int tok1 = (int)fdiv((uint32_t)(rows_end - 1), a.by_group);
   int lo, hi;
@@ -141,13 +253,16 @@ void mx4_few(Mx4Attention a) {
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
   const int steps = hi > j0 ? (hi - j0 + 31) / 32 : 0;
 
-  // the query rows' operand
-  const int row = min(t.row0 + r, t.rows - 1);
-  const int tok = (int)fdiv((uint32_t)row, a.by_group);
-  const int pos = position(t, tok);                        // the row sees up to pos
-  i32x8 q[NP][KC];
-  float c;                                                 // turns products into log2 units
-  {
+  // the query rows' operands
+  int pos[RT];                                             // a row sees up to pos
+  i32x8 q[RT][NP][KC];
+  float c[RT];                                             // turns products into log2 units
+  int unit0[RT];                                           // scale byte of the first piece
+#pragma unroll
+  for (int y = 0; y < RT; ++y) {
+    const int row = min(t.row0 + 16 * y + r, t.rows - 1);
+    const int tok = (int)fdiv((uint32_t)row, a.by_group);
+    pos[y] = position(t, tok);
     const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq +
                   (head * a.group + row - tok * a.group) * a.hsq;
     float f[KC][32];
@@ -156,7 +271,7 @@ void mx4_few(Mx4Attention a) {
     for (int k = 0; k < KC; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int ch = 128 * k + 64 * (i / 2) + 16 * h + 8 * (i % 2);
+        const int ch = 128 * k + Pieces::first(h) + Pieces::apart(128) * (i / 2) + 8 * (i % 2);
         float g[8];
         if (ch < d) load_q8(qp + ch, a.q_vec, g);
 #pragma unroll
@@ -169,16 +284,17 @@ void mx4_few(Mx4Attention a) {
     top = max(s16[0], s16[1]);
     const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     const float big = __uint_as_float(max(s32[0], s32[1]));
-    const bool bad = !(big < __builtin_inff());
-    const int ex = bad || big == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(big);
-    c = ldexpf(a.scale * 1.4426950408889634f, ex - 8);
+    const int shift = mx4_shift<T>(big);
+    // (never 0: hidden logits are -inf times it)
+    c[y] = fmaxf(ldexpf(a.scale * 1.4426950408889634f, -shift), 0x1p-126f);
+    // a row that is not finite has a scale that is no number: so is all that it meets
+    unit0[y] = big < __builtin_inff() ? 127 : kMx4Bad;
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e)
-        f[k][e] = bad ? __uint_as_float(0x7FC00000u) : ldexpf(f[k][e], 8 - ex);
+      for (int e = 0; e < 32; ++e) f[k][e] = ldexpf(f[k][e], shift);
 #pragma unroll
-      for (int n = 0; n < NP; ++n) q[n][k] = e4m3_piece(f[k]);
+      for (int n = 0; n < NP; ++n) q[y][n][k] = query_piece<T>(f[k], n);
     }
   }
 
@@ -206,137 +322,194 @@ void mx4_few(Mx4Attention a) {
     v_at[k] = (uint32_t)((h * 4 * groups + i) * 16);
     u_at[k] = (uint32_t)((h * groups + i / 4) * 4);
   }
-  f32x4 o[CT];
+  f32x4 o[RT][CT];
+  float m[RT], l[RT];                                      // m: in log2 units
 #pragma unroll
-  for (int x = 0; x < CT; ++x) o[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = kNegInf, l = 0.0f;
-  if (wave < steps) pages(j0 + 32 * wave);
-  for (int step = wave; step < steps; step += NW) {
-    const int j = j0 + 32 * step;
+  for (int y = 0; y < RT; ++y) {
+    m[y] = kNegInf;
+    l[y] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < CT; ++x) o[y][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // what a lane has of a step's 32 keys
+  struct Keys {
     i32x4 kr[2][KC];
     u32x4 vr[2][VC];
     uint32_t ks[2][KC], vs[2][VC];
     bool ok[2];
+  };
+  auto fetch = [&](Keys& g, int j) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      ok[u] = (uint32_t)page[u] < (uint32_t)n_pages;
+      g.ok[u] = (uint32_t)page[u] < (uint32_t)n_pages;
       // no page: any rows, which are masked
-      const int64_t row0 = (((int64_t)(ok[u] ? page[u] : 0) * a.c.heads + head) << lg) +
+      const int64_t row0 = (((int64_t)(g.ok[u] ? page[u] : 0) * a.c.heads + head) << lg) +
                            ((j + 16 * u) & in_page);
       const int64_t g0 = row0 * groups;
+      // scalar bases and the lane's own 32-bit offsets (opaque: added up outside the loop they would
+      // be a 64-bit sum for each load)
+      const uint8_t *kp = a.c.k + 16 * g0, *sp = a.c.ks + g0, *vp = a.c.v + 16 * g0,
+                    *up = a.c.vs + g0;
 #pragma unroll
       for (int k = 0; k < KC; ++k) {
-        kr[u][k] = *reinterpret_cast<const i32x4*>(a.c.k + 16 * g0 + k_at[k]);
-        ks[u][k] = *(a.c.ks + g0 + s_at[k]);
+        g.kr[u][k] = __builtin_nontemporal_load(
+            reinterpret_cast<const i32x4*>(kp + (uint32_t)opaque_int((int)k_at[k])));
+        g.ks[u][k] = sp[(uint32_t)opaque_int((int)s_at[k])];
       }
 #pragma unroll
       for (int k = 0; k < VC; ++k) {
-        vr[u][k] = *reinterpret_cast<const u32x4*>(a.c.v + 16 * g0 + v_at[k]);
-        vs[u][k] = *reinterpret_cast<const uint32_t*>(a.c.vs + g0 + u_at[k]);
+        g.vr[u][k] = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x4*>(vp + (uint32_t)opaque_int((int)v_at[k])));
+        g.vs[u][k] =
+            *reinterpret_cast<const uint32_t*>(up + (uint32_t)opaque_int((int)u_at[k]));
       }
     }
-    if (step + NW < steps) pages(j + 32 * NW);
-    float x[8];
+  };
+  auto use = [&](Keys& g, int j) __attribute__((always_inline)) {
+    float x[RT][8];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        const i32x8 kf = {kr[u][k][0], kr[u][k][1], kr[u][k][2], kr[u][k][3], 0, 0, 0, 0};
+      for (int y = 0; y < RT; ++y) {
+        f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int n = NP - 1; n >= 0; --n)
-          s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[n][k], s, kFp4, kFp8, 0,
-                                                               (int)ks[u][k], 0, 127 - 4 * n);
+        for (int k = 0; k < KC; ++k) {
+          const i32x8 kf = {g.kr[u][k][0], g.kr[u][k][1], g.kr[u][k][2], g.kr[u][k][3], 0, 0, 0, 0};
+#pragma unroll
+          for (int n = NP - 1; n >= 0; --n)
+            s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                kf, q[y][n][k], s, kFp4, Pieces::format, 0, (int)g.ks[u][k], 0,
+                n == 0 ? unit0[y] : 127 + Pieces::unit(n));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[y][4 * u + i] = s[i];
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * u + i] = s[i] * c;
-    }
     // values that were not finite: NaN to whoever sees them, in the weight
     bool any_bad = false;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) any_bad = any_bad || has_bad(vs[u][0]);
+    for (int u = 0; u < 2; ++u) any_bad = any_bad || has_bad(g.vs[u][0]);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_bad) != 0, 0)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (byte_of(vs[i / 4][0], i % 4) == kMx4Bad) x[i] = __uint_as_float(0x7FC00000u);
+        if (byte_of(g.vs[i / 4][0], i % 4) == kMx4Bad)
+#pragma unroll
+          for (int y = 0; y < RT; ++y) x[y][i] = __uint_as_float(0x7FC00000u);
     }
     // hidden keys: past the row's position (the last part's end), before its window, no page
-    if (j + 31 > pos0 || j < see1 || !ok[0] || !ok[1] ||
+    if (j + 31 > pos0 || j < see1 || !g.ok[0] || !g.ok[1] ||
         __builtin_amdgcn_ballot_w64(any_bad) != 0) {
-      const int see = a.window > 0 ? pos - a.window + 1 : 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = j + 16 * (i / 4) + 4 * h + i % 4;
-        if (key > pos || key < see || !ok[i / 4]) x[i] = kNegInf;
+#pragma unroll
+        for (int y = 0; y < RT; ++y) {
+          const int see = a.window > 0 ? pos[y] - a.window + 1 : 0;
+          if (key > pos[y] || key < see || !g.ok[i / 4]) x[y][i] = kNegInf;
+        }
         // what no row sees may hold anything: a weight of 0 needs a finite value beside it
         const uint32_t keep = 0xFFu << (8 * (i % 4));
 #pragma unroll
         for (int k = 0; k < VC; ++k)
-          if (key >= end || !ok[i / 4] || byte_of(vs[i / 4][k], i % 4) == kMx4Bad)
-            vs[i / 4][k] = (vs[i / 4][k] & ~keep) | (0x7F7F7F7Fu & keep);
+          if (key >= end || !g.ok[i / 4] || byte_of(g.vs[i / 4][k], i % 4) == kMx4Bad)
+            g.vs[i / 4][k] = (g.vs[i / 4][k] & ~keep) | (0x7F7F7F7Fu & keep);
       }
     }
-    float top = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(m, x[6], x[7]));
-    top = reduce_x16_x32(top, FMax{});
-    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-      const float f = top == kNegInf ? 1.0f : exp2_fast(m - top);
-      l *= f;
-#pragma unroll
-      for (int z = 0; z < CT; ++z) o[z] *= f;
-      m = top;
-    }
-    const float base = m == kNegInf ? 0.0f : m;
-    float w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = exp2_fast(x[i] - base);
-    bf16x8 p[WP];
-    weight_pieces<WP>(w, p);
-    l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-#pragma unroll
-    for (int k = 0; k < VC; ++k) {
+    constexpr int VF = RT == 1 ? 1 : VC;                   // decoded at once
+    bf16x8 vf[VF][CT / VC];
+    auto decode = [&](int k) __attribute__((always_inline)) {
       uint32_t v[8];
       float scale[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[i] = vr[i / 4][k][i % 4];
+        v[i] = g.vr[i / 4][k][i % 4];
         if (DT == 64) v[i] >>= 16 * (r % 2);               // its four of the eight channels
-        scale[i] = power_of_two((int)byte_of(vs[i / 4][k], i % 4));
+        scale[i] = power_of_two((int)byte_of(g.vs[i / 4][k], i % 4));
       }
-      auto products = [&](auto b) {
-        constexpr int B = decltype(b)::value;
-        bf16x8 vf[2];
-        values_across<B>(v, scale, vf);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int n = WP - 1; n >= 0; --n)
-            o[8 * k + 2 * B + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                vf[e], p[n], o[8 * k + 2 * B + e], 0, 0, 0);
-      };
-      products(std::integral_constant<int, 0>{});
-      products(std::integral_constant<int, 1>{});
+      bf16x8(&to)[CT / VC] = vf[k % VF];
+      values_across<0>(v, scale, *reinterpret_cast<bf16x8(*)[2]>(&to[0]));
+      values_across<1>(v, scale, *reinterpret_cast<bf16x8(*)[2]>(&to[2]));
       if constexpr (DT > 64) {
-        products(std::integral_constant<int, 2>{});
-        products(std::integral_constant<int, 3>{});
+        values_across<2>(v, scale, *reinterpret_cast<bf16x8(*)[2]>(&to[4]));
+        values_across<3>(v, scale, *reinterpret_cast<bf16x8(*)[2]>(&to[6]));
+      }
+    };
+    if constexpr (RT > 1) {                                // beside the logits' products
+#pragma unroll
+      for (int k = 0; k < VC; ++k) decode(k);
+    }
+    // The maximum that a row's weights are relative to rises only where a lane's own logits are more
+    // than 4 (2^2) above it; only then do the lanes of a row need one another's.
+    bool rise = false;
+    float top[RT];
+#pragma unroll
+    for (int y = 0; y < RT; ++y) {
+      top[y] = max3(max3(x[y][0], x[y][1], x[y][2]), max3(x[y][3], x[y][4], x[y][5]),
+                    max3(x[y][6], x[y][7], x[y][7]));
+      rise = rise || top[y] * c[y] > m[y] + kSlack;
+    }
+    if (__builtin_amdgcn_ballot_w64(rise)) {
+#pragma unroll
+      for (int y = 0; y < RT; ++y) {
+        const float now = fmaxf(m[y], reduce_x16_x32(top[y], FMax{}) * c[y]);
+        const float f = now == kNegInf ? 1.0f : exp2_fast(m[y] - now);
+        l[y] *= f;
+#pragma unroll
+        for (int z = 0; z < CT; ++z) o[y][z] *= f;
+        m[y] = now;
       }
     }
+    bf16x8 p[RT][WP];
+#pragma unroll
+    for (int y = 0; y < RT; ++y) {
+      const float base = m[y] == kNegInf ? 0.0f : m[y];
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = exp2_fast(fmaf(x[y][i], c[y], -base));
+      weight_pieces<WP>(w, p[y]);
+      l[y] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    }
+#pragma unroll
+    for (int k = 0; k < VC; ++k) {
+      if constexpr (RT == 1) decode(k);
+#pragma unroll
+      for (int z = 0; z < CT / VC; ++z)
+#pragma unroll
+        for (int y = 0; y < RT; ++y)
+#pragma unroll
+          for (int n = WP - 1; n >= 0; --n)
+            o[y][8 * k + z] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                vf[k % VF][z], p[y][n], o[y][8 * k + z], 0, 0, 0);
+    }
+  };
+  Keys g;
+  if (wave < steps) pages(j0 + 32 * wave);
+  for (int step = wave; step < steps; step += NW) {
+    const int j = j0 + 32 * step;
+    fetch(g, j);
+    if (step + NW < steps) pages(j + 32 * NW);
+    use(g, j);
   }
 
-  // the wavefronts' sums, joined in order
-  l = reduce_x16_x32(l, FAdd{});
-  if (h == 0) {
-    l_m[wave][r] = m;
-    l_l[wave][r] = l;
-  }
+  // the wavefronts' sums, joined in order, 16 rows at a time
   constexpr int PL = DT == 64 ? 4 : 8;                     // channels of a lane that lie together
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int y = 0; y < RT; ++y) {
+    if (y > 0) __syncthreads();
+    const float sum = reduce_x16_x32(l[y], FAdd{});
+    if (h == 0) {
+      l_m[wave][r] = m[y];
+      l_l[wave][r] = sum;
+    }
 #pragma unroll
-    for (int x = 0; x < CT; x += 4)
-      *reinterpret_cast<f32x4*>(&l_o[wave][r][x / PL * 128 + (4 * h + i) * PL + x % PL]) =
-          f32x4{o[x][i], o[x + 1][i], o[x + 2][i], o[x + 3][i]};
-  __syncthreads();
-  few_out<T>(a, l_o, l_m, l_l, t, rows_end, head, split);
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < CT; x += 4)
+        *reinterpret_cast<f32x4*>(&l_o[wave][r][x / PL * 128 + (4 * h + i) * PL + x % PL]) =
+            f32x4{o[y][x][i], o[y][x + 1][i], o[y][x + 2][i], o[y][x + 3][i]};
+    __syncthreads();
+    few_out<T>(a, l_o, l_m, l_l, t, rows_end, head, split);
+    t.row0 += 16;
+  }
 }
 
 // ---------------------------------------------------------------- many rows
@@ -365,7 +538,8 @@ struct Mx4Lds {                                            // bytes
 template <typename T, int W>
 __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a) {
   constexpr int DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
-  constexpr int NP = Mx4Pieces<T>::q, WP = sizeof(T) == 4 ? 3 : Mx4Pieces<T>::q - 1;
+  using Pieces = Mx4Pieces<T>;
+  constexpr int NP = Pieces::q, WP = std::is_same<T, __bf16>::value ? 1 : Pieces::w;
   constexpr int KS = (W + 63) / 64, CT = W / 32;
   using At = Mx4Lds<DT>;
   using Place = Mx4Places<DT>;
@@ -373,11 +547,10 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int r = lane % 32, h = lane / 32, d = a.c.d, groups = a.c.groups;
-  int head, tile, split;
-  if (!place(a, &head, &tile, &split)) return;
+  mx4_rest<T>(a);
+  int head, split;
   RowTile t;
-  // the last tiles of a sequence see most keys: first
-  if (!find_tile(a, (int)a.by_tiles.d - 1 - tile, 128, &t)) return;
+  if (!mx4_place(a, 128, &head, &t, &split)) return;
   const int rows_end = min(t.rows, t.row0 + 128);
   const int row = t.row0 + wave * 32 + r;
   const int row_c = min(row, t.rows - 1);
@@ -398,6 +571,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
 
   i32x8 q[NP][KS];
   float c;                                                 // turns products into log2 units
+  int unit0;                                               // scale byte of the first piece
   {
     const T* qp = static_cast<const T*>(a.q) + (int64_t)(t.token0 + tok) * a.ldq + qh * a.hsq;
     float f[KS][32];
@@ -406,7 +580,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int ch = 64 * k + 32 * (i / 2) + 16 * h + 8 * (i % 2);
+        const int ch = 64 * k + Pieces::first(h) + Pieces::apart(64) * (i / 2) + 8 * (i % 2);
         float g[8];
         load_q8(qp + (ch < d ? ch : 0), a.q_vec, g);       // all loads before the first use
 #pragma unroll
@@ -416,22 +590,23 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
-        if (64 * k + 32 * (i / 16) + 16 * h + 8 * (i / 8 % 2) >= d) f[k][i] = 0.0f;
+        if (64 * k + Pieces::first(h) + Pieces::apart(64) * (i / 16) + 8 * (i / 8 % 2) >= d)
+          f[k][i] = 0.0f;
         top = max(top, abs_bits(f[k][i]));
       }
     const auto s32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
     const float big = __uint_as_float(max(s32[0], s32[1]));
-    const bool bad = !(big < __builtin_inff());
-    const int ex = bad || big == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(big);
+    const int shift = mx4_shift<T>(big);
     // (never 0: hidden logits are -inf times it)
-    c = fmaxf(ldexpf(a.scale * 1.4426950408889634f, ex - 8), 0x1p-126f);
+    c = fmaxf(ldexpf(a.scale * 1.4426950408889634f, -shift), 0x1p-126f);
+    // a row that is not finite has a scale that is no number: so is all that it meets
+    unit0 = big < __builtin_inff() ? 127 : kMx4Bad;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e)
-        f[k][e] = bad ? __uint_as_float(0x7FC00000u) : ldexpf(f[k][e], 8 - ex);
+      for (int e = 0; e < 32; ++e) f[k][e] = ldexpf(f[k][e], shift);
 #pragma unroll
-      for (int n = 0; n < NP; ++n) q[n][k] = e4m3_piece(f[k]);
+      for (int n = 0; n < NP; ++n) q[n][k] = query_piece<T>(f[k], n);
     }
   }
 
@@ -609,7 +784,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
 #pragma unroll
         for (int n = NP - 1; n >= 0; --n)
           s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-              kf, q[n][K], s[u], kFp4, kFp8, K % 2 * 2, sa[u][K / 2], 0, 127 - 4 * n);
+              kf, q[n][K], s[u], kFp4, Pieces::format, K % 2 * 2, sa[u][K / 2], 0,
+              n == 0 ? unit0 : 127 + Pieces::unit(n));
       }
     };
     logits(std::integral_constant<int, 0>{});

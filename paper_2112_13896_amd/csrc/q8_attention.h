@@ -303,6 +303,8 @@ __device__ __forceinline__ void split_f16(const float (&w)[8], f16x8 (&p)[NP]) {
 
 // What a sum of weighted codes is multiplied by.
 constexpr float out_unit(const CacheView&) { return kCodeScale; }
+// Whether tokens past the last sequence have no parts: their zeros are written already.
+constexpr bool rest_apart(const CacheView&) { return false; }
 
 // The wavefronts' sums of up to 16 rows, in LDS, joined in order: 16 lanes to a
 // row.
@@ -957,6 +959,7 @@ __global__ __launch_bounds__(256) void attention_join(PagedAttentionOf<View> a) 
   const int lane = threadIdx.x % 64, d = a.c.d;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int64_t rows = (int64_t)a.tokens * a.q_heads, row = blockIdx.x;
+  if (rest_apart(a.c) && row >= (int64_t)a.starts[a.batch] * a.q_heads) return;
   float2 ml = float2{kNegInf, 0.0f};
   if (lane < a.splits) ml = a.part_ml[lane * rows + row];
   float top = ml.x;

@@ -8,10 +8,13 @@ from oracle import mx4_oracle as o4
 from paper_2112_13896_amd import ops
 from tests.q8_util import DTYPES, ROUND, f64, rand  # noqa: F401
 
-# a query's pieces: how far an element is held, of the row's largest and of itself
-QUERY = {torch.bfloat16: (2.0 ** -21, 0.0), torch.float16: (2.0 ** -25, 0.0),
-         torch.float32: (2.0 ** -37, 2.0 ** -24)}
-PIECES = {torch.bfloat16: 2, torch.float16: 3, torch.float32: 6}
+# A query's pieces: how far an element is held, of the row's largest.  bf16: two e4m3 pieces of a
+# row whose largest is at least 2^7, the second in units of 2^-4 and e4m3's steps at least 2^-9, so
+# half a step is 2^-14.  Otherwise e2m3 pieces of a row whose largest is in [3.5, 7): the first is
+# off by 2^-2, the second by 2^-3 in units of 2^-4, the others by 2^-4 in units of 2^-8, 2^-13,
+# 2^-18.  Four: 2^-17 / 3.5; five: 2^-22 / 3.5.
+QUERY = {torch.bfloat16: 2.0 ** -21, torch.float16: 2.0 ** -18.8, torch.float32: 2.0 ** -23.8}
+PIECES = {torch.bfloat16: 2, torch.float16: 4, torch.float32: 5}
 
 
 def pack_keys(code):
@@ -44,8 +47,7 @@ def bound_attention(o, spread, logit, peak, mass, length, d, dtype, one_piece=Fa
     weights below 2^-126 of the largest: 2^-100 of the row's largest part covers `length` of them."""
     rel, tiny = ROUND[dtype]
     weight = 2.0 ** -8 if one_piece else 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -16
-    of_max, of_it = QUERY[dtype]
-    dl = ((d * PIECES[dtype] + 8) * 2.0 ** -23 + of_it) * logit + of_max * mass
+    dl = (d * PIECES[dtype] + 8) * 2.0 ** -23 * logit + QUERY[dtype] * mass
     dl = dl[..., None] + 2.0 ** -16
     depth = (length / 16 + 64) * 2.0 ** -24 + 2.0 ** -21
     return rel * np.abs(o) + (weight + 2 * dl + depth) * spread + 2.0 ** -100 * peak[..., None] + \
