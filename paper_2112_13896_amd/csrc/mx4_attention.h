@@ -144,6 +144,14 @@ __device__ __forceinline__ void values_across(const uint32_t (&v)[8], const floa
   __builtin_memcpy(&out[1], hi, 16);
 }
 
+// A page number, as a scalar load whatever lies between it and the kernel's other
+// accesses (the table does not change): a vector load here would wait for all the
+// keys and values that are on their way.
+typedef __attribute__((address_space(4))) const int32_t* ConstantInts;
+__device__ __forceinline__ int mx4_page(const int32_t* table, int i) {
+  return ((ConstantInts)(uintptr_t)table)[__builtin_amdgcn_readfirstlane(i)];
+}
+
 // Whether one of a dword's bytes is 255.
 __device__ __forceinline__ bool has_bad(uint32_t w) {
   return ((~w - 0x01010101u) & w & 0x80808080u) != 0;
@@ -304,7 +312,7 @@ void mx4_few(Mx4Attention a) {
   auto pages = [&](int j) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      page[u] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * u, hi - 1) >> lg]);
+      page[u] = mx4_page(table, min(j + 16 * u, hi - 1) >> lg);
   };
   // the lane's bytes in a tile: groups past the last meet zeros in q, channels past it are not
   // stored
@@ -626,13 +634,14 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   const uint32_t u_off = (uint32_t)((v_chunk % 2 * groups + v_i / 4) * 4);
   i32x4 kr[PIECES];
   u32x4 vr[2];
-  uint32_t vs[2], ks[Place::words];
-  bool key_ok = false, key_bad = false;
+  uint32_t vs[2], ks[Place::words], kb[3];
+  uint32_t key_v = 0;                                      // a value scale of key `lane`
+  bool key_ok = false;
   int page[4];
   auto pages = [&](int j) {
 #pragma unroll
     for (int b = 0; b < 4; ++b)
-      page[b] = __builtin_amdgcn_readfirstlane(table[min(j + 16 * b, hi - 1) >> lg]);
+      page[b] = mx4_page(table, min(j + 16 * b, hi - 1) >> lg);
   };
   auto page_of = [&](int b) {                              // of the step's block of 16 keys b
     return b == 0 ? page[0] : b == 1 ? page[1] : b == 2 ? page[2] : page[3];
@@ -667,20 +676,15 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
       const int b = lane / 16, pg = page_of(b);
       const int64_t g0 = block_groups(pg, j, b);
       const uint8_t* sp = a.c.ks + g0 + lane % 16 * groups;
+      // (nothing is computed from them here: that would wait)
 #pragma unroll
-      for (int n = 0; n < Place::words; ++n) {
-        ks[n] = 0x7F7F7F7Fu;                               // groups that there are not
-        if (groups >= 4 * n + 4) {
-          __builtin_memcpy(&ks[n], sp + 4 * n, 4);
-        } else {
+      for (int n = 0; n < Place::words; ++n)
+        if (groups >= 4 * n + 4) __builtin_memcpy(&ks[n], sp + 4 * n, 4);
 #pragma unroll
-          for (int i = 0; i < 3; ++i)
-            if (4 * n + i < groups)
-              ks[n] = (ks[n] & ~(0xFFu << 8 * i)) | (uint32_t)sp[4 * n + i] << 8 * i;
-        }
-      }
+      for (int i = 0; i < 3; ++i)
+        if (i < groups % 4) kb[i] = sp[groups / 4 * 4 + i];
       key_ok = (uint32_t)pg < (uint32_t)n_pages;
-      key_bad = a.c.vs[g0 + lane % 16 / 4 * 4 * groups + lane % 4] == kMx4Bad;
+      key_v = a.c.vs[g0 + lane % 16 / 4 * 4 * groups + lane % 4];
     }
   };
   int k_put[PIECES];
@@ -721,11 +725,19 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     }
     if (wave == 3) {
 #pragma unroll
-      for (int n = 0; n < Place::words; ++n)
-        *reinterpret_cast<uint32_t*>(smem + At::ks + (P * Place::words + n) * 256 + 4 * lane) =
-            ks[n];
+      for (int n = 0; n < Place::words; ++n) {
+        uint32_t w = 0x7F7F7F7Fu;                          // groups that there are not
+        if (groups >= 4 * n + 4) {
+          w = ks[n];
+        } else if (groups > 4 * n) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (i < groups % 4) w = (w & ~(0xFFu << 8 * i)) | kb[i] << 8 * i;
+        }
+        *reinterpret_cast<uint32_t*>(smem + At::ks + (P * Place::words + n) * 256 + 4 * lane) = w;
+      }
       const uint64_t hidden = __builtin_amdgcn_ballot_w64(!key_ok);
-      const uint64_t bad = __builtin_amdgcn_ballot_w64(key_bad);
+      const uint64_t bad = __builtin_amdgcn_ballot_w64(key_v == (uint32_t)kMx4Bad);
       if (lane == 0)
         *reinterpret_cast<i32x4*>(smem + At::mask + 16 * P) =
             i32x4{(int)hidden, (int)(hidden >> 32), (int)bad, (int)(bad >> 32)};
