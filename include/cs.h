@@ -34,7 +34,7 @@
  *    channels.  G = d_out / n packed kernels.
  *  - Integer path: int8 activations and weights, int32 accumulation and bias
  *    (Section 4: weights and activations quantised to 8 bits).  Float path:
- *    fp32 throughout (CS_F16 and CS_BF16 are types of the 8-bit attention
+ *    fp32 throughout (CS_F16 and CS_BF16 are types of the attention layer's
  *    operators alone; every other call refuses them).  Integer sums wrap
  *    modulo 2^32 on overflow (the configurations used stay below 2^31 by a
  *    wide margin).
@@ -941,8 +941,8 @@ int cs_mx4_cache_read(const cs_mx4_cache* cache, const int64_t* slots, int64_t t
  * cs_mx4_paged_attention - cs_paged_attention over the 4-bit cache: the same
  * arguments, checks and errors.  Keys meet the queries as they are held, on the
  * matrix cores' own 4-bit form; a query head's elements are held to 2^-20 of its
- * largest and CS_BF16 otherwise in full (CS_F16: 2^-24, CS_F32: 2^-32 and 24
- * bits of each).  A key's weight has 16 bits (CS_F32: 24), but 8 where the call
+ * largest (CS_F16: 2^-18, CS_F32: 2^-23): the matrix cores take them in pieces of
+ * four significant bits, two for CS_BF16, four for CS_F16 and five for CS_F32.  A key's weight has 16 bits (CS_F32: 24), but 8 where the call
  * runs CS_BF16 rows 128 at a time (cs_mx4_paged_attention_plan's rows); the sum
  * of the weights is 32 bits wide.
  */

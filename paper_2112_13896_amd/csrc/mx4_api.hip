@@ -51,12 +51,13 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
                              int batch, int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
-  // Rows of a sequence (bf16, d 128, eight heads; 16 | 32 | 128 rows a workgroup, us).  One sequence
-  // of 32,768 keys: 32 rows 29.8 | 29.3 | 41, 64 37.6 | 36.5 | 44, 96 45.5 | 43.7 | 46, 128 - | 53 |
-  // 49; three of 85,000: 20 rows 103 | 87 | 185; eight of 8,192: 32 rows 38.8 | 38.6 | 62, 64 58 |
-  // 56 | 66, 96 78 | 84 | 73; 32 of 2,048: 64 rows 47 | 45 | 64, 96 69 | 72 | 73, 160 - | 110 | 91; 32
-  // of 200: 64 rows 13.6 | 13.9 | 16.4, 96 18.7 | 21.4 | 17.8.  fp32, 32 | 128: 128 rows 62 | 64, 106 |
-  // 107, 100 | 107, 31.8 | 25.6; 96 of eight sequences 100 | 101.
+  // Rows of a sequence (bf16, d 128, eight heads; 16 | 32 | 128 rows a workgroup, us).  One
+  // sequence of 32,768 keys: 32 rows 29.8 | 29.3 | 41, 64 37.6 | 36.5 | 44, 96 45.5 | 43.7 | 46,
+  // 128 - | 53 | 49; three of 85,000: 20 rows 103 | 87 | 185; eight of 8,192: 32 rows 38.8 | 38.6 |
+  // 62, 64 58 | 56 | 66, 96 78 | 84 | 73; 32 of 2,048: 64 rows 47 | 45 | 64, 96 69 | 72 | 73, 160 -
+  // | 110 | 91; 32 of 200: 64 rows 13.6 | 13.9 | 16.4, 96 18.7 | 21.4 | 17.8.  fp32, 32 | 128 rows a
+  // workgroup, 128 rows of the four: 62 | 64, 106 | 107, 100 | 107, 31.8 | 25.6; 96 rows of eight
+  // sequences 100 | 101.
   const int few = qt == CS_F32 ? 112 : 80;
   p.per = rows > few * (int64_t)batch ? 128 : rows > 16 * (int64_t)batch && c.d <= 128 ? 32 : 16;
   // numbers that mx4_place gives: sequences of at least a token, each with less than a tile of rows
@@ -68,11 +69,11 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + 64);
   // As many parts as fill the card once: four workgroups a compute unit (two or three where
   // registers are more).  More make sequences of unequal length even out better, but parts have to
-  // be joined: 96 sequences of up to 12,000 keys 144 us so, 140 at twice as many, 135 at three times;
-  // 96 of 6,000 108 | 117 | 123; 128 of 4,500 107 | 118 | 124.  128 rows take 1.5 times as long to
-  // join as a second part saves (32 sequences of 2,048 keys: whole 74 us, two parts 102; eight of
-  // 8,192 in four parts 93, in eight 79).  Short axes stay whole: the join is a launch of its own
-  // (1,500 keys of one sequence 12.2 us, 14.3 in parts).
+  // be joined: 96 sequences of up to 12,000 keys 144 us so, 140 at twice as many, 135 at three
+  // times; 96 of 6,000 108 | 117 | 123; 128 of 4,500 107 | 118 | 124.  128 rows take 1.5 times as
+  // long to join as a second part saves (32 sequences of 2,048 keys: whole 74 us, two parts 102;
+  // eight of 8,192 in four parts 93, in eight 79).  Short axes stay whole: the join is a launch of
+  // its own (1,500 keys of one sequence 12.2 us, 14.3 in parts).
   const int64_t per_seq = (rows + batch - 1) / batch;
   const int64_t items = batch * ((per_seq + p.per - 1) / p.per) * c.heads;
   const int wgs = p.per > 16 || c.d > 128 ? 2 : qt == CS_F32 ? 3 : 4;

@@ -6,12 +6,20 @@
 // places of workgroups are those of the 8-bit cache's kernels.  What differs:
 //  - Keys are never converted: the matrix cores multiply 4-bit codes, with a
 //    power of two for every 32 channels, as the cache holds both.  The other
-//    operand is 8 bits wide (e4m3, four significant bits), so a query row is the
-//    sum of pieces, each what the ones before leave, 2^-4 of them in size: two
-//    pieces hold bf16 in full, three fp16, six fp32.  A row is first scaled by a
-//    power of two so that its largest element lies in [2^7, 2^8); an element's
-//    last piece ends at 2^-9 of its unit (e4m3's smallest step), so N pieces
-//    leave 2^(-6 - 4 N) ... 2^-21 of the largest element for N = 2.
+//    operand has four significant bits, so a query row is the sum of pieces, each
+//    what the ones before leave, in units 2^-4 of theirs (2^-5 from the third on,
+//    where all that is left is below half a step).  The row is first scaled by a
+//    power of two, so that its largest element is near the end of the first
+//    piece's range.
+//    bf16: two pieces in e4m3, largest element in [2^7, 2^8).  They hold the eight
+//    bits of every element that is not small; e4m3's least step, 2^-9 in units of
+//    2^-4, leaves at most 2^-14 of the others: 2^-21 of the largest.
+//    fp16 and fp32: four and five pieces in e2m3, whose step is 1/8 throughout and
+//    which the matrix cores take at twice the rate; largest element in [3.5, 7).
+//    Half a step of the
+//    last, in units of 2^-13 and 2^-18, is
+//    2^-18.8 and 2^-23.8 of the largest element.  (e4m3 would take three and six
+//    pieces at half the rate: the time of six and twelve of these.)
 //  - Values go to bf16, exactly, by the scaled conversion, and meet weights
 //    e_j = 2^(x_j - m) in bf16 pieces: two (16 bits), three for fp32.  bf16 has
 //    the exponents of 32-bit floats, and the cache's scales end at 2^60, so no
@@ -162,8 +170,8 @@ __device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return w >> (8 
 // place()), then tiles, then parts, the last parts first: those are long
 // sequences', and whole.  Tiles are numbered sequence after sequence, with no
 // number left out, so that workgroups without rows are the last of all (at every
-// fourth place, say, they leave every fourth compute unit idle: three sequences'
-// 20 rows over 85,000 keys 139 us, 85 so).  Sequences' tiles are added up 64 at a
+// fourth place, say, they leave every fourth compute unit idle: three sequences of
+// 70,000 to 100,000 keys, 20 rows each, 139 us then, 85 so).  Sequences' tiles are added up 64 at a
 // time.  Tokens past the last sequence have none: mx4_rest writes their zeros.
 __device__ __forceinline__ bool mx4_place(const Mx4Attention& a, int per, int* head, RowTile* t,
                                           int* split) {
@@ -224,7 +232,16 @@ __device__ __forceinline__ void mx4_rest(const Mx4Attention& a) {
 
 // ---------------------------------------------------------------- few rows
 // mx4_few: up to 16 RT rows of a cache head to a workgroup of NW wavefronts, the
-// keys read once.  A wavefront takes 32 keys a step, every NW-th step of the
+// keys read once.  Memory bounds it: 96 sequences of up to 12,000 keys, one token
+// each, eight heads of 128 channels and four query heads to each (bf16), are 638
+// MB in 135 us, 4.7 TB/s of the 5.0 to 5.2 that a large copy reaches; the same
+// loads with no arithmetic take 123 us and the arithmetic with no loads 103.  What
+// is read once does not stay in the L2 (nontemporal: 157 us without).  With 32 rows
+// (RT 2) the keys' arithmetic serves both halves: three sequences of 70,000 to
+// 100,000 keys in fp16, 284 MB in 80 us, 3.6 TB/s, bound by turning values to bf16
+// and by weights.  One step's loads are on their way at a time, of all wavefronts: a
+// second set in registers gained nothing (140 us, 84).
+//  A wavefront takes 32 keys a step, every NW-th step of the
 // workgroup's part of the key axis, straight from memory to registers.
 // Lane = 16 h + r.  Keys: the lane has row (key) r of two tiles of 16, channels
 // 32 h .. of each 128: an operand as it lies.  Queries: row r, channels 16 h ..
@@ -255,7 +272,6 @@ void mx4_few(Mx4Attention a) {
   tile_keys(a, t, tok0, tok1, &lo, &hi);
   const int pos0 = position(t, tok0);                      // every row sees up to pos0 ...
   const int see1 = a.window > 0 ? position(t, tok1) - a.window + 1 : 0;   // ... from see1 on
-  const int end = hi;                                      // no row sees what is from here on
   // this workgroup's part
   const int j0 = lo / 32 * 32 + split * a.chunk;
   if (split + 1 < a.splits) hi = min(hi, j0 + a.chunk);
@@ -354,8 +370,8 @@ void mx4_few(Mx4Attention a) {
       const int64_t row0 = (((int64_t)(g.ok[u] ? page[u] : 0) * a.c.heads + head) << lg) +
                            ((j + 16 * u) & in_page);
       const int64_t g0 = row0 * groups;
-      // scalar bases and the lane's own 32-bit offsets (opaque: added up outside the loop they would
-      // be a 64-bit sum for each load)
+      // scalar bases and the lane's own 32-bit offsets (opaque: added up outside the loop they
+      // would be a 64-bit sum for each load)
       const uint8_t *kp = a.c.k + 16 * g0, *sp = a.c.ks + g0, *vp = a.c.v + 16 * g0,
                     *up = a.c.vs + g0;
 #pragma unroll
@@ -414,11 +430,12 @@ void mx4_few(Mx4Attention a) {
           const int see = a.window > 0 ? pos[y] - a.window + 1 : 0;
           if (key > pos[y] || key < see || !g.ok[i / 4]) x[y][i] = kNegInf;
         }
-        // what no row sees may hold anything: a weight of 0 needs a finite value beside it
+        // what no row sees may hold anything: a weight of 0 needs a finite value beside it (and
+        // NaN rows have codes of 0)
         const uint32_t keep = 0xFFu << (8 * (i % 4));
 #pragma unroll
         for (int k = 0; k < VC; ++k)
-          if (key >= end || !g.ok[i / 4] || byte_of(g.vs[i / 4][k], i % 4) == kMx4Bad)
+          if (byte_of(g.vs[i / 4][k], i % 4) > (uint32_t)(kMx4Most + 127))
             g.vs[i / 4][k] = (g.vs[i / 4][k] & ~keep) | (0x7F7F7F7Fu & keep);
       }
     }
@@ -445,8 +462,8 @@ void mx4_few(Mx4Attention a) {
 #pragma unroll
       for (int k = 0; k < VC; ++k) decode(k);
     }
-    // The maximum that a row's weights are relative to rises only where a lane's own logits are more
-    // than 4 (2^2) above it; only then do the lanes of a row need one another's.
+    // The maximum that a row's weights are relative to rises only where a lane's own logits are
+    // more than 4 (2^2) above it; only then do the lanes of a row need one another's.
     bool rise = false;
     float top[RT];
 #pragma unroll
@@ -528,6 +545,14 @@ void mx4_few(Mx4Attention a) {
 // products, and the loads for the one after that are then on their way under all
 // of its arithmetic; one barrier a step.  W <= DT: channels of values that are
 // computed, d rounded up to 32.
+// Both pipelines bound it: 5 sequences of 2,000 new tokens over up to 6,096 keys,
+// 32 query heads on eight of 128 channels (bf16), 555 GFLOP in 610 us, 0.91 PFLOP/s
+// of the 1.17 to 1.25 that a large bf16 product reaches.  Matrix instructions are 37 %
+// of the SIMDs' cycles and others 40 %, at 1.8 wavefronts a SIMD; with an eighth of
+// the logits' products 531 us, with a quarter of the values' 544, both 472; without
+// exponentials 561, without turning values 555, without loads 529.  The next step's
+// logits formed beside this step's weights, with keys two steps ahead, took 657 us;
+// a higher wave priority during the products 640.
 // Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y = 0..3) of
 // row r.  So a lane's eight weights of 16 keys are those at 4 h .. and 8 + 4 h ..,
 // and the values' chunk g = 2 s + h of a channel holds just the keys 16 s + 4 h ..
@@ -833,7 +858,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     }
     float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
-    for (int i = 3; i < 31; i += 2) top = max3(top, s[i / 16][i % 16], s[(i + 1) / 16][(i + 1) % 16]);
+    for (int i = 3; i < 31; i += 2)
+      top = max3(top, s[i / 16][i % 16], s[(i + 1) / 16][(i + 1) % 16]);
     top = fmaxf(top, s[1][15]);
     top = fmaxf(m, reduce_x32(top, FMax{}) * c);
     if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {

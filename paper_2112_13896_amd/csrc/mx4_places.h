@@ -44,7 +44,9 @@ struct Mx4Places {
   static constexpr int unit_bits(int t) {
     return 16 * (unit_chunk(t) ^ value_turn(unit_channels(t) * 8));
   }
-  static constexpr int value_put(int row, int bits, int c) { return row + c * 128 + (bits ^ 16 * c); }
+  static constexpr int value_put(int row, int bits, int c) {
+    return row + c * 128 + (bits ^ 16 * c);
+  }
   // key of the step's 64 whose value a chunk's half `i` (of 8) is
   static constexpr int value_key(int chunk, int i) {
     return chunk / 2 * 16 + chunk % 2 * 4 + i / 4 * 8 + i % 4;

@@ -63,7 +63,9 @@ struct RotaryVec {
 // rotary: a workgroup has `per` tokens and, of `parts` shares of their units,
 // one.  Cosines and sines of the tokens are formed once, in LDS, for all heads.
 // A unit is N pairs of a head, or N channels from rot on to copy: N elements
-// are 16 bytes (8 where pairs are neighbours: N / 2 pairs), or one pair.
+// are 16 bytes (8 where pairs are neighbours: N / 2 pairs), or one pair.  Memory
+// bounds it: 16,384 tokens of 40 heads of 128 channels in bf16, 336 MB, 65 us,
+// 5.2 TB/s, as fast as a large copy; one token 2.4 us, the time of a launch.
 template <typename T, int N, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void rotary(Rotary a) {
   extern __shared__ __align__(16) float2 l_turn[];         // [per][rot / 2]

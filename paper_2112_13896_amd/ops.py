@@ -1152,9 +1152,10 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
                     max_len: int | None = None, ws: torch.Tensor | None = None,
                     out: torch.Tensor | None = None) -> torch.Tensor:
     """Causal attention of each sequence's new tokens over the cache that already holds them
-    (cs_paged_attention, or cs_mx4_paged_attention for a PagedCache4).  q float [tokens][q_heads][d]; table int32 [batch][pages] page numbers;
-    lens int32 [batch] positions with the new ones; starts int32 [batch + 1] first new token of
-    each sequence in q.  scale: 1 / sqrt(d) by default.  window: positions seen, 0 for all.
+    (cs_paged_attention, or cs_mx4_paged_attention for a PagedCache4).  q float
+    [tokens][q_heads][d]; table int32 [batch][pages] page numbers; lens int32 [batch] positions
+    with the new ones; starts int32 [batch + 1] first new token of each sequence in q.  scale:
+    1 / sqrt(d) by default.  window: positions seen, 0 for all.
     max_len: the longest of lens if the caller knows it (a hint for how the work is split)."""
     qt, tokens, q_heads, b, width, ml = _attention_args(q, cache, table, max_len)
     if window > _INT_MAX:                                     # hides nothing either
@@ -1335,7 +1336,8 @@ class DevicePool:
             object.__setattr__(self, name, value)
 
     @classmethod
-    def empty(cls, sequences: int, width: int, pages: int, page: int, device="cuda") -> "DevicePool":
+    def empty(cls, sequences: int, width: int, pages: int, page: int,
+              device="cuda") -> "DevicePool":
         """No sequence holds anything; the stack gives page 0 first."""
         def zeros(*shape):
             return torch.zeros(shape, dtype=torch.int32, device=device)
@@ -1358,9 +1360,9 @@ def plan_step(pool: DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: i
     """Pages for the new[i] tokens that entry i brings to sequence seqs[i] (int32 [batch]; -1 names
     none), and the step (cs_plan_step): (table int32 [batch][width], lens int32 [batch], starts
     int32 [batch + 1], slots int64 [tokens], positions int32 [tokens], status int32 [2]).  `tokens`:
-    the most that the step may have; width: the pool's by default; the results are parts of one allocation unless `out`
-    gives them.  status is 0, 0 where the step
-    was planned; otherwise nothing was taken, and the step is empty."""
+    the most that the step may have; width: the pool's by default; the results are parts of one
+    allocation unless `out` gives them.  status is 0, 0 where the step was planned; otherwise
+    nothing was taken, and the step is empty."""
     gpu = _gpu(seqs, "seqs")
     batch = seqs.numel()
     width = pool.table.shape[1] if width is None else width

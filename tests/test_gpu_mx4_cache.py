@@ -135,7 +135,8 @@ def test_read_back(dtype, d):
     """Any order, repeats; each value is its code times its scale, rounded once to the type."""
     dt = DTYPES[dtype]
     r = np.random.default_rng(d)
-    x = torch.from_numpy(r.standard_normal((2, 50, 3, d)) * np.exp(r.standard_normal((2, 50, 3, 1))))
+    x = torch.from_numpy(r.standard_normal((2, 50, 3, d)) *
+                         np.exp(r.standard_normal((2, 50, 3, 1))))
     x = x.to(dt)
     cache = _written(x[0].cuda(), x[1].cuda(), np.arange(50) + 7, 4, 16)
     slots = r.integers(0, 50, size=77)

@@ -93,7 +93,8 @@ def test_random_steps(seed):
 def test_wrong_entries_change_nothing():
     b = Both(4, 4, 9, 16)
     b.plan([0, 1], [20, 3], 23)
-    for seqs, new, tokens, status in (([0, 4], [1, 1], 9, 1), ([-2], [1], 9, 1), ([2, 2], [1, 1], 9, 1),
+    for seqs, new, tokens, status in (([0, 4], [1, 1], 9, 1), ([-2], [1], 9, 1),
+                                      ([2, 2], [1, 1], 9, 1),
                                       ([1, 0, 1], [0, 0, 0], 9, 1), ([0], [-1], 9, 1),
                                       ([0], [45], 99, 1), ([0], [2 ** 31 - 1], 99, 1),
                                       ([0, 1], [3, 4], 6, 2), ([2, 3], [64, 64], 200, 3)):

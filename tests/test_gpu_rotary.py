@@ -130,7 +130,8 @@ def test_positions_below_zero_are_copied():
 def test_no_tokens_and_streams():
     ro = ops.Rotary.make(32)
     none = torch.empty((0, 2, 32), device="cuda")
-    assert ops.rotary(ro, torch.empty(0, dtype=torch.int32, device="cuda"), none).shape == none.shape
+    no_positions = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert ops.rotary(ro, no_positions, none).shape == none.shape
     x = torch.randn((40, 2, 32), device="cuda")
     pos = torch.arange(40, dtype=torch.int32, device="cuda")
     want = ops.rotary(ro, pos, x)

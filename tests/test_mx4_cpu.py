@@ -80,7 +80,8 @@ def test_attention_refusals(L):
         assert call(**big, ws=0) == CS_ERR_WORKSPACE
         assert call(**big, ws=P + 8) == CS_ERR_WORKSPACE
     for args in ((CS_I8, 1, 4, 1, 4, 0), (CS_BF16, 0, 4, 1, 4, 0), (CS_BF16, 1, 3, 1, 4, 0),
-                 (CS_BF16, 1, 4, 0, 4, 0), (CS_BF16, 1, 4, 1, 0, 0), (CS_BF16, 1, 4, 1, 1 << 30, 0)):
+                 (CS_BF16, 1, 4, 0, 4, 0), (CS_BF16, 1, 4, 1, 0, 0),
+                 (CS_BF16, 1, 4, 1, 1 << 30, 0)):
         assert L.cs_mx4_paged_attention_workspace_bytes(_cache(), *args) == 0
 
 
@@ -317,7 +318,8 @@ def test_frequencies():
     # 1000 positions: 159, 16, 1.6 and 0.16 turns; kept, kept, (1.6 - 1) / 3 kept, divided
     g, a = ops.rotary_frequencies(8, 10000.0, "bands", factor=4.0, original=1000)
     keep = (10 / (2 * math.pi) - 1) / 3
-    assert np.allclose(g, [1, 0.1, 0.01 * (keep + (1 - keep) / 4), 0.001 / 4], rtol=1e-12) and a == 1
+    assert np.allclose(g, [1, 0.1, 0.01 * (keep + (1 - keep) / 4), 0.001 / 4], rtol=1e-12)
+    assert a == 1
     # 32 turns at place 0.70, one at 2.20: kept up to 0, divided from 3 on, thirds between
     g, a = ops.rotary_frequencies(8, 10000.0, "ramp", factor=4.0, original=1000)
     want = f * (1 - np.arange(4) / 3) + f / 4 * (np.arange(4) / 3)
