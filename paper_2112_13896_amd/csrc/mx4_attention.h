@@ -548,7 +548,7 @@ void mx4_few(Mx4Attention a) {
 // Both pipelines bound it: 5 sequences of 2,000 new tokens over up to 6,096 keys,
 // 32 query heads on eight of 128 channels (bf16), 555 GFLOP in 610 us, 0.91 PFLOP/s
 // of the 1.17 to 1.25 that a large bf16 product reaches.  Matrix instructions are 37 %
-// of the SIMDs' cycles and others 40 %, at 1.8 wavefronts a SIMD; with an eighth of
+// of the SIMDs' cycles and vector instructions 46 %, at 1.8 wavefronts a SIMD; with an eighth of
 // the logits' products 531 us, with a quarter of the values' 544, both 472; without
 // exponentials 561, without turning values 555, without loads 529.  The next step's
 // logits formed beside this step's weights, with keys two steps ahead, took 657 us;
