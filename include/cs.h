@@ -942,9 +942,10 @@ int cs_mx4_cache_read(const cs_mx4_cache* cache, const int64_t* slots, int64_t t
  * arguments, checks and errors.  Keys meet the queries as they are held, on the
  * matrix cores' own 4-bit form; a query head's elements are held to 2^-20 of its
  * largest (CS_F16: 2^-18, CS_F32: 2^-23): the matrix cores take them in pieces of
- * four significant bits, two for CS_BF16, four for CS_F16 and five for CS_F32.  A key's weight has 16 bits (CS_F32: 24), but 8 where the call
- * runs CS_BF16 rows 128 at a time (cs_mx4_paged_attention_plan's rows); the sum
- * of the weights is 32 bits wide.
+ * four significant bits, two for CS_BF16, four for CS_F16 and five for CS_F32.
+ * A key's weight has 16 bits (CS_F32: 24), but 8 where the call runs CS_BF16 rows
+ * 128 at a time (cs_mx4_paged_attention_plan's rows); the sum of the weights is
+ * 32 bits wide.  Slots that no new token sees may hold anything.
  */
 int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
                            int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,
@@ -994,8 +995,8 @@ int cs_rotary(cs_dtype xt, const uint64_t* turns, int rot, int interleaved, floa
  * holds the pages table[s][0 .. ceil(lengths[s] / page) - 1]; the free pages are
  * a stack, free_pages[0 .. count - 1].  marks belongs to the calls: all
  * 0x7FFFFFFF before the first one and after each.
- *  page   as the cache's.  sequences * width and pages are at most 2^31 - 1,
- *         width * page at most CS_MAX_Q8_LEN.
+ *  page   as the cache's.  sequences * width and pages * page are at most
+ *         2^31 - 1, width * page at most CS_MAX_Q8_LEN.
  * The struct itself is host memory.  Calls on one pool are made in stream order.
  */
 typedef struct {

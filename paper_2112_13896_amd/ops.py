@@ -1001,7 +1001,10 @@ class PagedCache:
     k_scale: torch.Tensor
     v_scale: torch.Tensor
 
-    _entry = "cs_"                    # its calls' names start so
+    # its calls
+    _write, _read, _attention = "cs_cache_write", "cs_cache_read", "cs_paged_attention"
+    _attention_bytes = "cs_paged_attention_workspace_bytes"
+    _attention_plan = "cs_paged_attention_plan"
 
     def __post_init__(self):
         if self.k.dim() != 4:
@@ -1048,7 +1051,10 @@ class PagedCache4(PagedCache):
     and [pages][heads][page / 4][groups][4]."""
     d: int
 
-    _entry = "cs_mx4_"
+    _write, _read, _attention = ("cs_mx4_cache_write", "cs_mx4_cache_read",
+                                 "cs_mx4_paged_attention")
+    _attention_bytes = "cs_mx4_paged_attention_workspace_bytes"
+    _attention_plan = "cs_mx4_paged_attention_plan"
 
     def __post_init__(self):
         if self.k.dim() != 4:
@@ -1081,8 +1087,7 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torc
     shape = k.shape
     if k.dtype != v.dtype or v.shape != shape or shape[1] != cache.heads or shape[2] != cache.d:
         raise ValueError(f"k and v must be of one type and [tokens][{cache.heads}][{cache.d}]")
-    name = cache._entry + "cache_write"
-    _call(name, gpu, getattr(lib(), name),
+    _call(cache._write, gpu, getattr(lib(), cache._write),
           cache._ptr(gpu), _float_dt(k.dtype), pk, ldk, hsk, pv, ldv, hsv,
           _vector(slots, "slots", torch.int64, shape[0], gpu), shape[0])
 
@@ -1099,8 +1104,7 @@ def cache_read(cache: PagedCache, slots: torch.Tensor, dtype: torch.dtype,
         for t in out:
             if t.dtype != dtype or t.shape != shape:
                 raise ValueError(f"out must be {dtype} {list(shape)}")
-    name = cache._entry + "cache_read"
-    _call(name, gpu, getattr(lib(), name),
+    _call(cache._read, gpu, getattr(lib(), cache._read),
           cache._ptr(gpu), _vector(slots, "slots", torch.int64, shape[0], gpu), shape[0],
           _float_dt(dtype), _dense(out[0], "out", gpu), _dense(out[1], "out", gpu))
     return out
@@ -1124,8 +1128,8 @@ def _attention_args(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, max
 def paged_attention_workspace(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
                               max_len: int | None = None) -> torch.Tensor:
     """Workspace of paged_attention for arguments of these shapes."""
-    need = getattr(lib(), cache._entry + "paged_attention_workspace_bytes")
-    n = need(cache._ref, *_attention_args(q, cache, table, max_len))
+    n = getattr(lib(), cache._attention_bytes)(
+        cache._ref, *_attention_args(q, cache, table, max_len))
     return torch.empty((int(n),), dtype=torch.uint8, device=q.device)
 
 
@@ -1140,8 +1144,7 @@ def paged_attention_plan(dtype: torch.dtype, heads: int, page: int, d: int, toke
     # the cache's arrays are not touched; any aligned address stands for them
     cache = struct(16, 16, 16, 16, 1, heads, page, d)
     info = (ctypes.c_int64 * 6)()
-    name = kind._entry + "paged_attention_plan"
-    check(name, getattr(lib(), name)(
+    check(kind._attention_plan, getattr(lib(), kind._attention_plan)(
         ctypes.byref(cache), _float_dt(dtype), tokens, q_heads, batch, table_width,
         0 if max_len is None else min(int(max_len), _INT_MAX), min(window, _INT_MAX), info))
     return dict(zip(("rows", "parts", "part", "wavefronts", "workgroups", "bytes"), info))
@@ -1166,10 +1169,10 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
         out = q.new_empty(q.shape)
     elif out.dtype != q.dtype or out.shape != q.shape:
         raise ValueError("out must be of q's type and shape")
-    L, name = lib(), cache._entry + "paged_attention"
-    ws, pws, nws = _ws(ws, lambda: getattr(L, name + "_workspace_bytes")(
+    L = lib()
+    ws, pws, nws = _ws(ws, lambda: getattr(L, cache._attention_bytes)(
         cache._ref, qt, tokens, q_heads, b, width, ml), q.device, gpu)
-    _call(name, gpu, getattr(L, name),
+    _call(cache._attention, gpu, getattr(L, cache._attention),
           cache._ptr(gpu), qt, pq, ldq, hsq, tokens, q_heads, b, _dense(table, "table", gpu), width,
           _vector(lens, "lens", torch.int32, b, gpu),
           _vector(starts, "starts", torch.int32, b + 1, gpu), ml,
