@@ -243,7 +243,12 @@ int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q
     };
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
-      hipLaunchKernelGGL((cs::mx4_many<T, W>), grid, dim3(256), cs::Mx4Lds<DT>::bytes, s, a);
+      if (c.page_log >= 6)
+        hipLaunchKernelGGL((cs::mx4_many<T, W, true>), grid, dim3(256), cs::Mx4Lds<DT>::bytes, s,
+                           a);
+      else
+        hipLaunchKernelGGL((cs::mx4_many<T, W, false>), grid, dim3(256), cs::Mx4Lds<DT>::bytes, s,
+                           a);
     };
     if (p.per < 128) with_width(c.d, few);
     else if (c.d > 64 && c.d <= 96) many(std::integral_constant<int, 96>{});

@@ -568,7 +568,7 @@ struct Mx4Lds {                                            // bytes
   static constexpr int bytes = mask + 32;
 };
 
-template <typename T, int W>
+template <typename T, int W, bool WHOLE>
 __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a) {
   constexpr int DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
   using Pieces = Mx4Pieces<T>;
@@ -649,14 +649,20 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
   constexpr int PIECES = (64 * Place::KC + 255) / 256;
   const bool has_keys = tid < 64 * Place::KC;              // (DT 64: half of them)
-  const bool has_values = tid < DT;
+  constexpr int SHARE = 256 / DT, CH = 8 / SHARE;          // threads to a unit, channels of each
+  const int unit = tid % DT, v_part = tid / DT;
   const int piece_key = Place::piece_key(tid);
-  const uint32_t k_off = (uint32_t)(piece_key % 16 * 16 * groups +
+  // offsets from the first key of the step where one page holds it all, else of the block of 16
+  const uint32_t k_off = (uint32_t)((WHOLE ? piece_key : piece_key % 16) * 16 * groups +
                                     (tid % Place::KC < groups ? 16 * (tid % Place::KC) : 0));
-  const int v_chunk = Place::unit_chunk(tid), v_eight = Place::unit_channels(tid);
+  const int v_chunk = Place::unit_chunk(unit), v_eight = Place::unit_channels(unit);
   const int v_i = v_eight < 4 * groups ? v_eight : 0;
-  const uint32_t v_off = (uint32_t)((v_chunk % 2 * 4 * groups + v_i) * 16);
-  const uint32_t u_off = (uint32_t)((v_chunk % 2 * groups + v_i / 4) * 4);
+  const int v_four = (WHOLE ? v_chunk / 2 * 4 : 0) + v_chunk % 2;   // block of four tokens
+  const uint32_t v_off = (uint32_t)((v_four * 4 * groups + v_i) * 16);
+  const uint32_t u_off = (uint32_t)((v_four * groups + v_i / 4) * 4);
+  const int s_key = WHOLE ? lane : lane % 16;
+  const uint32_t s_off = (uint32_t)(s_key * groups);
+  const uint32_t m_off = (uint32_t)(s_key / 4 * 4 * groups + lane % 4);
   i32x4 kr[PIECES];
   u32x4 vr[2];
   uint32_t vs[2], ks[Place::words], kb[3];
@@ -665,8 +671,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   int page[4];
   auto pages = [&](int j) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
-      page[b] = mx4_page(table, min(j + 16 * b, hi - 1) >> lg);
+    for (int b = 0; b < (WHOLE ? 1 : 4); ++b) page[b] = mx4_page(table, min(j + 16 * b, hi - 1) >> lg);
   };
   auto page_of = [&](int b) {                              // of the step's block of 16 keys b
     return b == 0 ? page[0] : b == 1 ? page[1] : b == 2 ? page[2] : page[3];
@@ -676,7 +681,39 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     return ((((int64_t)((uint32_t)pg < (uint32_t)n_pages ? pg : 0) * a.c.heads + head) << lg) +
             ((j + 16 * b) & in_page)) * groups;
   };
-  auto fetch = [&](int j) {
+  auto fetch_scales = [&](int pg, int64_t g0) __attribute__((always_inline)) {   // key `lane`
+    const uint8_t* sp = a.c.ks + g0 + s_off;
+    // (nothing is computed from them here: that would wait)
+#pragma unroll
+    for (int n = 0; n < Place::words; ++n)
+      if (groups >= 4 * n + 4) __builtin_memcpy(&ks[n], sp + 4 * n, 4);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < groups % 4) kb[i] = sp[groups / 4 * 4 + i];
+    key_ok = (uint32_t)pg < (uint32_t)n_pages;
+    key_v = a.c.vs[g0 + m_off];
+  };
+  auto fetch_values = [&](int64_t g0) __attribute__((always_inline)) {
+    const uint8_t* vp = a.c.v + 16 * g0 + v_off;
+    const uint8_t* up = a.c.vs + g0 + u_off;
+    vr[0] = *reinterpret_cast<const u32x4*>(vp);
+    vr[1] = *reinterpret_cast<const u32x4*>(vp + 128 * groups);
+    vs[0] = *reinterpret_cast<const uint32_t*>(up);
+    vs[1] = *reinterpret_cast<const uint32_t*>(up + 8 * groups);
+  };
+  auto fetch = [&](int j) __attribute__((always_inline)) {
+    if constexpr (WHOLE) {                                 // one page: scalar addresses
+      const int64_t g0 = block_groups(page[0], j, 0);
+      const uint8_t* kp = a.c.k + 16 * g0;
+      if (has_keys) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+          kr[p] = *reinterpret_cast<const i32x4*>(kp + p * (256 / Place::KC * 16) * groups + k_off);
+      }
+      fetch_values(g0);
+      if (wave == 3) fetch_scales(page[0], g0);
+      return;
+    }
     if (has_keys) {
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
@@ -687,66 +724,51 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
                                                 k_off);
       }
     }
-    if (has_values) {
-      const int b = v_chunk / 2;
-      const int64_t g0 = block_groups(page_of(b), j, b);
-      const uint8_t* vp = a.c.v + 16 * g0 + v_off;
-      const uint8_t* up = a.c.vs + g0 + u_off;
-      vr[0] = *reinterpret_cast<const u32x4*>(vp);
-      vr[1] = *reinterpret_cast<const u32x4*>(vp + 128 * groups);
-      vs[0] = *reinterpret_cast<const uint32_t*>(up);
-      vs[1] = *reinterpret_cast<const uint32_t*>(up + 8 * groups);
-    }
-    if (wave == 3) {                                       // key `lane` of the step
+    fetch_values(block_groups(page_of(v_chunk / 2), j, v_chunk / 2));
+    if (wave == 3) {
       const int b = lane / 16, pg = page_of(b);
-      const int64_t g0 = block_groups(pg, j, b);
-      const uint8_t* sp = a.c.ks + g0 + lane % 16 * groups;
-      // (nothing is computed from them here: that would wait)
-#pragma unroll
-      for (int n = 0; n < Place::words; ++n)
-        if (groups >= 4 * n + 4) __builtin_memcpy(&ks[n], sp + 4 * n, 4);
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-        if (i < groups % 4) kb[i] = sp[groups / 4 * 4 + i];
-      key_ok = (uint32_t)pg < (uint32_t)n_pages;
-      key_v = a.c.vs[g0 + lane % 16 / 4 * 4 * groups + lane % 4];
+      fetch_scales(pg, block_groups(pg, j, b));
     }
   };
   int k_put[PIECES];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) k_put[p] = At::k + Place::piece_put(tid + 256 * p);
-  const int v_row = At::v + Place::unit_row(tid), v_bits = Place::unit_bits(tid);
-  auto stage = [&](auto par) {                             // buffer par
+  // (its channels from CH v_part on: the turn of their rows is that of the first, xor the channel)
+  const int v_row = At::v + Place::unit_row(unit) + CH * v_part * 128;
+  const int v_bits = Place::unit_bits(unit) ^ 16 * CH * v_part;
+  auto stage_values = [&](auto par) {                      // buffer par
+    constexpr int P = decltype(par)::value;
+    const int bits = opaque_int(v_bits);                   // (eight addresses, not eight registers)
+    uint32_t v[8];
+    float scale[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = vr[i / 4][i % 4];
+      if (SHARE > 1) v[i] >>= 4 * CH * v_part;
+      // what no row sees may hold anything: a weight of 0 needs a finite value beside it (and
+      // NaN rows have codes of 0)
+      scale[i] = power_of_two((int)min(byte_of(vs[i / 4], i % 4), (uint32_t)(kMx4Most + 127)));
+    }
+    auto put = [&](auto b) {
+      constexpr int B = decltype(b)::value;
+      bf16x8 o[2];
+      values_across<B>(v, scale, o);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        *reinterpret_cast<bf16x8*>(smem + P * Place::value_bytes +
+                                   Place::value_put(v_row, bits, 2 * B + e)) = o[e];
+    };
+    put(std::integral_constant<int, 0>{});
+    if constexpr (CH > 2) put(std::integral_constant<int, 1>{});
+    if constexpr (CH > 4) put(std::integral_constant<int, 2>{});
+    if constexpr (CH > 4) put(std::integral_constant<int, 3>{});
+  };
+  auto stage_keys = [&](auto par) {
     constexpr int P = decltype(par)::value;
     if (has_keys) {
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
         *reinterpret_cast<i32x4*>(smem + P * Place::key_bytes + k_put[p]) = kr[p];
-    }
-    if (has_values) {
-      const int bits = opaque_int(v_bits);                 // (eight addresses, not eight registers)
-      uint32_t v[8];
-      float scale[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[i] = vr[i / 4][i % 4];
-        // what no row sees may hold anything: a weight of 0 needs a finite value beside it (and
-        // NaN rows have codes of 0)
-        scale[i] = power_of_two((int)min(byte_of(vs[i / 4], i % 4), (uint32_t)(kMx4Most + 127)));
-      }
-      auto put = [&](auto b) {
-        constexpr int B = decltype(b)::value;
-        bf16x8 o[2];
-        values_across<B>(v, scale, o);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          *reinterpret_cast<bf16x8*>(smem + P * Place::value_bytes +
-                                     Place::value_put(v_row, bits, 2 * B + e)) = o[e];
-      };
-      put(std::integral_constant<int, 0>{});
-      put(std::integral_constant<int, 1>{});
-      put(std::integral_constant<int, 2>{});
-      put(std::integral_constant<int, 3>{});
     }
     if (wave == 3) {
 #pragma unroll
@@ -785,7 +807,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   if (steps > 0) {
     pages(j0);
     fetch(j0);
-    stage(Even{});
+    stage_keys(Even{});
+    stage_values(Even{});
     pages(j0 + 64);
     if (steps > 1) fetch(j0 + 64);
     pages(j0 + 128);
@@ -794,11 +817,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   auto advance = [&](auto par, auto other, int step) {
     constexpr int P = decltype(par)::value;
     const int j = j0 + 64 * step;
-    if (step + 1 < steps) stage(other);
-    if (step + 2 < steps) {
-      fetch(j + 128);
-      pages(j + 192);
-    }
+    stage_keys(other);                                     // (past the last step: not used)
     f32x16 s[2];
     int sa[2][Place::words];
 #pragma unroll
@@ -811,13 +830,19 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
                              smem + At::ks + (P * Place::words + n) * 256 + 4 * (32 * u + r)) >>
                          8 * h);
     }
+    i32x4 kc[2][KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        kc[u][k] = *reinterpret_cast<const i32x4*>(smem + P * Place::key_bytes +
+                                                   Place::key_at(k_at[k], u));
+    stage_values(other);
     auto logits = [&](auto kk) {
       constexpr int K = decltype(kk)::value;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const i32x4 kc = *reinterpret_cast<const i32x4*>(smem + P * Place::key_bytes +
-                                                         Place::key_at(k_at[K], u));
-        const i32x8 kf = {kc[0], kc[1], kc[2], kc[3], 0, 0, 0, 0};
+        const i32x8 kf = {kc[u][K][0], kc[u][K][1], kc[u][K][2], kc[u][K][3], 0, 0, 0, 0};
 #pragma unroll
         for (int n = NP - 1; n >= 0; --n)
           s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
@@ -829,6 +854,18 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     if constexpr (KS > 1) logits(std::integral_constant<int, 1>{});
     if constexpr (KS > 2) logits(std::integral_constant<int, 2>{});
     if constexpr (KS > 3) logits(std::integral_constant<int, 3>{});
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * KS + 2 * Place::words, 0);
+    __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * KS * NP; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
+    }
+    asm volatile("" : "+v"(s[0]), "+v"(s[1]));             // (the products stay up there)
+    if (step + 2 < steps) {
+      fetch(j + 128);
+      pages(j + 192);
+    }
     const i32x4 marks = *reinterpret_cast<const i32x4*>(smem + At::mask + 16 * P);
     if (__builtin_expect(
             __builtin_amdgcn_readfirstlane(marks[0] | marks[1] | marks[2] | marks[3]) != 0, 0)) {
@@ -872,32 +909,57 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
       m = top;
     }
     const float base = m == kNegInf ? 0.0f : m;
+    bf16x8 vf[2][CT], p[2][WP];
+    auto values = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
+      for (int ct = 0; ct < CT; ++ct)
+        vf[v % 2][ct] = *reinterpret_cast<const bf16x8*>(
+            smem + P * Place::value_bytes + Place::value_at(v_at[Place::column_of(v, ct)], ct));
+    };
+    auto weights = [&](int v) __attribute__((always_inline)) {
       float w[8];
 #pragma unroll
       for (int y = 0; y < 8; ++y)
         w[y] = exp2_fast(fmaf(s[v / 2][v % 2 * 8 + y], c, -base));
-      bf16x8 p[WP];
-      weight_pieces<WP>(w, p);
+      weight_pieces<WP>(w, p[v % 2]);
       if constexpr (WP == 1) {
         // one piece: the sum is of the weights as rounded, so that they still sum to 1
         const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[0][2 * y], p[0][2 * y + 1]}, one, l, false);
+          l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[v % 2][0][2 * y], p[v % 2][0][2 * y + 1]},
+                                              one, l, false);
       } else {
         l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
       }
+    };
+    values(0);
+    weights(0);
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(
-            smem + P * Place::value_bytes + Place::value_at(v_at[Place::column_of(v, ct)], ct));
+    for (int v = 0; v < 4; ++v) {
+      if (v < 3) values(v + 1);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int n = WP - 1; n >= 0; --n)
-          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[n], o[ct], 0, 0, 0);
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[v % 2][ct], p[v % 2][n], o[ct], 0, 0,
+                                                          0);
+      if (v < 3) weights(v + 1);
+    }
+    // (in this order: each operand is read during the products before)
+    constexpr int each = WP == 1 ? 24 : WP == 2 ? 44 : 64;
+    __builtin_amdgcn_sched_group_barrier(0x100, CT, 1);
+    __builtin_amdgcn_sched_group_barrier(0x2, each, 1);
+#pragma unroll
+    for (int v = 0; v < 3; ++v) {
+      __builtin_amdgcn_sched_group_barrier(0x100, CT, 1);
+#pragma unroll
+      for (int ct = 0; ct < CT * WP; ++ct) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x2, each / (CT * WP), 1);
       }
     }
+    __builtin_amdgcn_sched_group_barrier(0x8, CT * WP, 1);
     __syncthreads();
   };
   for (int step = 0; step < steps; step += 2) {
