@@ -541,18 +541,21 @@ void mx4_few(Mx4Attention a) {
 // mx4_many: 128 rows of a cache head to a workgroup of four wavefronts, 32 rows
 // each, 64 keys a step, two buffers (Mx4Places).  Keys' codes go to LDS as they
 // are; values are turned to bf16 and transposed once for all four wavefronts.
-// The next step's operands are written at the start of a step, beside its first
-// products, and the loads for the one after that are then on their way under all
-// of its arithmetic; one barrier a step.  W <= DT: channels of values that are
-// computed, d rounded up to 32.
+// The next step's values are turned beside the logits' products, and the loads for
+// the step after that are then on their way under the rest of the arithmetic; one
+// barrier a step.  W <= DT: channels of values that are computed, d rounded up to
+// 32.  WHOLE: a page holds a step's 64 keys, so that all its addresses are scalar.
 // Both pipelines bound it: 5 sequences of 2,000 new tokens over up to 6,096 keys,
-// 32 query heads on eight of 128 channels (bf16), 555 GFLOP in 610 us, 0.91 PFLOP/s
-// of the 1.17 to 1.25 that a large bf16 product reaches.  Matrix instructions are 37 %
-// of the SIMDs' cycles and vector instructions 46 %, at 1.8 wavefronts a SIMD; with an eighth of
-// the logits' products 531 us, with a quarter of the values' 544, both 472; without
-// exponentials 561, without turning values 555, without loads 529.  The next step's
-// logits formed beside this step's weights, with keys two steps ahead, took 657 us;
-// a higher wave priority during the products 640.
+// 32 query heads on eight of 128 channels (bf16), 555 GFLOP in 558 us, 0.99 PFLOP/s
+// of the 1.17 to 1.25 that a large bf16 product reaches.  Matrix instructions are
+// 42 % of the SIMDs' cycles and vector instructions 52 %, at 1.7 wavefronts a SIMD.
+// Values turned by half of the wavefronts before the products, and each operand read
+// right before its product: 610 us.  From there: with an eighth of the logits'
+// products 531, with a quarter of the values' 544, both 472; without exponentials
+// 561, without turning values 555, without loads 529.  The next step's logits formed
+// beside this step's weights, with keys two steps ahead, took 657; a higher wave
+// priority during the products 640.  Where pages are shorter than a step: 700 tokens
+// of four sequences over 2,700 keys 102 us (92 where they are not).
 // Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y = 0..3) of
 // row r.  So a lane's eight weights of 16 keys are those at 4 h .. and 8 + 4 h ..,
 // and the values' chunk g = 2 s + h of a channel holds just the keys 16 s + 4 h ..
@@ -567,6 +570,8 @@ struct Mx4Lds {                                            // bytes
   static constexpr int mask = ks + 2 * Place::words * 256; // [2] keys without a page, NaN values
   static constexpr int bytes = mask + 32;
 };
+
+constexpr int kVector = 0x2, kProducts = 0x8, kLdsReads = 0x100;   // kinds of instructions
 
 template <typename T, int W, bool WHOLE>
 __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a) {
@@ -643,8 +648,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     }
   }
 
-  // staging: pieces of keys tid, tid + 256, ..; a unit of values to each of the first DT threads;
-  // wavefront 3 has a key's scales and marks to a lane
+  // staging: pieces of keys tid, tid + 256, ..; a unit of values to SHARE threads, CH of its eight
+  // channels each; wavefront 3 has a key's scales and marks to a lane
   const int32_t* table = a.table + (int64_t)t.b * a.table_width;
   const int lg = a.c.page_log, in_page = (1 << lg) - 1, n_pages = (int)(a.c.slots >> lg);
   constexpr int PIECES = (64 * Place::KC + 255) / 256;
@@ -854,14 +859,15 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
     if constexpr (KS > 1) logits(std::integral_constant<int, 1>{});
     if constexpr (KS > 2) logits(std::integral_constant<int, 2>{});
     if constexpr (KS > 3) logits(std::integral_constant<int, 3>{});
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * KS + 2 * Place::words, 0);
-    __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
+    // in this order: reads, the values' scales, and then their conversion beside the products
+    __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * KS + 2 * Place::words, 0);
+    __builtin_amdgcn_sched_group_barrier(kVector, 24, 0);
 #pragma unroll
     for (int i = 0; i < 2 * KS * NP; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
+      __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kVector, 8, 0);
     }
-    asm volatile("" : "+v"(s[0]), "+v"(s[1]));             // (the products stay up there)
+    asm volatile("" : "+v"(s[0]), "+v"(s[1]));             // (the products stay before the loads)
     if (step + 2 < steps) {
       fetch(j + 128);
       pages(j + 192);
@@ -909,11 +915,16 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
       m = top;
     }
     const float base = m == kNegInf ? 0.0f : m;
-    bf16x8 vf[2][CT], p[2][WP];
+    // Operands of values and weights are formed a product ahead, where registers hold two of each
+    // (fp32, four sequences of 700 new tokens and 2,700 keys, ahead | not: 128 channels, of which
+    // 256 registers do not, 193 | 167 us, 192 channels 324 | 335, 256 498 | 509).
+    constexpr bool AHEAD = WP < 3 || W != 128;
+    constexpr int SETS = AHEAD ? 2 : 1;
+    bf16x8 vf[SETS][CT], p[SETS][WP];
     auto values = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
-        vf[v % 2][ct] = *reinterpret_cast<const bf16x8*>(
+        vf[v % SETS][ct] = *reinterpret_cast<const bf16x8*>(
             smem + P * Place::value_bytes + Place::value_at(v_at[Place::column_of(v, ct)], ct));
     };
     auto weights = [&](int v) __attribute__((always_inline)) {
@@ -921,45 +932,53 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
 #pragma unroll
       for (int y = 0; y < 8; ++y)
         w[y] = exp2_fast(fmaf(s[v / 2][v % 2 * 8 + y], c, -base));
-      weight_pieces<WP>(w, p[v % 2]);
+      weight_pieces<WP>(w, p[v % SETS]);
       if constexpr (WP == 1) {
         // one piece: the sum is of the weights as rounded, so that they still sum to 1
         const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[v % 2][0][2 * y], p[v % 2][0][2 * y + 1]},
+          l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[v % SETS][0][2 * y], p[v % SETS][0][2 * y + 1]},
                                               one, l, false);
       } else {
         l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
       }
     };
-    values(0);
-    weights(0);
+    if (AHEAD) {
+      values(0);
+      weights(0);
+    }
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      if (v < 3) values(v + 1);
+      if (!AHEAD) {
+        weights(v);
+        values(v);
+      } else if (v < 3) {
+        values(v + 1);
+      }
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int n = WP - 1; n >= 0; --n)
-          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[v % 2][ct], p[v % 2][n], o[ct], 0, 0,
-                                                          0);
-      if (v < 3) weights(v + 1);
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[v % SETS][ct], p[v % SETS][n], o[ct],
+                                                          0, 0, 0);
+      if (AHEAD && v < 3) weights(v + 1);
     }
-    // (in this order: each operand is read during the products before)
-    constexpr int each = WP == 1 ? 24 : WP == 2 ? 44 : 64;
-    __builtin_amdgcn_sched_group_barrier(0x100, CT, 1);
-    __builtin_amdgcn_sched_group_barrier(0x2, each, 1);
+    if constexpr (AHEAD) {                                 // in this order
+      constexpr int each = WP == 1 ? 24 : WP == 2 ? 44 : 64;   // instructions to form weights
+      __builtin_amdgcn_sched_group_barrier(kLdsReads, CT, 1);
+      __builtin_amdgcn_sched_group_barrier(kVector, each, 1);
 #pragma unroll
-    for (int v = 0; v < 3; ++v) {
-      __builtin_amdgcn_sched_group_barrier(0x100, CT, 1);
+      for (int v = 0; v < 3; ++v) {
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, CT, 1);
 #pragma unroll
-      for (int ct = 0; ct < CT * WP; ++ct) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(0x2, each / (CT * WP), 1);
+        for (int i = 0; i < CT * WP; ++i) {
+          __builtin_amdgcn_sched_group_barrier(kProducts, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(kVector, each / (CT * WP), 1);
+        }
       }
+      __builtin_amdgcn_sched_group_barrier(kProducts, CT * WP, 1);
     }
-    __builtin_amdgcn_sched_group_barrier(0x8, CT * WP, 1);
     __syncthreads();
   };
   for (int step = 0; step < steps; step += 2) {

@@ -1205,15 +1205,14 @@ class Rotary:
     def of(cls, frequencies, interleaved: bool = False, amplitude: float = 1.0,
            device="cuda") -> "Rotary":
         """Of these frequencies (radians a position, 64 bits)."""
-        turns = []
-        for f in frequencies:
-            t = float(f) / (2 * math.pi)
-            if not math.isfinite(t):
-                raise ValueError("a frequency is not finite")
-            n = int(math.ldexp(t - math.floor(t), 64)) % 2 ** 64
-            turns.append(n - 2 ** 64 if n >= 2 ** 63 else n)
-        return cls(torch.tensor(turns, dtype=torch.int64, device=device), 2 * len(turns),
-                   bool(interleaved), float(amplitude))
+        t = np.array([float(f) for f in frequencies]) / (2 * math.pi)
+        if not np.isfinite(t).all():
+            raise ValueError("a frequency is not finite")
+        t -= np.floor(t)
+        t[t == 1.0] = 0.0                                    # (from below 0 by less than a rounding)
+        turns = np.ldexp(t, 64).astype(np.uint64).view(np.int64)
+        return cls(torch.from_numpy(turns).to(device), 2 * len(turns), bool(interleaved),
+                   float(amplitude))
 
     @classmethod
     def make(cls, rot: int, base: float = 10000.0, *, interleaved: bool = False,
