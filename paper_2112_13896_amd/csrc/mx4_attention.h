@@ -676,7 +676,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
   int page[4];
   auto pages = [&](int j) {
 #pragma unroll
-    for (int b = 0; b < (WHOLE ? 1 : 4); ++b) page[b] = mx4_page(table, min(j + 16 * b, hi - 1) >> lg);
+    for (int b = 0; b < (WHOLE ? 1 : 4); ++b)
+      page[b] = mx4_page(table, min(j + 16 * b, hi - 1) >> lg);
   };
   auto page_of = [&](int b) {                              // of the step's block of 16 keys b
     return b == 0 ? page[0] : b == 1 ? page[1] : b == 2 ? page[2] : page[3];
@@ -938,8 +939,8 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
         const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[v % SETS][0][2 * y], p[v % SETS][0][2 * y + 1]},
-                                              one, l, false);
+          l = __builtin_amdgcn_fdot2_f32_bf16(
+              bf16x2{p[v % SETS][0][2 * y], p[v % SETS][0][2 * y + 1]}, one, l, false);
       } else {
         l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
       }
