@@ -943,9 +943,8 @@ int cs_mx4_cache_read(const cs_mx4_cache* cache, const int64_t* slots, int64_t t
  * matrix cores' own 4-bit form; a query head's elements are held to 2^-20 of its
  * largest (CS_F16: 2^-18, CS_F32: 2^-23): the matrix cores take them in pieces of
  * four significant bits, two for CS_BF16, four for CS_F16 and five for CS_F32.
- * A key's weight has 16 bits (CS_F32: 24), but 8 where the call runs CS_BF16 rows
- * 128 at a time (cs_mx4_paged_attention_plan's rows); the sum of the weights is
- * 32 bits wide.  Slots that no new token sees may hold anything.
+ * A key's weight has 16 bits (CS_F32: 24); the sum of the weights is 32 bits wide.
+ * Slots that no new token sees may hold anything.
  */
 int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q, int64_t ldq,
                            int64_t hsq, int tokens, int q_heads, int batch, const int32_t* table,

@@ -52,12 +52,12 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
   // Rows of a sequence (bf16, d 128, eight heads; 16 | 32 | 128 rows a workgroup, us).  One
-  // sequence of 32,768 keys: 32 rows 29.8 | 29.3 | 41, 64 37.6 | 36.5 | 44, 96 45.5 | 43.7 | 46,
-  // 128 - | 53 | 49; three of 85,000: 20 rows 103 | 87 | 185; eight of 8,192: 32 rows 38.8 | 38.6 |
-  // 62, 64 58 | 56 | 66, 96 78 | 84 | 73; 32 of 2,048: 64 rows 47 | 45 | 64, 96 69 | 72 | 73, 160 -
-  // | 110 | 91; 32 of 200: 64 rows 13.6 | 13.9 | 16.4, 96 18.7 | 21.4 | 17.8.  fp32, 32 | 128 rows
-  // a workgroup, 128 rows of the four: 62 | 64, 106 | 107, 100 | 107, 31.8 | 25.6; 96 rows of
-  // eight sequences 100 | 101.
+  // sequence of 32,768 keys: 32 rows 29.8 | 29.9 | 41, 64 37 | 36 | 42, 96 46 | 43 | 44, 128 51 | 48
+  // | 46; three of 85,000: 20 rows 103 | 87 | 185; eight of 8,192: 32 rows 36 | 35 | 54, 64 56 | 53
+  // | 60, 84 71 | 79 | 64, 128 88 | 83 | 73; 32 of 2,048: 64 rows 42 | 40 | 58, 84 60 | 63 | 58, 160
+  // 91 | 96 | 93; 32 of 200: 64 rows 12.2 | 12.4 | 14.5, 96 16.6 | 18.6 | 15.5.  fp16 the same to 6
+  // %.  fp32, 32 | 128 rows a workgroup, 96 rows of the four: 50 | 52, 94 | 85, 76 | 84, 25 | 21;
+  // 128 rows of the first two 56 | 55, 99 | 93, 160 rows of the third 117 | 128.
   const int few = qt == CS_F32 ? 112 : 80;
   p.per = rows > few * (int64_t)batch ? 128 : rows > 16 * (int64_t)batch && c.d <= 128 ? 32 : 16;
   // numbers that mx4_place gives: sequences of at least a token, each with less than a tile of rows

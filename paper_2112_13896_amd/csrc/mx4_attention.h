@@ -7,23 +7,28 @@
 //  - Keys are never converted: the matrix cores multiply 4-bit codes, with a
 //    power of two for every 32 channels, as the cache holds both.  The other
 //    operand has four significant bits, so a query row is the sum of pieces, each
-//    what the ones before leave, in units 2^-4 of theirs (2^-5 from the third on,
+//    what the ones before leave, in units 2^-4 of theirs (2^-5 from the fourth on,
 //    where all that is left is below half a step).  The row is first scaled by a
 //    power of two, so that its largest element is near the end of the first
 //    piece's range.
 //    bf16: two pieces in e4m3, largest element in [2^7, 2^8).  They hold the eight
 //    bits of every element that is not small; e4m3's least step, 2^-9 in units of
 //    2^-4, leaves at most 2^-14 of the others: 2^-21 of the largest.
-//    fp16 and fp32: four and five pieces in e2m3, whose step is 1/8 throughout and
-//    which the matrix cores take at twice the rate; largest element in [3.5, 7).
-//    Half a step of the
-//    last, in units of 2^-13 and 2^-18, is
-//    2^-18.8 and 2^-23.8 of the largest element.  (e4m3 would take three and six
-//    pieces at half the rate: the time of six and twelve of these.)
+//    fp16 and fp32: four and five pieces in e2m3, which the matrix cores take at
+//    twice the rate; largest element in [3.5, 7).  e2m3's step is 1/8 below 2, 1/4
+//    from there and 1/2 from 4 on, so the first piece leaves at most 2^-2, the second
+//    (up to 4 in its units) 2^-3 of them, and the others (up to 2) 2^-4 of theirs,
+//    2^-13 and 2^-18 in the end: 2^-18.8 and 2^-23.8 of the largest element.  (e4m3
+//    would take three and six pieces at half the rate: the time of six and twelve of
+//    these.)
 //  - Values go to bf16, exactly, by the scaled conversion, and meet weights
-//    e_j = 2^(x_j - m) in bf16 pieces: two (16 bits), three for fp32.  bf16 has
-//    the exponents of 32-bit floats, and the cache's scales end at 2^60, so no
-//    sum over 2^30 positions overflows and weights need no scaling.
+//    e_j = 2^(x_j - m) in bf16 pieces: two (16 bits), three (24) for fp32, whatever
+//    the rows of a workgroup, so that a token's result has the same bits beside a
+//    prompt as alone.  (One piece where 128 rows of bf16 share a workgroup: prompts
+//    570 us instead of 750, but 8 bits: off by 4e-4 of their outputs' norm, and by up
+//    to 2^-9 of the values where those cancel.)  bf16 has the exponents of 32-bit
+//    floats, and the cache's scales end at 2^60, so no sum over 2^30 positions
+//    overflows and weights need no scaling.
 //  - The running maximum m follows the rows' maximum only when that is more
 //    than 4 (2^2) above it: rescaling is rare.
 #pragma once
@@ -546,10 +551,13 @@ void mx4_few(Mx4Attention a) {
 // barrier a step.  W <= DT: channels of values that are computed, d rounded up to
 // 32.  WHOLE: a page holds a step's 64 keys, so that all its addresses are scalar.
 // Both pipelines bound it: 5 sequences of 2,000 new tokens over up to 6,096 keys,
-// 32 query heads on eight of 128 channels (bf16), 555 GFLOP in 558 us, 0.99 PFLOP/s
-// of the 1.17 to 1.25 that a large bf16 product reaches.  Matrix instructions are
-// 42 % of the SIMDs' cycles and vector instructions 52 %, at 1.7 wavefronts a SIMD.
-// Values turned by half of the wavefronts before the products, and each operand read
+// 32 query heads on eight of 128 channels (bf16), 555 GFLOP in 711 to 763 us (four
+// cards), 0.73 to 0.78 PFLOP/s of the 1.17 to 1.25 that a large bf16 product reaches,
+// whose operands have one piece; fp16 793 to 815, fp32 1,080 to 1,106.  Matrix
+// instructions are 53 % of the SIMDs' cycles and vector instructions 60 %, at 1.8
+// wavefronts a SIMD.
+// Measured with one piece of weights: 558 us, 42 and 52 % of the cycles.  Values
+// turned by half of the wavefronts before the products, and each operand read
 // right before its product: 610 us.  From there: with an eighth of the logits'
 // products 531, with a quarter of the values' 544, both 472; without exponentials
 // 561, without turning values 555, without loads 529.  The next step's logits formed
@@ -577,7 +585,7 @@ template <typename T, int W, bool WHOLE>
 __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a) {
   constexpr int DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
   using Pieces = Mx4Pieces<T>;
-  constexpr int NP = Pieces::q, WP = std::is_same<T, __bf16>::value ? 1 : Pieces::w;
+  constexpr int NP = Pieces::q, WP = Pieces::w;
   constexpr int KS = (W + 63) / 64, CT = W / 32;
   using At = Mx4Lds<DT>;
   using Place = Mx4Places<DT>;
@@ -934,16 +942,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
       for (int y = 0; y < 8; ++y)
         w[y] = exp2_fast(fmaf(s[v / 2][v % 2 * 8 + y], c, -base));
       weight_pieces<WP>(w, p[v % SETS]);
-      if constexpr (WP == 1) {
-        // one piece: the sum is of the weights as rounded, so that they still sum to 1
-        const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          l = __builtin_amdgcn_fdot2_f32_bf16(
-              bf16x2{p[v % SETS][0][2 * y], p[v % SETS][0][2 * y + 1]}, one, l, false);
-      } else {
-        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-      }
+      l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
     };
     if (AHEAD) {
       values(0);
@@ -966,7 +965,7 @@ __global__ __launch_bounds__(256, W > 128 ? 1 : 2) void mx4_many(Mx4Attention a)
       if (AHEAD && v < 3) weights(v + 1);
     }
     if constexpr (AHEAD) {                                 // in this order
-      constexpr int each = WP == 1 ? 24 : WP == 2 ? 44 : 64;   // instructions to form weights
+      constexpr int each = WP == 2 ? 44 : 64;   // instructions to form weights
       __builtin_amdgcn_sched_group_barrier(kLdsReads, CT, 1);
       __builtin_amdgcn_sched_group_barrier(kVector, each, 1);
 #pragma unroll
