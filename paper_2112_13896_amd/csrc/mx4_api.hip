@@ -51,6 +51,10 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
                              int batch, int table_width, int max_len, int window) {
   AttentionPlan p;
   const int64_t group = q_heads / c.heads, rows = tokens * group;
+  // Sequences with tokens, at most.  The other entries of a padded batch have no work, and counted
+  // as sequences they took the parts from those that have (three tokens over 100,000 keys each in
+  // a table of 256 entries 871 us, 63 so; five over 8,192 in 64 entries 43.6, 20.7).
+  const int64_t seqs = std::min(batch, tokens);
   // Rows of a sequence (bf16, d 128, eight heads; 16 | 32 | 128 rows a workgroup, us).  One
   // sequence of 32,768 keys: 32 rows 29.8 | 29.9 | 41, 64 37 | 36 | 42, 96 46 | 43 | 44, 128 51 | 48
   // | 46; three of 85,000: 20 rows 103 | 87 | 185; eight of 8,192: 32 rows 36 | 35 | 54, 64 56 | 53
@@ -59,10 +63,9 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
   // %.  fp32, 32 | 128 rows a workgroup, 96 rows of the four: 50 | 52, 94 | 85, 76 | 84, 25 | 21;
   // 128 rows of the first two 56 | 55, 99 | 93, 160 rows of the third 117 | 128.
   const int few = qt == CS_F32 ? 112 : 80;
-  p.per = rows > few * (int64_t)batch ? 128 : rows > 16 * (int64_t)batch && c.d <= 128 ? 32 : 16;
+  p.per = rows > few * seqs ? 128 : rows > 16 * seqs && c.d <= 128 ? 32 : 16;
   // numbers that mx4_place gives: sequences of at least a token, each with less than a tile of rows
   // that are not there, in steps of what divides both
-  const int64_t seqs = std::min(batch, tokens);
   p.tiles = (rows + seqs * (p.per - std::gcd(group, (int64_t)p.per))) / p.per;
   int64_t len = (int64_t)table_width << c.page_log;
   if (max_len > 0) len = std::min<int64_t>(len, max_len);
@@ -74,8 +77,8 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
   // long to join as a second part saves (32 sequences of 2,048 keys: whole 74 us, two parts 102;
   // eight of 8,192 in four parts 93, in eight 79).  Short axes stay whole: the join is a launch of
   // its own (1,500 keys of one sequence 12.2 us, 14.3 in parts).
-  const int64_t per_seq = (rows + batch - 1) / batch;
-  const int64_t items = batch * ((per_seq + p.per - 1) / p.per) * c.heads;
+  const int64_t per_seq = (rows + seqs - 1) / seqs;
+  const int64_t items = seqs * ((per_seq + p.per - 1) / p.per) * c.heads;
   const int wgs = p.per > 16 || c.d > 128 ? 2 : qt == CS_F32 ? 3 : 4;
   int64_t splits = std::min<int64_t>({256 * wgs / items, len / 256, cs::kMaxSplits});
   if (splits < (p.per == 128 ? 3 : 1) || len <= 2048) splits = 1;
