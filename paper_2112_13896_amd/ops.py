@@ -1391,7 +1391,7 @@ def plan_step(pool: DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: i
         p_starts = p_lens + 4 * batch
         p_positions = p_starts + 4 * batch + 4
         p_status = p_positions + 4 * tokens
-        if own:
+        if ws is None:
             pws, nws = at + 4 * (words + pad), own
         else:
             _, pws, nws = _ws(ws, None, seqs.device, gpu)
