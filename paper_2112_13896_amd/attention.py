@@ -22,6 +22,7 @@ from __future__ import annotations
 
 from dataclasses import dataclass, field
 
+import numpy as np
 import torch
 
 from . import ops
@@ -82,20 +83,27 @@ class Step:
         for s, n in zip(seqs, new):
             if not 0 <= n <= s.length or len(s.pages) * page < s.length:
                 raise ValueError("a sequence lacks the tokens or pages that the step needs")
-        width = max(width, 1, max(len(s.pages) for s in seqs))
-        table = torch.full((len(seqs), width), -1, dtype=torch.int32)
-        starts = torch.zeros(len(seqs) + 1, dtype=torch.int32)
-        slots, positions = [], []
-        for i, (s, n) in enumerate(zip(seqs, new)):
-            table[i, :len(s.pages)] = torch.tensor(s.pages, dtype=torch.int32)
-            starts[i + 1] = starts[i] + n
-            slots += [s.pages[j // page] * page + j % page for j in range(s.length - n, s.length)]
-            positions += range(s.length - n, s.length)
-        lens = torch.tensor([s.length for s in seqs], dtype=torch.int32)
-        return cls(table.to(device), lens.to(device), starts.to(device),
-                   torch.tensor(slots, dtype=torch.int64).to(device),
-                   max(s.length for s in seqs),
-                   torch.tensor(positions, dtype=torch.int32).to(device))
+        batch, width = len(seqs), max(width, 1, max(len(s.pages) for s in seqs))
+        tokens, fresh = int(sum(new)), np.array(new, dtype=np.int32)
+        # parts of one buffer, so that a step is one copy to the device, positions among it
+        sizes = (2 * tokens, batch * width, batch, batch + 1, tokens)
+        host = np.empty(sum(sizes), dtype=np.int32)
+        slots, table, lens, starts, positions = np.split(host, np.cumsum(sizes)[:-1])
+        slots, table = slots.view(np.int64), table.reshape(batch, width)
+        table.fill(-1)
+        for i, s in enumerate(seqs):
+            table[i, :len(s.pages)] = s.pages
+        lens[:] = [s.length for s in seqs]
+        starts[0] = 0
+        np.cumsum(fresh, out=starts[1:])
+        # token t of sequence i is at position t - starts[i] + lens[i] - new[i]
+        positions[:] = np.arange(tokens) + np.repeat(lens - starts[1:], fresh)
+        slots[:] = table[np.repeat(np.arange(batch), fresh), positions // page]
+        slots *= page
+        slots += positions % page
+        slots, table, lens, starts, positions = torch.from_numpy(host).to(device).split(sizes)
+        return cls(table.view(batch, width), lens, starts, slots.view(torch.int64),
+                   max(s.length for s in seqs), positions)
 
     @classmethod
     def plan(cls, pool: ops.DevicePool, seqs: torch.Tensor, new: torch.Tensor, tokens: int,
