@@ -111,10 +111,12 @@ class Step:
              into: "Step | None" = None) -> "Step":
         """The step in which new[i] tokens come to sequence seqs[i] of the pool, planned by a kernel
         (ops.plan_step): of up to `tokens` tokens, padded to that many, and sequences of up to
-        max_len positions as far as the caller knows.  `into`: an earlier step of these sizes,
+        max_len positions as far as the caller knows.  `into`: an earlier planned step of these sizes,
         overwritten and returned.  The step's status is 0, 0 unless the pool could not give it."""
         out = None
         if into is not None:
+            if into.positions is None or into.status is None:
+                raise ValueError("into must be a step planned on the GPU")
             out = (into.table, into.lens, into.starts, into.slots, into.positions, into.status)
         table, lens, starts, slots, positions, status = ops.plan_step(pool, seqs, new, tokens,
                                                                       width, ws, out)

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2112_13896_amd import _lib, ops
+from paper_2112_13896_amd.attention import Sequence, Step
 from tests.test_q8_devices_cpu import at
 
 I32 = torch.int32
@@ -37,3 +38,14 @@ def test_a_step_of_too_many_entries(stream, own):
         ops.plan_step(_pool(), seqs, seqs, 5, 1, ws=ws, out=out)
     with pytest.raises(_lib.CSError, match="cs_pool_truncate"):
         ops.pool_truncate(_pool(), seqs)
+
+
+def test_into_a_step_of_the_hosts(stream):
+    """It has no status to write."""
+    seqs = at(0, 1, dtype=I32)
+    host = Step.of([Sequence([0], 3)], [2], 16, device="cpu", width=3)
+    with pytest.raises(ValueError, match="into"):
+        Step.plan(_pool(), seqs, seqs, 2, 16, into=host)
+    host.positions, host.status = None, at(0, 2, dtype=I32)
+    with pytest.raises(ValueError, match="into"):
+        Step.plan(_pool(), seqs, seqs, 2, 16, into=host)
