@@ -18,10 +18,13 @@ namespace {
 
 constexpr int kMaxRotaryHeads = 65535, kMaxRotaryD = 1024;
 constexpr int kMaxBatch = 1 << 20;
-// Cells and tokens of a step that the workgroup which plans it writes itself: 64 entries of 160
-// columns 7.9 us, 4.0 + 2.2 and the host's second launch (3 us) otherwise; 1,001 entries of 600
-// columns 390 us against 4.0 + 6.2.
-constexpr int64_t kFillItems = 32768;
+// Cells and tokens of a step that the workgroup which plans it writes itself.  One launch | two, us
+// a call, eager and then recorded (16 to 600 columns, which differ by less than 1 us): 4,000 items
+// 9.2 | 12.0, 5.9 | 5.9; 8,000 9.1 | 12.3, 7.8 | 6.0; 12,000 9.5 | 12.2, 8.9 | 6.0; 14,000 9.7 | 12.2,
+// 9.3 | 6.1; 16,000 10.7 | 12.3, 10.4 | 6.0; 20,000 12.0 | 12.3, 11.7 | 5.9; 32,000 16.1 | 12.5, 15.8
+// | 5.9.  Eager calls would draw the line at 20,000 and recorded ones at 4,000; here one kind loses
+// as much as the other gains.
+constexpr int64_t kFillItems = 12288;
 
 template <typename T, int N, bool NEIGHBOURS>
 int rotary_launch(cs::Rotary a, hipStream_t s) {
