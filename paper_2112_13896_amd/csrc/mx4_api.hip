@@ -74,8 +74,8 @@ AttentionPlan attention_plan(const cs::Mx4View& c, cs_dtype qt, int tokens, int 
   // registers are more).  More make sequences of unequal length even out better, but parts have to
   // be joined: 96 sequences of up to 12,000 keys 144 us so, 140 at twice as many, 135 at three
   // times; 96 of 6,000 108 | 117 | 123; 128 of 4,500 107 | 118 | 124.  128 rows take 1.5 times as
-  // long to join as a second part saves (32 sequences of 2,048 keys: whole 74 us, two parts 102;
-  // eight of 8,192 in four parts 93, in eight 79).  Short axes stay whole: the join is a launch of
+  // long to join as a second part saves (with weights of one piece, 32 sequences of 2,048 keys: whole
+  // 74 us, two parts 102; eight of 8,192 in four parts 93, in eight 79).  Short axes stay whole: the join is a launch of
   // its own (1,500 keys of one sequence 12.2 us, 14.3 in parts).
   const int64_t per_seq = (rows + seqs - 1) / seqs;
   const int64_t items = seqs * ((per_seq + p.per - 1) / p.per) * c.heads;
@@ -247,7 +247,7 @@ int cs_mx4_paged_attention(const cs_mx4_cache* cache, cs_dtype qt, const void* q
     auto many = [&](auto dt) {
       constexpr int W = decltype(dt)::value, DT = W <= 64 ? 64 : W <= 128 ? 128 : 256;
       // a page that holds a step's 64 keys: one scalar address (four sequences of 700 tokens over
-      // 2,700 keys 92 us, 104 with an address for every 16 keys)
+      // 2,700 keys 169 us, 182 and 196 with an address for every 16 keys at pages of 32 and 16)
       if (c.page_log >= 6)
         hipLaunchKernelGGL((cs::mx4_many<T, W, true>), grid, dim3(256), cs::Mx4Lds<DT>::bytes, s,
                            a);

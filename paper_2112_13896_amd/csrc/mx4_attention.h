@@ -243,8 +243,11 @@ __device__ __forceinline__ void mx4_rest(const Mx4Attention& a) {
 // loads with no arithmetic take 123 us and the arithmetic with no loads 103.  What
 // is read once does not stay in the L2 (nontemporal: 157 us without).  With 32 rows
 // (RT 2) the keys' arithmetic serves both halves: three sequences of 70,000 to
-// 100,000 keys in fp16, 284 MB in 80 us, 3.6 TB/s, bound by turning values to bf16
-// and by weights.  One step's loads are on their way at a time, of all wavefronts: a
+// 100,000 keys in fp16, 284 MB in 82 us, 3.5 TB/s.  There its loads alone take 47 us and
+// its arithmetic alone 56, which 1.5 wavefronts a SIMD overlap too little; no part
+// stands out (of 82: one of four pieces of a query 75, one of two of a weight 73,
+// values not turned 79, no exponentials 80), vector instructions are 50 % of the
+// SIMDs' cycles and matrix instructions 25 %.  One step's loads are on their way at a time, of all wavefronts: a
 // second set in registers gained nothing (140 us, 84).
 //  A wavefront takes 32 keys a step, every NW-th step of the
 // workgroup's part of the key axis, straight from memory to registers.
@@ -563,7 +566,10 @@ void mx4_few(Mx4Attention a) {
 // 561, without turning values 555, without loads 529.  The next step's logits formed
 // beside this step's weights, with keys two steps ahead, took 657; a higher wave
 // priority during the products 640.  Where pages are shorter than a step: 700 tokens
-// of four sequences over 2,700 keys 102 us (92 where they are not).
+// of four sequences over 2,700 keys, the same heads, 182 us at pages of 32 and 196
+// of 16 (169 where they are not).  Registers spill in <float, 256> (38, 68 where
+// pages are shorter), <fp16, 256> and <fp16, 128> (13 and 4, shorter pages alone)
+// and <float, 96> (2); in none for bf16.
 // Lane = 32 h + r.  Logits (32 keys x 32 rows): keys 8 y + 4 h .. +3 (y = 0..3) of
 // row r.  So a lane's eight weights of 16 keys are those at 4 h .. and 8 + 4 h ..,
 // and the values' chunk g = 2 s + h of a channel holds just the keys 16 s + 4 h ..

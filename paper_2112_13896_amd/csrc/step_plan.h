@@ -182,7 +182,11 @@ __device__ __forceinline__ void plan_token(const PlanStep& a, const Planned& f, 
 // FILL, this workgroup also writes the cells and tokens.  Latency bounds it: it
 // reads and writes some 30 bytes an entry.  1,001 entries take 4.0 us (11 with sums by
 // 64-bit atomics in LDS); 64 entries with a token and 160 pages each 8 us, cells and
-// tokens in the same launch.
+// tokens in the same launch, where each of ten rounds of cells waits for its entries'
+// sequences, then for the table.  Past 1,024 entries the sequences are marked in
+// memory and the entries read four times, 1,024 at a time: with the cut that takes the
+// step back, a token each, 1,024 entries 18 us, 1,025 29, 5,000 79, 20,000 292,
+// 100,000 1,546.
 template <bool SMALL, bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void plan_scan(PlanStep a) {
   __shared__ int l_wrong;
@@ -312,7 +316,8 @@ __global__ __launch_bounds__(256) void plan_fill(PlanStep a) {
 
 // Pages past the new lengths back onto the stack: entry after entry from the
 // top down, so one workgroup adds up how many there are and then moves them.
-// SMALL as above.  2.3 us where few pages move, 7.5 for 1,001 entries.
+// SMALL as above.  2.3 us where few pages move, 7.5 for 1,001 entries, whose every
+// page is looked up among the entries by halving.
 template <bool SMALL>
 __global__ __launch_bounds__(kPlanThreads) void pool_truncate(PoolView p, const int32_t* seqs,
                                                               const int32_t* lens, int batch) {
